@@ -503,6 +503,138 @@ int mustafar_window_step_grouped(mustafar_window_t* w, mustafar_ccache_t* Kc, mu
                                  const void* k_new, const void* v_new, const void* active,
                                  float* acc, void* stream);
 
+/* THE PAGED DENSE CACHE. A prompt arrives in chunks, for many requests at once;
+ * until its tokens are compressed, their keys and values lie dense in pages of a
+ * pool that all requests share, and every chunk attends to the pages of its
+ * request. A step of a serving loop is mustafar_paged_plan (tables and slots from
+ * the requests' lengths), mustafar_paged_write (the step's keys and values),
+ * mustafar_paged_attn (its queries), per layer; a request whose prompt is done goes
+ * through mustafar_paged_gather to mustafar_window_prefill or
+ * mustafar_prune_compress.
+ *   k, v      pages of fp16 or bf16 (type), 16-byte aligned: token o of page p and
+ *             kv-head h has its d channels at element p * page_stride +
+ *             h * head_stride + o * token_stride (strides in elements, multiples of
+ *             8: [n_pages][H][P][d] and [n_pages][P][H][d] are both pages)
+ *   table     [B][max_pages] int32: page i of entry b holds its tokens
+ *             i * P .. i * P + P - 1, P = page_tokens
+ *   state     [B + 2] int32: the tokens that each entry holds, the number of free
+ *             pages, and a word that mustafar_paged_plan uses (zeroed by the caller
+ *             once, left 0 by every call)
+ *   free_pages [n_pages] int32: a stack of free pages, the top at index count - 1
+ * All are device memory of the caller, who sets them for an empty cache (lengths 0,
+ * n_pages free pages, every page on the stack; tables need no setting). */
+enum mustafar_type { MUSTAFAR_FP16 = 0, MUSTAFAR_BF16 = 1 };
+
+#define MUSTAFAR_PAGED_MAX_BATCH 4096       /* entries of a paged cache               */
+#define MUSTAFAR_PAGED_MAX_STEP (1 << 19)   /* slots of a step, and pages of an entry */
+#define MUSTAFAR_PAGED_MAX_GROUP 64         /* query heads per kv-head                */
+
+typedef struct mustafar_pages {
+    void* k;
+    void* v;
+    int32_t* table;
+    int32_t* state;
+    int32_t* free_pages;
+    int32_t B, H, d;          /* entries, kv-heads, head dimension (64, 128, 256)  */
+    int32_t page_tokens;      /* 16 to 1024, a power of two                        */
+    int32_t n_pages;          /* n_pages * page_tokens < 2^31                      */
+    int32_t max_pages;        /* of an entry                                       */
+    int32_t type;             /* mustafar_type of k and v                          */
+    int64_t page_stride, head_stride, token_stride;
+} mustafar_pages_t;
+
+/* Fills *p for caller-allocated buffers (host only; touches no buffer). Errors:
+ * EINVAL (pointers, alignment, sizes, a page's rows that overlap, a page of 2^31
+ * bytes or more). */
+int mustafar_paged_init(mustafar_pages_t* p, void* k, void* v, void* table, void* state,
+                        void* free_pages, int B, int H, int d, int page_tokens, int n_pages,
+                        int max_pages, int type, int64_t page_stride, int64_t head_stride,
+                        int64_t token_stride);
+
+/* Page status word of mustafar_paged_plan: 0, or the sum of */
+#define MUSTAFAR_PLAN_PAGES 1  /* too few free pages                                  */
+#define MUSTAFAR_PLAN_TABLE 2  /* an entry would need more than max_pages pages       */
+#define MUSTAFAR_PLAN_SLOTS 4  /* more than n_slots new tokens                        */
+#define MUSTAFAR_PLAN_STATE 8  /* a negative new_len, or a state that is none         */
+
+/* One step's block tables, slots and sequence starts from the entries' lengths.
+ * Entry b holds len = p->state[b] tokens in ceil(len / P) pages; the step keeps the
+ * first min(max(keep[b], 0), len) of them (keep NULL: all; 0 takes the entry from one
+ * request to the next, less than len takes tokens back) and adds new_len[b]. Pages
+ * that are given up go on the free stack, the last entry's last page first; pages
+ * that are needed are then taken off its top, for entry 0 first, and entered in the
+ * table (so a step that is taken back leaves the stack as it was). Then
+ *   state_out [B + 2]  the new lengths, the new number of free pages, 0
+ *   cu [B + 1]         cu[b] = the sum of new_len over the entries before b
+ *   slots [n_slots]    slots[cu[b] + i] = page * P + place of the i-th new token of
+ *                      entry b; -1 from cu[B] on
+ *   status [1]         0
+ * A step that cannot be planned (see the bits above) writes its status, state_out =
+ * state, cu = 0 and slots = -1 and changes neither tables nor the stack. state_out is
+ * p->state (the step is taken in place) or does not overlap it (the caller's next
+ * step, planned while kernels still read the present lengths; the tables' and the
+ * stack's entries that the present state uses stay as they are). All pointers are
+ * int32 device memory; keep and new_len have B elements and do not overlap the
+ * outputs. Errors: EINVAL (descriptor, pointers, n_slots < 0 or >
+ * MUSTAFAR_PAGED_MAX_STEP; slots may be NULL when n_slots == 0). */
+int mustafar_paged_plan(const mustafar_pages_t* p, const void* keep, const void* new_len,
+                        void* state_out, void* cu, void* slots, int n_slots, void* status,
+                        void* stream);
+
+/* Writes the keys and values of n_new tokens into their slots. k_new, v_new: the
+ * cache's type, 16-byte aligned, token t's H * d elements at t * k_stride (v_stride),
+ * multiples of 8 and at least H * d (a packed projection is read in place). slots
+ * [n_new] int32: tokens whose slot is outside [0, n_pages * P) are left out, so the
+ * slots of a padded step can be passed whole; the others are distinct. Errors: EINVAL
+ * (n_new < 0, pointers, alignment, strides). */
+int mustafar_paged_write(const mustafar_pages_t* p, const void* k_new, int64_t k_stride,
+                         const void* v_new, int64_t v_stride, const void* slots, int n_new,
+                         void* stream);
+
+/* The entries' tokens as dense fp16 tensors, the input of mustafar_window_prefill and
+ * mustafar_prune_compress: x_k, x_v [B][H][n_max][d], row j of entry b its token
+ * first[b] + j (first: int32 device [B], NULL: 0) for the tokens it holds; rows behind
+ * the last are left as they were. bf16 is rounded to the nearest fp16, magnitudes
+ * over 65504 to 65504 (the compression takes finite inputs), NaN stays NaN. Errors:
+ * EINVAL (n_max < 0, pointers, alignment). */
+int mustafar_paged_gather(const mustafar_pages_t* p, const void* first, void* x_k, void* x_v,
+                          int n_max, void* stream);
+
+/* Device workspace of mustafar_paged_attn for these sizes (0: none needed). n_splits
+ * <= 0 sizes for the split that such a call takes. 0 for invalid arguments. */
+size_t mustafar_paged_attn_workspace_bytes(const mustafar_pages_t* p, int Hq, int n_q, int max_q,
+                                           int max_tokens, int n_splits);
+
+/* Causal attention of every entry's new tokens over its pages, single tokens and
+ * chunks of prompts alike. cu [B + 1] (int32 device, ascending from 0) divides the
+ * n_q rows of q among the entries; the rows of entry b are its last cu[b+1] - cu[b]
+ * tokens, row i at position pos = state[b] - (cu[b+1] - cu[b]) + i. It sees token j
+ * of its entry if
+ *   j <= pos  and  (window == 0  or  j > pos - window  or  j < sinks)
+ * (a sliding window of the newest `window` tokens, itself among them, and the first
+ * `sinks` tokens, which stay visible), and for query head h (kv-head h / (Hq/H))
+ *   out = softmax over the visible tokens of (scale * q.k) . v
+ *   q    rows of Hq * d elements, row t at t * q_stride; the cache's type, 16-byte
+ *        aligned, stride a multiple of 8
+ *   out  the same type and layout with out_stride, rounded once from fp32; does not
+ *        overlap q. A row that sees nothing (pos < 0) is 0, rows from cu[B] on are
+ *        left as they were
+ *   scale  <= 0 selects 1/sqrt(d)
+ *   max_q, max_tokens  bounds of an entry's new tokens and of state[b] for the choice
+ *        of kernel and split; larger ones give the same result, later
+ *   n_splits  ranges of an entry's visible tokens processed in parallel (<= 0: by the
+ *        sizes); ws: mustafar_paged_attn_workspace_bytes, 16-byte aligned
+ * Only tokens that a row sees take part: others may hold infinities or NaN, and table
+ * entries of pages that no row sees need not be valid. (An entry outside [0, n_pages)
+ * is read as page 0, and a length as at most max_pages * P.) Probabilities are
+ * rounded to the cache's type for the product with the values, the softmax's maximum,
+ * sum and output are held in fp32. Errors: EINVAL, EUNSUPPORTED (Hq/H over
+ * MUSTAFAR_PAGED_MAX_GROUP), EWORKSPACE. */
+int mustafar_paged_attn(const void* q, int64_t q_stride, int n_q, int Hq, const mustafar_pages_t* p,
+                        const void* cu, int window, int sinks, float scale, void* out,
+                        int64_t out_stride, int max_q, int max_tokens, int n_splits, void* ws,
+                        size_t ws_bytes, void* stream);
+
 /* Static message for a status code. */
 const char* mustafar_strerror(int status);
 

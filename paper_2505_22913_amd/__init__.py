@@ -58,9 +58,22 @@ class prune_opts_t(ctypes.Structure):
                 ("weights", ctypes.c_void_p)]
 
 
+class pages_t(ctypes.Structure):
+    """Mirror of ``mustafar_pages_t``."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("state", ctypes.c_void_p), ("free_pages", ctypes.c_void_p),
+                ("B", ctypes.c_int32), ("H", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("page_tokens", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("type", ctypes.c_int32),
+                ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64)]
+
+
 PRUNE_MAGNITUDE, PRUNE_2_4, PRUNE_OUTPUT_AWARE = 0, 1, 2
 PRUNE_CHANNEL, PRUNE_CHANNEL_OUTPUT_AWARE = 3, 4
 ATTN_SPARSE, ATTN_DENSE = 0, 1
+FP16, BF16 = 0, 1
+PLAN_PAGES, PLAN_TABLE, PLAN_SLOTS, PLAN_STATE = 1, 2, 4, 8   # status bits of mustafar_paged_plan
 GROUP = 32  # tokens per group of per-channel value pruning
 
 _SIGS = {
@@ -151,6 +164,21 @@ _SIGS = {
                                           ctypes.POINTER(prune_opts_t), ctypes.c_void_p]),
     "mustafar_query_lookahead": (ctypes.c_int, [ctypes.c_void_p] + [ctypes.c_int] * 6
                                  + [ctypes.c_void_p, ctypes.c_void_p]),
+    "mustafar_paged_init": (ctypes.c_int, [ctypes.POINTER(pages_t)] + [ctypes.c_void_p] * 5
+                            + [ctypes.c_int] * 7 + [ctypes.c_int64] * 3),
+    "mustafar_paged_plan": (ctypes.c_int, [ctypes.POINTER(pages_t)] + [ctypes.c_void_p] * 5
+                            + [ctypes.c_int] + [ctypes.c_void_p] * 2),
+    "mustafar_paged_write": (ctypes.c_int, [ctypes.POINTER(pages_t), ctypes.c_void_p, ctypes.c_int64,
+                                            ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                            ctypes.c_int, ctypes.c_void_p]),
+    "mustafar_paged_gather": (ctypes.c_int, [ctypes.POINTER(pages_t)] + [ctypes.c_void_p] * 3
+                              + [ctypes.c_int, ctypes.c_void_p]),
+    "mustafar_paged_attn_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(pages_t)] + [ctypes.c_int] * 5),
+    "mustafar_paged_attn": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_int,
+                                           ctypes.POINTER(pages_t), ctypes.c_void_p, ctypes.c_int,
+                                           ctypes.c_int, ctypes.c_float, ctypes.c_void_p, ctypes.c_int64,
+                                           ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_void_p,
+                                           ctypes.c_size_t, ctypes.c_void_p]),
     "mustafar_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     "mustafar_stream_read_sink_bytes": (ctypes.c_size_t, []),
     "mustafar_stream_read": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p,
@@ -566,6 +594,197 @@ def mustafar_window_step_grouped(win: DenseWindow, Kc: CompressedCache, Vc: Comp
     _check("mustafar_window_step_grouped", lib().mustafar_window_step_grouped(
         ctypes.byref(win.desc), ctypes.byref(Kc.desc), ctypes.byref(Vc.desc), _dptr(k_new),
         _dptr(v_new), _dptr(active), _dptr(acc), _stream(stream)))
+
+
+# ---- the paged dense cache ----------------------------------------------------------------
+class PagedCache:
+    """Dense keys and values of B requests in pages of a shared pool, with the C descriptor.
+
+    k, v [n_pages][H][page_tokens][d] (fp16 or bf16), table [B][max_pages], state [B + 2]
+    (the requests' lengths, the free pages, a word of the library's) and free [n_pages] (the
+    stack of free pages), int32. Tensors that are given are used as they are (k and v in any
+    order of pages, heads and tokens whose channels are contiguous); the others are made, for an
+    empty cache. max_pages: pages of the longest request (default: all).
+    """
+
+    def __init__(self, B: int, H: int, d: int, n_pages: int, page_tokens: int = 64, max_pages: int | None = None,
+                 dtype=None, device="cuda", k=None, v=None, table=None, state=None, free=None):
+        import torch
+        dtype = dtype or (k.dtype if k is not None else torch.float16)
+        types = {torch.float16: FP16, torch.bfloat16: BF16}
+        if dtype not in types:
+            raise ValueError(f"pages hold float16 or bfloat16, not {dtype}")
+        device = k.device if k is not None else device
+        if max_pages is None:
+            max_pages = table.shape[1] if table is not None else n_pages
+        if k is None:
+            k = torch.zeros((n_pages, H, page_tokens, d), dtype=dtype, device=device)
+        if v is None:
+            v = torch.zeros_like(k)
+        if table is None:
+            table = torch.zeros((B, max_pages), dtype=torch.int32, device=device)
+        if state is None:
+            state = torch.zeros(B + 2, dtype=torch.int32, device=device)
+            state[B] = n_pages
+        if free is None:
+            free = torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device)
+        for name, x in (("k", k), ("v", v)):
+            if tuple(x.shape) != (n_pages, H, page_tokens, d) or x.dtype != dtype or x.stride(3) != 1:
+                raise ValueError(f"{name}: [{n_pages}][{H}][{page_tokens}][{d}] of {dtype} with contiguous channels expected")
+        if k.stride() != v.stride():
+            raise ValueError("k and v have the same strides")
+        for name, x, shape in (("table", table, (B, max_pages)), ("state", state, (B + 2,)), ("free", free, (n_pages,))):
+            _want(name, x, shape, torch.int32, k.device)
+        _want("v", v, tuple(k.shape), dtype, k.device, dense=False)
+        self.k, self.v, self.table, self.state, self.free = k, v, table, state, free
+        self.dtype, self.device = dtype, k.device
+        self.desc = pages_t()
+        _check("mustafar_paged_init", lib().mustafar_paged_init(
+            ctypes.byref(self.desc), _dptr(k), _dptr(v), _dptr(table), _dptr(state), _dptr(free), B, H, d,
+            int(page_tokens), int(n_pages), int(max_pages), types[dtype], k.stride(0), k.stride(1), k.stride(2)))
+
+    @property
+    def B(self) -> int:
+        return self.desc.B
+
+    @property
+    def page_tokens(self) -> int:
+        return self.desc.page_tokens
+
+    @property
+    def lens(self):
+        """The requests' lengths (a view of the state)."""
+        return self.state[:self.desc.B]
+
+
+def _want(name, x, shape, dtype, device, dense=True):
+    """Raises unless x is a tensor of this shape, type and device, contiguous if `dense`."""
+    if tuple(x.shape) != tuple(shape) or x.dtype != dtype or (dense and not x.is_contiguous()):
+        raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} expected, "
+                         f"not {x.dtype} {tuple(x.shape)}")
+    if x.device != device:
+        raise ValueError(f"{name} is on {x.device}, the cache on {device}")
+
+
+def _paged_device(cache, *tensors):
+    """The cache's device is the current one (the launches go there) and holds every tensor."""
+    import torch
+    if cache.device.index != torch.cuda.current_device():
+        raise ValueError(f"the cache is on {cache.device}, the current device is cuda:{torch.cuda.current_device()}")
+    for x in tensors:
+        if x is not None and x.device != cache.device:
+            raise ValueError(f"a tensor is on {x.device}, the cache on {cache.device}")
+
+
+def _rows(name, x, heads, d, dtype):
+    """Stride of the rows of x [n][heads][d], whose rows are contiguous."""
+    if x.dim() != 3 or tuple(x.shape[1:]) != (heads, d) or x.dtype != dtype:
+        raise ValueError(f"{name}: [n][{heads}][{d}] of {dtype} expected, not {tuple(x.shape)} of {x.dtype}")
+    if x.shape[0] and (x.stride(2) != 1 or (heads > 1 and x.stride(1) != d)):
+        raise ValueError(f"{name}: rows of {heads} x {d} contiguous elements expected")
+    return x.stride(0) if x.shape[0] > 1 else heads * d
+
+
+def _on_stream(stream):
+    """Allocations of a call go to the stream that it works on."""
+    import contextlib
+    import torch
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def mustafar_paged_plan(cache: PagedCache, new_len, n_slots: int, keep=None, state_out=None, cu=None, slots=None,
+                        status=None, stream=None):
+    """A step's pages, sequence starts and slots: new_len [B] (int32, device) new tokens behind the
+    first keep [B] of every request (None: all it holds). Returns cu [B + 1] and slots [n_slots]. The
+    cache's state advances in place, or is written to state_out [B + 2]. status [1] is 0, or PLAN_
+    bits of a step that was refused and changed nothing."""
+    import torch
+    B, i32 = cache.desc.B, torch.int32
+    _paged_device(cache, new_len, keep, state_out, cu, slots, status)
+    with _on_stream(stream):
+        cu = torch.empty(B + 1, dtype=i32, device=cache.device) if cu is None else cu
+        slots = torch.empty(n_slots, dtype=i32, device=cache.device) if slots is None else slots
+        status = torch.empty(1, dtype=i32, device=cache.device) if status is None else status
+    state_out = cache.state if state_out is None else state_out
+    for name, x, n in (("new_len", new_len, B), ("keep", keep, B), ("state_out", state_out, B + 2), ("cu", cu, B + 1),
+                       ("slots", slots, n_slots), ("status", status, 1)):
+        if x is not None:
+            _want(name, x, (n,), i32, cache.device)
+    _check("mustafar_paged_plan", lib().mustafar_paged_plan(
+        ctypes.byref(cache.desc), _dptr(keep), _dptr(new_len), _dptr(state_out), _dptr(cu), _dptr(slots),
+        int(n_slots), _dptr(status), _stream(stream)))
+    return cu, slots
+
+
+def mustafar_paged_write(cache: PagedCache, k_new, v_new, slots, stream=None) -> None:
+    """k_new, v_new [n][H][d] (the cache's type; rows of a packed projection too) into their slots
+    [n] (int32; negative: left out)."""
+    import torch
+    n, H, d = int(k_new.shape[0]), cache.desc.H, cache.desc.d
+    _paged_device(cache, k_new, v_new, slots)
+    ks, vs = _rows("k_new", k_new, H, d, cache.dtype), _rows("v_new", v_new, H, d, cache.dtype)
+    if v_new.shape[0] != n:
+        raise ValueError("as many values as keys")
+    _want("slots", slots, (n,), torch.int32, cache.device)
+    _check("mustafar_paged_write", lib().mustafar_paged_write(
+        ctypes.byref(cache.desc), _dptr(k_new), ks, _dptr(v_new), vs, _dptr(slots), n, _stream(stream)))
+
+
+def mustafar_paged_gather(cache: PagedCache, n_max: int, first=None, x_k=None, x_v=None, stream=None):
+    """The requests' tokens first[b] (int32 [B], None: 0) .. as dense fp16 x_k, x_v [B][H][n_max][d], the
+    input of mustafar_window_prefill; rows behind a request's last are left as they were (0 in
+    tensors that the call makes)."""
+    import torch
+    shape = (cache.desc.B, cache.desc.H, int(n_max), cache.desc.d)
+    _paged_device(cache, first, x_k, x_v)
+    with _on_stream(stream):
+        x_k = torch.zeros(shape, dtype=torch.float16, device=cache.device) if x_k is None else x_k
+        x_v = torch.zeros(shape, dtype=torch.float16, device=cache.device) if x_v is None else x_v
+    _want("x_k", x_k, shape, torch.float16, cache.device)
+    _want("x_v", x_v, shape, torch.float16, cache.device)
+    if first is not None:
+        _want("first", first, (shape[0],), torch.int32, cache.device)
+    _check("mustafar_paged_gather", lib().mustafar_paged_gather(
+        ctypes.byref(cache.desc), _dptr(first), _dptr(x_k), _dptr(x_v), shape[2], _stream(stream)))
+    return x_k, x_v
+
+
+def mustafar_paged_attn_workspace_bytes(cache: PagedCache, Hq: int, n_q: int, max_q: int, max_tokens: int,
+                                        n_splits: int = 0) -> int:
+    return lib().mustafar_paged_attn_workspace_bytes(ctypes.byref(cache.desc), int(Hq), int(n_q), int(max_q),
+                                                     int(max_tokens), int(n_splits))
+
+
+def mustafar_paged_attn(q, cache: PagedCache, cu, max_q: int | None = None, max_tokens: int | None = None,
+                        window: int = 0, sinks: int = 0, scale: float = 0.0, out=None, n_splits: int = 0, ws=None,
+                        stream=None):
+    """Causal attention of q [n_q][Hq][d] (the cache's type; rows of a packed projection too), the last
+    cu[b+1] - cu[b] tokens of every request b, over its pages; window > 0: the newest `window` tokens
+    and the first `sinks`. max_q and max_tokens: bounds of a request's rows and length (default: one
+    row each if n_q <= B, else n_q; all that a table can hold). Returns out [n_q][Hq][d]."""
+    import torch
+    n_q, Hq, d = (int(s) for s in q.shape)
+    B = cache.desc.B
+    _paged_device(cache, q, cu, out, ws)
+    max_q = (1 if n_q <= B else n_q) if max_q is None else max_q
+    if max_tokens is None:
+        max_tokens = min(cache.desc.max_pages, cache.desc.n_pages) * cache.desc.page_tokens
+    qs = _rows("q", q, Hq, cache.desc.d, cache.dtype)
+    _want("cu", cu, (B + 1,), torch.int32, cache.device)
+    need = mustafar_paged_attn_workspace_bytes(cache, Hq, n_q, max_q, max_tokens, n_splits)
+    with _on_stream(stream):
+        if out is None:
+            out = torch.empty((n_q, Hq, d), dtype=cache.dtype, device=cache.device)
+        if ws is None and need > 0:
+            ws = torch.empty(need, dtype=torch.uint8, device=cache.device)
+    if out.shape[0] != n_q:
+        raise ValueError("as many rows of out as of q")
+    os_ = _rows("out", out, Hq, d, cache.dtype)
+    _check("mustafar_paged_attn", lib().mustafar_paged_attn(
+        _dptr(q), qs, n_q, Hq, ctypes.byref(cache.desc), _dptr(cu), int(window), int(sinks), float(scale), _dptr(out),
+        os_, int(max_q), int(max_tokens), int(n_splits), _dptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
+        _stream(stream)))
+    return out
 
 
 ROUTE_DEFAULT, ROUTE_WALKS, ROUTE_MATRIX_CORES = 0, 1, 2
