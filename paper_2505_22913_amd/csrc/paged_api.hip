@@ -10,6 +10,7 @@ namespace {
 
 constexpr int kTile = MUSTAFAR_TILE;
 constexpr int64_t kMaxGroups = 0x7fffffff;  // workgroups of a launch
+constexpr int kMaxSplits = 1 << 16;
 
 bool aligned(const void* p, uintptr_t a) { return p && ((uintptr_t)p % a) == 0; }
 
@@ -144,8 +145,11 @@ int mustafar_paged_gather(const mustafar_pages_t* p, const void* first, void* x_
 
 size_t mustafar_paged_attn_workspace_bytes(const mustafar_pages_t* p, int Hq, int n_q, int max_q, int max_tokens,
                                            int n_splits) {
-  (void)p, (void)Hq, (void)n_q, (void)max_q, (void)max_tokens, (void)n_splits;
-  return 0;
+  if (check_pages(p) != MUSTAFAR_OK || Hq < 1 || Hq % p->H != 0 || Hq / p->H > MUSTAFAR_PAGED_MAX_GROUP) return 0;
+  if (n_q < 1 || max_q < 0 || max_tokens < 0 || n_splits > kMaxSplits || (int64_t)n_q * Hq >= kMaxGroups) return 0;
+  const mf::PagedView v = view_of(p);
+  if (n_splits <= 0) n_splits = mf::paged_splits(v, Hq / p->H, n_q, max_q, max_tokens);
+  return (size_t)mf::paged_ws_bytes(v, Hq, n_q, n_splits);
 }
 
 int mustafar_paged_attn(const void* q, int64_t q_stride, int n_q, int Hq, const mustafar_pages_t* p, const void* cu,
@@ -163,11 +167,19 @@ int mustafar_paged_attn(const void* q, int64_t q_stride, int n_q, int Hq, const 
       out_stride > (int64_t)1 << 31)
     return MUSTAFAR_EINVAL;
   if ((int64_t)n_q * Hq >= kMaxGroups) return MUSTAFAR_EINVAL;
-  if (n_splits > (1 << 20)) return MUSTAFAR_EINVAL;
-  const size_t need = mustafar_paged_attn_workspace_bytes(p, Hq, n_q, max_q, max_tokens, n_splits);
-  if (need > 0 && (!aligned(ws, 16) || ws_bytes < need)) return MUSTAFAR_EWORKSPACE;
+  if (n_splits > kMaxSplits) return MUSTAFAR_EINVAL;
   mf::PagedAttnArgs a;
   a.p = view_of(p);
+  const size_t need = mustafar_paged_attn_workspace_bytes(p, Hq, n_q, max_q, max_tokens, n_splits);
+  if (need > 0 && (!aligned(ws, 16) || ws_bytes < need)) return MUSTAFAR_EWORKSPACE;
+  if (n_splits <= 0) {
+    // (what the rows see: never more than the workspace was sized for)
+    const int64_t seen = window > 0 ? (int64_t)window + max_q + sinks : max_tokens;
+    n_splits = mf::paged_splits(a.p, Hq / p->H, n_q, max_q, seen < max_tokens ? seen : max_tokens);
+  }
+  if (mf::paged_tiles(a.p, Hq / p->H, n_q) * p->H * n_splits >= kMaxGroups) return MUSTAFAR_EINVAL;
+  a.n_splits = n_splits;
+  a.ws = ws;
   a.q = (const uint16_t*)q;
   a.out = (uint16_t*)out;
   a.cu = (const int32_t*)cu;

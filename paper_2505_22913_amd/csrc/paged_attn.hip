@@ -5,112 +5,483 @@
 
 namespace mf {
 
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 
+// ------------------------------------------------------------------------------------------
+// The two 16-bit types.
+// ------------------------------------------------------------------------------------------
 template <bool BF16>
 __device__ __forceinline__ float to_float(uint32_t bits) {
   if constexpr (BF16) return __builtin_bit_cast(float, bits << 16);
   else return (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
 }
 
+// Two values rounded to nearest even, the first in the low half.
 template <bool BF16>
-__device__ __forceinline__ uint16_t from_float(float x) {
-  if constexpr (BF16) return __builtin_bit_cast(uint16_t, (__bf16)x);
-  else return __builtin_bit_cast(uint16_t, (_Float16)x);
+__device__ __forceinline__ uint32_t pack2(float x, float y) {
+  const f32x2 v = {x, y};
+  if constexpr (BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+  else return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, half2_t));
 }
 
-// The request of row t: the last b with cu[b] <= t.
-__device__ __forceinline__ int request_of(const int32_t* cu, int B, int t) {
-  int lo = 0, hi = B;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (cu[mid] <= t) lo = mid;
-    else hi = mid;
+// c + the sum of a pair.
+template <bool BF16>
+__device__ __forceinline__ float add_pair(uint32_t pair, float c) {
+  if constexpr (BF16) {
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), (bf16x2){(__bf16)1.f, (__bf16)1.f}, c, false);
+  } else {
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(half2_t, pair), (half2_t){(_Float16)1.f, (_Float16)1.f}, c, false);
   }
-  return lo;
 }
 
-// Element offset of token j of entry b, kv-head h.
-__device__ __forceinline__ int64_t token_at(const PagedView& p, int b, int h, int j) {
-  int page = p.table[(int64_t)b * p.max_pages + (j >> p.log2_page)];
-  if ((uint32_t)page >= (uint32_t)p.n_pages) page = 0;
-  return (int64_t)page * p.page_stride + (int64_t)h * p.head_stride +
-         (int64_t)(j & ((1 << p.log2_page) - 1)) * p.token_stride;
+// D[32][32] = A[32][16] B[16][32] + C: lane l holds A's row and B's column l % 32 at k = 8 (l / 32) + i,
+// and column l % 32 of the result at rows 8 (r / 4) + 4 (l / 32) + r % 4.
+template <bool BF16>
+__device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+  if constexpr (BF16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
 }
 
+// ------------------------------------------------------------------------------------------
+// Rows, tokens, tiles.
+// ------------------------------------------------------------------------------------------
+// The rows of a request are its new tokens times the G query heads of a kv-head, so that
+// a kv-head's keys are read once for all of them; a workgroup takes BM consecutive ones. Request b owns
+// workgroups (cu[b] G) / BM + b up to those of request b + 1: as many as its rows need, or one more.
+struct RowTile {
+  int b, row0, rows;  // request, first row, rows of the request (row0 >= rows: nothing to do)
+  int base;           // position of the request's first new token
+  int tok0;           // its row in q
+};
+
+__device__ __forceinline__ int first_tile(int cu, int b, int G, int BM) { return (int)((int64_t)cu * G / BM) + b; }
+
+// Two rounds of 64 entries at most, one load each.
+__device__ __forceinline__ RowTile row_tile(const PagedAttnArgs& a, int tile, int BM) {
+  const int B = a.p.B, lane = (int)lane_id();
+  const int stride = (B + kWave - 1) / kWave;
+  int b = min(lane * stride, B - 1);
+  uint64_t below = ballot(lane * stride < B && first_tile(a.cu[b], b, a.G, BM) <= tile);
+  b = (63 - __builtin_clzll(below | 1)) * stride;
+  if (stride > 1) {
+    const int c = min(b + lane, B - 1);
+    below = ballot(lane < stride && b + lane < B && first_tile(a.cu[c], c, a.G, BM) <= tile);
+    b += 63 - __builtin_clzll(below | 1);
+  }
+  b = __builtin_amdgcn_readfirstlane(b);
+  RowTile r;
+  r.b = b;
+  r.tok0 = __builtin_amdgcn_readfirstlane(a.cu[b]);
+  const int nq = min(__builtin_amdgcn_readfirstlane(a.cu[b + 1]), a.n_q) - r.tok0;
+  r.rows = nq * a.G;
+  r.row0 = (tile - first_tile(r.tok0, b, a.G, BM)) * BM;
+  const int64_t most = (int64_t)a.p.max_pages << a.p.log2_page;
+  const int len = __builtin_amdgcn_readfirstlane((int)min((int64_t)max(a.p.state[b], 0), most));
+  r.base = len - nq;
+  return r;
+}
+
+// The tokens that rows at positions [pos0, pos1] see between them, [0, sinks) and [lo, hi], in tiles of BN:
+// tile i of the list starts at token start(i).
+struct TileList {
+  int sinks, lo, hi;
+  int first, n_first;  // the tile of lo (or 0), and how many of the sinks' come before it
+  int n;
+  __device__ __forceinline__ TileList(int pos0, int pos1, int window, int n_sinks, int BN) {
+    hi = pos1;
+    lo = window > 0 ? max(pos0 - window + 1, 0) : 0;
+    sinks = min(n_sinks, lo);
+    n_first = (sinks + BN - 1) / BN;
+    first = lo / BN;
+    if (n_first >= first) {
+      n_first = 0;
+      if (sinks > 0) first = 0;
+    }
+    n = hi < 0 ? 0 : n_first + hi / BN - first + 1;
+  }
+  __device__ __forceinline__ int start(int i, int BN) const { return (i < n_first ? i : first + i - n_first) * BN; }
+};
+
+__device__ __forceinline__ bool sees(int pos, int j, int window, int n_sinks) {
+  return j <= pos && (window == 0 || j > pos - window || j < n_sinks);
+}
+
+__device__ __forceinline__ int page_of(const PagedView& p, int b, int j) {
+  // (through the scalar cache: uniform, and nothing in the launch writes the table)
+  const auto* t = (const __attribute__((address_space(4))) int32_t*)(p.table + (int64_t)b * p.max_pages);
+  const int page = t[j >> p.log2_page];
+  return (uint32_t)page < (uint32_t)p.n_pages ? page : 0;
+}
+
+// ------------------------------------------------------------------------------------------
+// A row by itself, one wave: every product in fp32 on the vector units, and nothing of a token that
+// the row does not see. The kernels below come here with the rows of a wave whose result is not
+// finite: their matrix products take whole tiles, so that a value that is not finite reaches
+// the rows that do not see it (0 times infinity).
+// ------------------------------------------------------------------------------------------
 // The least weight of a visible token: an infinite value that one sees stays infinite
 // where its probability is under fp32's range (0 times infinity would be NaN).
 constexpr float kLeast = 0x1p-120f;
 __device__ __forceinline__ float at_least(float x) { return x < kLeast ? kLeast : x; }  // (NaN stays)
 
-// One wave per row and query head, 64 tokens at a time: lane = token for the scores, lane =
-// channel for the values.
+template <int T>
+struct RowState {
+  float m, l, o[T];  // o: channels lane + 64 c
+};
+
 template <int T, bool BF16>
-__global__ __launch_bounds__(64) void k_paged_attn_row(PagedAttnArgs a) {
+__device__ __forceinline__ RowState<T> one_row(const PagedAttnArgs& a, int b, int h, const uint16_t* q, int pos, TileList tl,
+                                            int t0, int t1, int BN) {
   constexpr int d = kTile * T;
-  __shared__ float qs[d];
   const PagedView& p = a.p;
-  const int t = blockIdx.x / a.Hq, hq = blockIdx.x % a.Hq, h = hq / a.G;
-  if (t >= a.cu[p.B]) return;
-  const uint32_t lane = lane_id();
-  const int b = request_of(a.cu, p.B, t);
-  const int64_t most = (int64_t)p.max_pages << p.log2_page;
-  const int len = (int)min((int64_t)max(p.state[b], 0), most);
-  const int pos = len - (a.cu[b + 1] - t);
-#pragma unroll
-  for (int c = 0; c < T; ++c) qs[lane + kTile * c] = to_float<BF16>(a.q[t * a.q_stride + hq * d + kTile * c + lane]);
-  __syncthreads();
-  const int lo = a.window > 0 ? max(pos - a.window + 1, 0) : 0, sinks = min(a.sinks, lo);
-  const int n = pos < 0 ? 0 : sinks + pos + 1 - lo;
-  float m = -INFINITY, l = 0.f, o[T];
-#pragma unroll
-  for (int c = 0; c < T; ++c) o[c] = 0.f;
-  for (int u0 = 0; u0 < n; u0 += kWave) {
-    const int u = min(u0 + (int)lane, n - 1);
-    const int64_t at = token_at(p, b, h, u < sinks ? u : lo + u - sinks);
-    float s = 0.f;
-#pragma unroll 4
-    for (int c = 0; c < d; c += 8) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(p.k + at + c);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        s = fmaf(qs[c + 2 * e], to_float<BF16>(w[e] & 0xffffu), s);
-        s = fmaf(qs[c + 2 * e + 1], to_float<BF16>(w[e] >> 16), s);
-      }
+  const int lane = (int)lane_id();
+  RowState<T> s;
+  s.m = -INFINITY;
+  s.l = 0.f;
+  for (int c = 0; c < T; ++c) s.o[c] = 0.f;
+  for (int t = t0; t < t1; ++t) {
+    const int j0 = tl.start(t, BN), j = j0 + lane;
+    const bool seen = lane < BN && j <= tl.hi && sees(pos, j, a.window, a.sinks);
+    int64_t at = 0;
+    float x = -INFINITY;
+    if (seen) {
+      int page = p.table[(int64_t)b * p.max_pages + (j >> p.log2_page)];
+      if ((uint32_t)page >= (uint32_t)p.n_pages) page = 0;
+      at = (int64_t)page * p.page_stride + (int64_t)h * p.head_stride +
+           (int64_t)(j & ((1 << p.log2_page) - 1)) * p.token_stride;
+      x = 0.f;
+      for (int c = 0; c < d; ++c) x = fmaf(to_float<BF16>(q[c]), to_float<BF16>(p.k[at + c]), x);
     }
-    if (u0 + (int)lane >= n) s = -INFINITY;
-    const float mnew = fmaxf(m, wave_max(s));
-    const float alpha = m == -INFINITY ? 1.f : at_least(__builtin_amdgcn_exp2f((m - mnew) * a.scale_log2));
-    float w = s == -INFINITY ? 0.f : at_least(__builtin_amdgcn_exp2f((s - mnew) * a.scale_log2));
-    m = mnew;
-    l = fmaf(l, alpha, wave_sum(w));
-#pragma unroll
-    for (int c = 0; c < T; ++c) o[c] *= alpha;
-    for (int i = 0; i < min(kWave, n - u0); ++i) {
+    const float mnew = fmaxf(s.m, wave_max(x));
+    const float alpha = s.m == -INFINITY ? 1.f : at_least(__builtin_amdgcn_exp2f((s.m - mnew) * a.scale_log2));
+    const float w = x == -INFINITY ? 0.f : at_least(__builtin_amdgcn_exp2f((x - mnew) * a.scale_log2));
+    s.m = mnew;
+    s.l = fmaf(s.l, alpha, wave_sum(w));
+    for (int c = 0; c < T; ++c) s.o[c] *= alpha;
+    for (uint64_t left = ballot(seen); left; left &= left - 1) {
+      const int i = __builtin_ctzll(left);
       const float wi = __shfl(w, i, kWave);
       const int64_t ai = __shfl(at, i, kWave);
-#pragma unroll
-      for (int c = 0; c < T; ++c) o[c] = fmaf(wi, to_float<BF16>(p.v[ai + kTile * c + lane]), o[c]);
+      for (int c = 0; c < T; ++c) s.o[c] = fmaf(wi, to_float<BF16>(p.v[ai + kTile * c + lane]), s.o[c]);
     }
   }
-#pragma unroll
-  for (int c = 0; c < T; ++c)
-    a.out[t * a.out_stride + hq * d + kTile * c + lane] = from_float<BF16>(n > 0 ? o[c] / l : 0.f);
+  return s;
 }
 
+// ------------------------------------------------------------------------------------------
+// Results: the rounded output, or one range's share of it for k_paged_merge: the reference of its weights (a score, -inf
+// before the first), their sum (-1 for a row that sees nothing at all) and the weighted values.
+// ------------------------------------------------------------------------------------------
+struct PartOut {
+  float2* ml;  // [n_splits][n_q * Hq]
+  float* o;    // [n_splits][n_q * Hq][d]
+  int n_splits;
+};
+
+template <int T, bool BF16>
+__device__ __forceinline__ void redo_rows(const PagedAttnArgs& a, const PartOut& part, const RowTile& rt, int h, int first_row,
+                                       int n_rows, TileList tl, int t0, int t1, int split, int BN) {
+  constexpr int d = kTile * T;
+  const int lane = (int)lane_id();
+  for (int r = first_row; r < min(first_row + n_rows, rt.rows); ++r) {
+    const int tok = r / a.G, hq = h * a.G + (r - tok * a.G), t = rt.tok0 + tok, pos = rt.base + tok;
+    const RowState<T> s = one_row<T, BF16>(a, rt.b, h, a.q + t * a.q_stride + hq * d, pos, tl, t0, t1, BN);
+    if (part.n_splits > 1) {
+      const int64_t row = (int64_t)split * a.n_q * a.Hq + (int64_t)t * a.Hq + hq;
+      if (lane == 0) part.ml[row] = make_float2(s.m, pos < 0 ? -1.f : s.l);
+      for (int c = 0; c < T; ++c) part.o[row * d + kTile * c + lane] = s.o[c];
+    } else {
+      for (int c = 0; c < T; ++c)
+        a.out[t * a.out_stride + hq * d + kTile * c + lane] = (uint16_t)pack2<BF16>(pos < 0 ? 0.f : s.o[c] / s.l, 0.f);
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// k_paged_chunk: 128 rows a workgroup, 32 a wave, tiles of 64 tokens (32 at d = 256).
+//
+// Both products have the rows as columns: S^T = K Q^T leaves a lane with scores of one row (column l % 32),
+// so the softmax's shift and sum are per lane (two lanes hold a row's tokens), and its 8-token groups,
+// rounded to the type, are the B operand of O^T = V^T P^T as they lie; V^T comes out of LDS transposed.
+// ------------------------------------------------------------------------------------------
 template <int T>
-static hipError_t attn_T(const PagedAttnArgs& a, hipStream_t s) {
-  const dim3 grid((uint32_t)a.n_q * (uint32_t)a.Hq);
-  if (a.p.bf16) hipLaunchKernelGGL((k_paged_attn_row<T, true>), grid, dim3(kWave), 0, s, a);
-  else hipLaunchKernelGGL((k_paged_attn_row<T, false>), grid, dim3(kWave), 0, s, a);
+constexpr int chunk_tile() { return T == 4 ? 32 : 64; }
+
+// A probability is 2^kBias at the reference, which follows the largest score once that is more than 2^kSlack above it:
+// at most 2^15 (inside fp16), and fp16 keeps those down to 2^-31 of the reference.
+constexpr float kBias = 7.f, kUnit = 0x1p-7f, kSlack = 8.f;
+
+// 16-byte pieces of a row are stored at their place XOR these, so that the lanes of a read (K: one piece of
+// many rows; V: 32 or 64 bytes of four rows) find them in different banks.
+template <int T>
+__device__ __forceinline__ uint32_t swizzle_k(uint32_t row) { return T == 1 ? row % 8 : row % 16; }
+template <int T>
+__device__ __forceinline__ uint32_t swizzle_v(uint32_t row) {
+  return T == 1 ? 2 * (row & 3) : ((row & 1) ? 6u : 0u) ^ ((row & 2) ? 10u : 0u);
+}
+
+// 16 bytes a lane from base + offset to LDS at dst + 16 lane; wait_loads() waits for them.
+__device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t dst) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)((const char*)base + offset),
+                                   reinterpret_cast<__attribute__((address_space(3))) void*>(dst), 16, 0, 0);
+}
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+template <typename V>
+__device__ __forceinline__ V lds_load(uint32_t byte_addr) {
+  return *reinterpret_cast<const __attribute__((address_space(3))) V*>(byte_addr);
+}
+// Four tokens of one channel: the 16 lanes of a group address 4 x 16 elements, and each gets a column.
+__device__ __forceinline__ u32x2 lds_load_tr(uint32_t byte_addr) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                       reinterpret_cast<__attribute__((address_space(3))) s16x4*>(byte_addr)));
+}
+
+template <int T, bool BF16>
+__global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttnArgs a, PartOut part) {
+  constexpr int d = kTile * T, BN = chunk_tile<T>(), NK = BN / 32, NC = d / 16, ND = d / 32;
+  constexpr uint32_t kRow = 2 * d, kBuf = BN * kRow;  // bytes
+  constexpr int kRowsPerLoad = 1024 / (2 * d), kLoads = BN / 4 / kRowsPerLoad;
+  extern __shared__ __align__(16) unsigned char smem[];  // K, K, V, V
+  const PagedView& p = a.p;
+  const int h = blockIdx.x % p.H, split = (blockIdx.x / p.H) % part.n_splits;
+  const int tile = (int)(gridDim.x / (p.H * part.n_splits)) - 1 - (int)(blockIdx.x / (p.H * part.n_splits));
+  const RowTile rt = row_tile(a, tile, kChunkRows);
+  if (rt.row0 >= rt.rows) return;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+  const uint32_t lane = lane_id(), r32 = lane % 32, half = lane / 32;
+  const int row = min(rt.row0 + 32 * wave + (int)r32, rt.rows - 1);
+  const int tok = row / a.G, hq = h * a.G + (row - tok * a.G), pos = rt.base + tok;
+  const int last = min(rt.row0 + kChunkRows, rt.rows) - 1;
+  const int pos0 = rt.base + rt.row0 / a.G, pos1 = rt.base + last / a.G;
+  const TileList tl(pos0, pos1, a.window, a.sinks, BN);
+  const int t0 = (int)((int64_t)tl.n * split / part.n_splits), t1 = (int)((int64_t)tl.n * (split + 1) / part.n_splits);
+
+  // Q as the B operand: column = row of the wave, k = 16 c + 8 half + i.
+  u32x4 qb[NC];
+  {
+    const uint16_t* q = a.q + (int64_t)(rt.tok0 + tok) * a.q_stride + hq * d + 8 * half;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) qb[c] = *reinterpret_cast<const u32x4*>(q + 16 * c);
+  }
+
+  // Wave w stages rows BN / 4 w .. of a tile. Pages hold 16 tokens or more, so a wave's rows share one. A row that no row
+  // of q sees is replaced by one that some does: the wave's group of 16 by the nearest with such a row, the row by the nearest of
+  // the group.
+  const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
+  auto stage = [&](int i, uint32_t buf) {
+    const int j = tl.start(i, BN) + BN / 4 * wave;
+    int g0 = j & ~15, from, to;
+    if (g0 < tl.sinks) {
+      from = 0;
+      to = tl.lo <= g0 + 15 ? tl.hi : tl.sinks - 1;
+    } else {
+      g0 = min(max(g0, tl.lo & ~15), tl.hi & ~15);
+      from = tl.lo;
+      to = tl.hi;
+    }
+    from = max(from, g0) - g0;
+    to = min(to, g0 + 15) - g0;
+    const int64_t at = (int64_t)page_of(p, rt.b, g0) * p.page_stride + (int64_t)h * p.head_stride;
+    const uint16_t *kb = p.k + at, *vb = p.v + at;
+    const int in_page = g0 & ((1 << p.log2_page) - 1);
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) {
+      const uint32_t r = kRowsPerLoad * n + lane / (kWave / kRowsPerLoad), piece = lane % (kWave / kRowsPerLoad);
+      const uint32_t tr = BN / 4 * wave + r;  // row of the tile
+      const int src = min(max((int)r + (j & 15), from), to) + in_page;
+      const uint32_t off = 2u * (uint32_t)src * (uint32_t)p.token_stride;
+      const uint32_t dst = lds0 + buf * kBuf + (BN / 4 * wave + kRowsPerLoad * n) * kRow;
+      load_to_lds(kb, off + 16u * (piece ^ swizzle_k<T>(tr)), dst);
+      load_to_lds(vb, off + 16u * (piece ^ swizzle_v<T>(tr)), dst + 2 * kBuf);
+    }
+  };
+
+  float l = 0.f;
+  bool started = false;  // the reference is that of a visible score
+  f32x16 ref = {};       // minus the reference, what the scores' products start from
+  f32x16 o[ND];
+#pragma unroll
+  for (int c = 0; c < ND; ++c) o[c] = (f32x16){};
+
+  if (t0 < t1) stage(t0, 0);
+  for (int t = t0; t < t1; ++t) {
+    const uint32_t buf = (uint32_t)(t - t0) & 1u;
+    wait_loads();
+    __syncthreads();
+    if (t + 1 < t1) stage(t + 1, buf ^ 1u);
+    const int j0 = tl.start(t, BN);
+
+    f32x16 s[NK];
+    const uint32_t kbase = lds0 + buf * kBuf + r32 * kRow;
+#pragma unroll
+    for (int n = 0; n < NK; ++n) {
+      s[n] = ref;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const u32x4 kf = lds_load<u32x4>(kbase + 32 * n * kRow + 16u * ((2 * c + half) ^ swizzle_k<T>(r32)));
+        s[n] = mfma32<BF16>(kf, qb[c], s[n]);
+      }
+    }
+
+    // Tokens that a row does not see.
+    if (j0 + BN - 1 > pos0 || j0 + BN - 1 > tl.hi || (a.window > 0 && j0 <= pos1 - a.window && j0 + BN > a.sinks)) {
+#pragma unroll
+      for (int n = 0; n < NK; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int j = j0 + 32 * n + 8 * (r / 4) + 4 * (int)half + r % 4;
+          if (!sees(pos, j, a.window, a.sinks)) s[n][r] = -INFINITY;
+        }
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int n = 0; n < NK; ++n)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = fmaxf(top, s[n][r]);
+    top = fmaxf(top, __shfl_xor(top, 32, kWave));
+    const bool move = started ? top * a.scale_log2 > kSlack : top > -INFINITY;
+    if (ballot(move)) {
+      const float by = move ? top : 0.f;
+      const float alpha = !move ? 1.f : started ? __builtin_amdgcn_exp2f(-by * a.scale_log2) : 0.f;
+      started |= move;
+      const float r0 = ref[0] - by;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) ref[r] = r0;
+#pragma unroll
+      for (int n = 0; n < NK; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[n][r] -= by;
+      l *= alpha;
+#pragma unroll
+      for (int c = 0; c < ND; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[c][r] *= alpha;
+    }
+    // Probabilities, rounded; the sum is that of the rounded ones.
+    u32x4 pb[2 * NK];
+#pragma unroll
+    for (int n = 0; n < NK; ++n)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[n][2 * e], a.scale_log2, kBias));
+        const float y = __builtin_amdgcn_exp2f(fmaf(s[n][2 * e + 1], a.scale_log2, kBias));
+        const uint32_t xy = pack2<BF16>(x, y);
+        l = add_pair<BF16>(xy, l);
+        pb[2 * n + e / 4][e % 4] = xy;
+      }
+    // O^T += V^T P^T, 16 tokens at a time: k slot 8 half + i is token 8 (i / 4) + 4 half + i % 4, as the scores lie.
+    const uint32_t vrow = 4 * half + (lane % 16) / 4;
+    const uint32_t vbase = lds0 + 2 * kBuf + buf * kBuf + vrow * kRow + 8 * (lane & 1);
+    const uint32_t vpiece = ((lane / 16) & 1) * 2 + (lane % 4) / 2;
+#pragma unroll
+    for (int c = 0; c < ND; ++c)
+#pragma unroll
+      for (int k = 0; k < 2 * NK; ++k) {
+        const uint32_t at = vbase + 16 * k * kRow + 16u * ((4 * c + vpiece) ^ swizzle_v<T>(vrow));
+        const u32x2 lo = lds_load_tr(at), hi = lds_load_tr(at + 8 * kRow);
+        o[c] = mfma32<BF16>((u32x4){lo.x, lo.y, hi.x, hi.y}, pb[k], o[c]);
+      }
+  }
+
+  l += __shfl_xor(l, 32, kWave);
+  const bool mine = rt.row0 + 32 * wave + (int)r32 < rt.rows;
+  float odd = l * 0.f;  // NaN if something is not finite
+#pragma unroll
+  for (int c = 0; c < ND; ++c)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) odd = fmaf(o[c][r], 0.f, odd);
+  if (ballot(mine && odd != odd)) {
+    redo_rows<T, BF16>(a, part, rt, h, rt.row0 + 32 * wave, 32, tl, t0, t1, split, BN);
+    return;
+  }
+  if (!mine) return;
+  const int64_t t = rt.tok0 + tok;
+  if (part.n_splits > 1) {
+    const int64_t orow = (int64_t)split * a.n_q * a.Hq + t * a.Hq + hq;
+    if (half == 0) part.ml[orow] = make_float2(started ? -ref[0] : -INFINITY, pos < 0 ? -1.f : l * kUnit);
+    float* dst = part.o + orow * d + 4 * half;
+#pragma unroll
+    for (int c = 0; c < ND; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *reinterpret_cast<f32x4*>(dst + 32 * c + 2 * r) =
+            (f32x4){o[c][r], o[c][r + 1], o[c][r + 2], o[c][r + 3]} * kUnit;
+  } else {
+    const float inv = pos < 0 ? 0.f : 1.f / l;
+    uint16_t* dst = a.out + t * a.out_stride + hq * d + 4 * half;
+#pragma unroll
+    for (int c = 0; c < ND; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *reinterpret_cast<u32x2*>(dst + 32 * c + 2 * r) =
+            (u32x2){pack2<BF16>(o[c][r] * inv, o[c][r + 1] * inv), pack2<BF16>(o[c][r + 2] * inv, o[c][r + 3] * inv)};
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// k_paged_merge: the ranges of a row together, one wave a row.
+// ------------------------------------------------------------------------------------------
+template <int T, bool BF16>
+__global__ __launch_bounds__(64) void k_paged_merge(PagedAttnArgs a, PartOut part) {
+  constexpr int d = kTile * T;
+  const int lane = (int)lane_id();
+  const int64_t rows = (int64_t)a.n_q * a.Hq, row = blockIdx.x;
+  const int t = (int)(row / a.Hq), hq = (int)(row - (int64_t)t * a.Hq);
+  if (t >= a.cu[a.p.B]) return;
+  float M = -INFINITY;
+  bool nothing = false;
+  for (int s = lane; s < part.n_splits; s += kWave) {
+    const float2 ml = part.ml[s * rows + row];
+    M = fmaxf(M, ml.x);
+    nothing |= ml.y < 0.f;
+  }
+  M = wave_max(M);
+  float l = 0.f, o[T] = {};
+  for (int s = 0; s < part.n_splits; ++s) {
+    const float2 ml = part.ml[s * rows + row];
+    if (ml.x == -INFINITY && ml.y == 0.f) continue;
+    const float w = at_least(__builtin_amdgcn_exp2f((ml.x - M) * a.scale_log2));
+    l = fmaf(ml.y, w, l);
+#pragma unroll
+    for (int c = 0; c < T; ++c) o[c] = fmaf(part.o[(s * rows + row) * d + kTile * c + lane], w, o[c]);
+  }
+  const bool zero = ballot(nothing) != 0;
+#pragma unroll
+  for (int c = 0; c < T; ++c)
+    a.out[t * a.out_stride + hq * d + kTile * c + lane] = (uint16_t)pack2<BF16>(zero ? 0.f : o[c] / l, 0.f);
+}
+
+template <int T, bool BF16>
+static hipError_t attn_launch(const PagedAttnArgs& a, hipStream_t s) {
+  constexpr int BN = chunk_tile<T>();
+  const int64_t rows = (int64_t)a.n_q * a.Hq;
+  PartOut part = {(float2*)a.ws, nullptr, a.n_splits};
+  part.o = (float*)(part.ml + (int64_t)a.n_splits * rows);
+  const int64_t groups = paged_tiles(a.p, a.G, a.n_q) * a.p.H * a.n_splits;
+  hipLaunchKernelGGL((k_paged_chunk<T, BF16>), dim3((uint32_t)groups), dim3(256), 4 * BN * 2 * kTile * T, s, a, part);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.n_splits == 1) return e;
+  hipLaunchKernelGGL((k_paged_merge<T, BF16>), dim3((uint32_t)rows), dim3(kWave), 0, s, a, part);
   return hipGetLastError();
 }
 
 hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s) {
   switch (a.p.d) {
-    case 64: return attn_T<1>(a, s);
-    case 128: return attn_T<2>(a, s);
-    default: return attn_T<4>(a, s);
+    case 64: return a.p.bf16 ? attn_launch<1, true>(a, s) : attn_launch<1, false>(a, s);
+    case 128: return a.p.bf16 ? attn_launch<2, true>(a, s) : attn_launch<2, false>(a, s);
+    default: return a.p.bf16 ? attn_launch<4, true>(a, s) : attn_launch<4, false>(a, s);
   }
 }
 

@@ -103,7 +103,7 @@ def test_attention_refuses(lib):
     p, _ = init()
     for bad in (dict(q=0), dict(q=0x18), dict(qs=32 * 128 - 8), dict(qs=32 * 128 + 4), dict(qs=1 << 32), dict(n_q=-1),
                 dict(Hq=0), dict(Hq=33), dict(cu=0), dict(cu=0x22), dict(window=-1), dict(sinks=-1), dict(out=0),
-                dict(out=0x38), dict(os=128), dict(max_q=-1), dict(max_tokens=-1), dict(n_splits=(1 << 20) + 1),
+                dict(out=0x38), dict(os=128), dict(max_q=-1), dict(max_tokens=-1), dict(n_splits=(1 << 16) + 1),
                 dict(n_q=0x7fffffff)):
         assert attn(p, **bad) == mf.EINVAL, bad
     assert attn(p, Hq=8 * 65, qs=8 * 65 * 128, os=8 * 65 * 128) == mf.EUNSUPPORTED
