@@ -180,8 +180,8 @@ __device__ __forceinline__ RowState<T> one_row(const PagedAttnArgs& a, int b, in
 }
 
 // ------------------------------------------------------------------------------------------
-// Results: the rounded output, or one range's share of it for k_paged_merge: the reference of its weights (a score, -inf
-// before the first), their sum (-1 for a row that sees nothing at all) and the weighted values.
+// Results: the rounded output, or one range's share of it for k_paged_merge: the log2 of what its weights are multiples of
+// (-inf if it has none), their sum (-1 for a row that sees nothing at all) and the weighted values.
 // ------------------------------------------------------------------------------------------
 struct PartOut {
   float2* ml;  // [n_splits][n_q * Hq]
@@ -199,7 +199,7 @@ __device__ __forceinline__ void redo_rows(const PagedAttnArgs& a, const PartOut&
     const RowState<T> s = one_row<T, BF16>(a, rt.b, h, a.q + t * a.q_stride + hq * d, pos, tl, t0, t1, BN);
     if (part.n_splits > 1) {
       const int64_t row = (int64_t)split * a.n_q * a.Hq + (int64_t)t * a.Hq + hq;
-      if (lane == 0) part.ml[row] = make_float2(s.m, pos < 0 ? -1.f : s.l);
+      if (lane == 0) part.ml[row] = make_float2(s.m * a.scale_log2, pos < 0 ? -1.f : s.l);
       for (int c = 0; c < T; ++c) part.o[row * d + kTile * c + lane] = s.o[c];
     } else {
       for (int c = 0; c < T; ++c)
@@ -219,8 +219,11 @@ template <int T>
 constexpr int chunk_tile() { return T == 4 ? 32 : 64; }
 
 // A probability is 2^kBias at the reference, which follows the largest score once that is more than 2^kSlack above it:
-// at most 2^15 (inside fp16), and fp16 keeps those down to 2^-31 of the reference.
-constexpr float kBias = 7.f, kUnit = 0x1p-7f, kSlack = 8.f;
+// at most 2^15 (inside fp16), and fp16 keeps those down to 2^-31 of the reference. It is exp2(score * scale +
+// shift) with shift = kBias - reference * scale rounded: one shift for all weights of a row, so its rounding is a
+// factor of them all. (Scores of 2^23 and more, where that factor leaves fp16, give infinities or zeros, and
+// the row is done by itself.)
+constexpr float kBias = 7.f, kSlack = 8.f;
 
 // 16-byte pieces of a row are stored at their place XOR these, so that the lanes of a read (K: one piece of
 // many rows; V: 32 or 64 bytes of four rows) find them in different banks.
@@ -231,10 +234,13 @@ __device__ __forceinline__ uint32_t swizzle_v(uint32_t row) {
   return T == 1 ? 2 * (row & 3) : ((row & 1) ? 6u : 0u) ^ ((row & 2) ? 10u : 0u);
 }
 
-// 16 bytes a lane from base + offset to LDS at dst + 16 lane; wait_loads() waits for them.
+// 16 bytes a lane from base + offset to LDS at dst + 16 lane; wait_loads() waits for them. (Inline: behind the builtin the
+// compiler waits for every such load before the next transposing LDS read of any address. The load has no register
+// output; m0, its LDS address, is put back.)
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t dst) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)((const char*)base + offset),
-                                   reinterpret_cast<__attribute__((address_space(3))) void*>(dst), 16, 0, 0);
+  uint32_t m0;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0) : "s"(dst), "v"(offset), "s"(base) : "memory");
 }
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
@@ -248,12 +254,29 @@ __device__ __forceinline__ u32x2 lds_load_tr(uint32_t byte_addr) {
                                        reinterpret_cast<__attribute__((address_space(3))) s16x4*>(byte_addr)));
 }
 
+// Largest over the two lanes of a row.
+__device__ __forceinline__ float max_halves(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+
+template <int NK>
+__device__ __forceinline__ float max_of(const f32x16 (&s)[NK]) {
+  float top = s[0][0];
+#pragma unroll
+  for (int n = 0; n < NK; ++n)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[n][r]);
+  return top;
+}
+
 template <int T, bool BF16>
-__global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttnArgs a, PartOut part) {
+__global__ __launch_bounds__(256, T == 4 ? 1 : 2) void k_paged_chunk(PagedAttnArgs a, PartOut part) {
   constexpr int d = kTile * T, BN = chunk_tile<T>(), NK = BN / 32, NC = d / 16, ND = d / 32;
   constexpr uint32_t kRow = 2 * d, kBuf = BN * kRow;  // bytes
   constexpr int kRowsPerLoad = 1024 / (2 * d), kLoads = BN / 4 / kRowsPerLoad;
-  extern __shared__ __align__(16) unsigned char smem[];  // K, K, V, V
+  extern __shared__ __align__(1024) unsigned char smem[];  // K, K, V, V
   const PagedView& p = a.p;
   const int h = blockIdx.x % p.H, split = (blockIdx.x / p.H) % part.n_splits;
   const int tile = (int)(gridDim.x / (p.H * part.n_splits)) - 1 - (int)(blockIdx.x / (p.H * part.n_splits));
@@ -262,7 +285,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttnArgs a, PartOut
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
   const uint32_t lane = lane_id(), r32 = lane % 32, half = lane / 32;
   const int row = min(rt.row0 + 32 * wave + (int)r32, rt.rows - 1);
-  const int tok = row / a.G, hq = h * a.G + (row - tok * a.G), pos = rt.base + tok;
+  const int tok = row / a.G, pos = rt.base + tok;
   const int last = min(rt.row0 + kChunkRows, rt.rows) - 1;
   const int pos0 = rt.base + rt.row0 / a.G, pos1 = rt.base + last / a.G;
   const TileList tl(pos0, pos1, a.window, a.sinks, BN);
@@ -271,72 +294,102 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttnArgs a, PartOut
   // Q as the B operand: column = row of the wave, k = 16 c + 8 half + i.
   u32x4 qb[NC];
   {
-    const uint16_t* q = a.q + (int64_t)(rt.tok0 + tok) * a.q_stride + hq * d + 8 * half;
+    const uint16_t* q = a.q + (int64_t)(rt.tok0 + tok) * a.q_stride + (h * a.G + row - tok * a.G) * d + 8 * half;
 #pragma unroll
     for (int c = 0; c < NC; ++c) qb[c] = *reinterpret_cast<const u32x4*>(q + 16 * c);
+    // (here: a wait for them inside the loop would be one for a tile's loads too)
+#pragma unroll
+    for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(qb[c]));
   }
 
   // Wave w stages rows BN / 4 w .. of a tile. Pages hold 16 tokens or more, so a wave's rows share one. A row that no row
   // of q sees is replaced by one that some does: the wave's group of 16 by the nearest with such a row, the row by the nearest of
   // the group.
   const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
-  auto stage = [&](int i, uint32_t buf) {
-    const int j = tl.start(i, BN) + BN / 4 * wave;
-    int g0 = j & ~15, from, to;
-    if (g0 < tl.sinks) {
-      from = 0;
-      to = tl.lo <= g0 + 15 ? tl.hi : tl.sinks - 1;
-    } else {
-      g0 = min(max(g0, tl.lo & ~15), tl.hi & ~15);
-      from = tl.lo;
-      to = tl.hi;
+  struct Place {
+    int64_t at;    // element of the group's first row in k and v
+    int from, to;  // rows of the group that some row of q sees
+  };
+  // The pages of 64 tiles at a time, one a lane.
+  int pages = 0;
+  auto group_of = [&](int i) {
+    const int j = (tl.start(i, BN) + BN / 4 * wave) & ~15;
+    return j < tl.sinks ? j : min(max(j, tl.lo & ~15), tl.hi & ~15);
+  };
+  auto place = [&](int i) {
+    if (((i - t0) & (kWave - 1)) == 0) {
+      const int page = p.table[(int64_t)rt.b * p.max_pages + (group_of(min(i + (int)lane, t1 - 1)) >> p.log2_page)];
+      pages = (uint32_t)page < (uint32_t)p.n_pages ? page : 0;
     }
-    from = max(from, g0) - g0;
-    to = min(to, g0 + 15) - g0;
-    const int64_t at = (int64_t)page_of(p, rt.b, g0) * p.page_stride + (int64_t)h * p.head_stride;
-    const uint16_t *kb = p.k + at, *vb = p.v + at;
-    const int in_page = g0 & ((1 << p.log2_page) - 1);
+    const int g0 = group_of(i), page = __builtin_amdgcn_readlane(pages, (i - t0) & (kWave - 1));
+    Place w;
+    w.at = (int64_t)page * p.page_stride + (int64_t)h * p.head_stride +
+           (int64_t)(g0 & ((1 << p.log2_page) - 1)) * p.token_stride;
+    const bool first = g0 < tl.sinks;
+    w.from = first ? 0 : max(tl.lo - g0, 0);
+    w.to = min((first && tl.lo > g0 + 15 ? tl.sinks - 1 : tl.hi) - g0, 15);
+    return w;
+  };
+  // This lane's row of the wave's first load, in bytes, and its piece of the row. (Opaque in every call: kept in
+  // registers for each load of a tile, their addresses would push others into scratch, whose loads wait for a tile's.)
+  constexpr uint32_t kLanes = kWave / kRowsPerLoad;  // of a row
+  const uint32_t lane_row = lane / kLanes, row_bytes = 2u * (uint32_t)p.token_stride;
+  const uint32_t lane_off = lane_row * row_bytes, piece_k = 16u * (lane % kLanes ^ swizzle_k<T>(lane_row)),
+                 piece_v = 16u * (lane % kLanes ^ swizzle_v<T>(lane_row));
+  auto stage = [&](const Place& w, bool values, uint32_t buf) {
+    const uint16_t* base = (values ? p.v : p.k) + w.at;
+    const uint32_t first = (BN / 4 * wave) & 15;  // row of the group
+    const uint32_t dst = lds0 + (buf + (values ? 2 : 0)) * kBuf + BN / 4 * wave * kRow;
+    uint32_t piece = values ? piece_v : piece_k, off = lane_off;
+    asm volatile("" : "+v"(piece), "+v"(off));
+    const bool whole = w.from <= (int)first && w.to >= (int)first + BN / 4 - 1;
 #pragma unroll
     for (int n = 0; n < kLoads; ++n) {
-      const uint32_t r = kRowsPerLoad * n + lane / (kWave / kRowsPerLoad), piece = lane % (kWave / kRowsPerLoad);
-      const uint32_t tr = BN / 4 * wave + r;  // row of the tile
-      const int src = min(max((int)r + (j & 15), from), to) + in_page;
-      const uint32_t off = 2u * (uint32_t)src * (uint32_t)p.token_stride;
-      const uint32_t dst = lds0 + buf * kBuf + (BN / 4 * wave + kRowsPerLoad * n) * kRow;
-      load_to_lds(kb, off + 16u * (piece ^ swizzle_k<T>(tr)), dst);
-      load_to_lds(vb, off + 16u * (piece ^ swizzle_v<T>(tr)), dst + 2 * kBuf);
+      const uint32_t r = first + kRowsPerLoad * n;  // of the group, this load's first
+      // (the places' XORs are linear in the row's bits: this load's share of them)
+      const uint32_t at = piece ^ (16u * (values ? swizzle_v<T>(r) : swizzle_k<T>(r)));
+      uint32_t row = off + r * row_bytes;
+      if (!whole) row = (uint32_t)min(max((int)(r + lane_row), w.from), w.to) * row_bytes;
+      load_to_lds(base, row + at, dst + kRowsPerLoad * n * kRow);
     }
   };
 
-  float l = 0.f;
-  bool started = false;  // the reference is that of a visible score
-  f32x16 ref = {};       // minus the reference, what the scores' products start from
+  float l = 0.f, shift = 0.f;
+  bool started = false;  // the shift is that of a visible score
   f32x16 o[ND];
 #pragma unroll
   for (int c = 0; c < ND; ++c) o[c] = (f32x16){};
 
-  if (t0 < t1) stage(t0, 0);
-  for (int t = t0; t < t1; ++t) {
+  // Operand i of the scores (tokens 32 (i % NK) .., channels 16 (i / NK) ..) and of the outputs (channels 32 (i % ND) .., tokens
+  // 16 (i / ND) .., k slot 8 half + i being token 8 (i / 4) + 4 half + i % 4, as the scores lie). A row of LDS is a
+  // multiple of its pieces' places, so that XOR selects the piece.
+  constexpr int kS = NK * NC, kO = 2 * NK * ND, kAhead = 4;
+  const uint32_t kaddr = lds0 + r32 * kRow + 16u * (half ^ swizzle_k<T>(r32));
+  const uint32_t vrow = 4 * half + (lane % 16) / 4;
+  const uint32_t vaddr = lds0 + 2 * kBuf + vrow * kRow + 16u * ((((lane / 16) & 1) * 2 + (lane % 4) / 2) ^ swizzle_v<T>(vrow)) + 8 * (lane & 1);
+  auto load_k = [&](uint32_t at, int i) { return lds_load<u32x4>((at ^ (32u * (i / NK))) + 32 * (i % NK) * kRow); };
+  auto load_v = [&](uint32_t at, int i) {
+    const uint32_t x = (at ^ (64u * (i % ND))) + 16 * (i / ND) * kRow;
+    const u32x2 lo = lds_load_tr(x), hi = lds_load_tr(x + 8 * kRow);
+    return (u32x4){lo.x, lo.y, hi.x, hi.y};
+  };
+
+  // One tile: its scores are in s (top: this lane's largest), those of the next go to sn while this one's probabilities are
+  // computed, their maximum while the values are multiplied.
+  float top = -INFINITY;
+  Place next = {};
+  auto step = [&](int t, f32x16 (&s)[NK], f32x16 (&sn)[NK]) {
     const uint32_t buf = (uint32_t)(t - t0) & 1u;
     wait_loads();
     __syncthreads();
-    if (t + 1 < t1) stage(t + 1, buf ^ 1u);
-    const int j0 = tl.start(t, BN);
-
-    f32x16 s[NK];
-    const uint32_t kbase = lds0 + buf * kBuf + r32 * kRow;
-#pragma unroll
-    for (int n = 0; n < NK; ++n) {
-      s[n] = ref;
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const u32x4 kf = lds_load<u32x4>(kbase + 32 * n * kRow + 16u * ((2 * c + half) ^ swizzle_k<T>(r32)));
-        s[n] = mfma32<BF16>(kf, qb[c], s[n]);
-      }
+    if (t + 1 < t1) stage(next, true, buf ^ 1u);
+    if (t + 2 < t1) {
+      next = place(t + 2);
+      stage(next, false, buf);
     }
-
+    const int j0 = tl.start(t, BN);
     // Tokens that a row does not see.
-    if (j0 + BN - 1 > pos0 || j0 + BN - 1 > tl.hi || (a.window > 0 && j0 <= pos1 - a.window && j0 + BN > a.sinks)) {
+    if (j0 + BN - 1 > pos0 || (a.window > 0 && j0 <= pos1 - a.window && j0 + BN > a.sinks)) {
 #pragma unroll
       for (int n = 0; n < NK; ++n)
 #pragma unroll
@@ -344,25 +397,15 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttnArgs a, PartOut
           const int j = j0 + 32 * n + 8 * (r / 4) + 4 * (int)half + r % 4;
           if (!sees(pos, j, a.window, a.sinks)) s[n][r] = -INFINITY;
         }
+      top = max_of<NK>(s);
     }
-    float top = s[0][0];
-#pragma unroll
-    for (int n = 0; n < NK; ++n)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) top = fmaxf(top, s[n][r]);
-    top = fmaxf(top, __shfl_xor(top, 32, kWave));
-    const bool move = started ? top * a.scale_log2 > kSlack : top > -INFINITY;
+    top = max_halves(top);
+    const bool move = started ? fmaf(top, a.scale_log2, shift) > kBias + kSlack : top > -INFINITY;
     if (ballot(move)) {
-      const float by = move ? top : 0.f;
-      const float alpha = !move ? 1.f : started ? __builtin_amdgcn_exp2f(-by * a.scale_log2) : 0.f;
+      const float to = move ? fmaf(-top, a.scale_log2, kBias) : shift;
+      const float alpha = started ? __builtin_amdgcn_exp2f(to - shift) : 1.f;  // (nothing is there before the start)
       started |= move;
-      const float r0 = ref[0] - by;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) ref[r] = r0;
-#pragma unroll
-      for (int n = 0; n < NK; ++n)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[n][r] -= by;
+      shift = to;
       l *= alpha;
 #pragma unroll
       for (int c = 0; c < ND; ++c)
@@ -371,56 +414,100 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedAttnArgs a, PartOut
     }
     // Probabilities, rounded; the sum is that of the rounded ones.
     u32x4 pb[2 * NK];
+    auto pair = [&](int i) {
+      const float x = __builtin_amdgcn_exp2f(fmaf(s[i / 8][2 * (i % 8)], a.scale_log2, shift));
+      const float y = __builtin_amdgcn_exp2f(fmaf(s[i / 8][2 * (i % 8) + 1], a.scale_log2, shift));
+      const uint32_t xy = pack2<BF16>(x, y);
+      l = add_pair<BF16>(xy, l);
+      pb[i / 4][i % 4] = xy;
+    };
+    uint32_t kat = kaddr + (buf ^ 1u) * kBuf, vat = vaddr + buf * kBuf;
+    asm volatile("" : "+v"(kat), "+v"(vat));  // (as in stage)
+    u32x4 vf[kAhead];
+    if (t + 1 < t1) {
+      u32x4 kf[kAhead];
 #pragma unroll
-    for (int n = 0; n < NK; ++n)
+      for (int i = 0; i < kAhead; ++i) kf[i] = load_k(kat, i);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float x = __builtin_amdgcn_exp2f(fmaf(s[n][2 * e], a.scale_log2, kBias));
-        const float y = __builtin_amdgcn_exp2f(fmaf(s[n][2 * e + 1], a.scale_log2, kBias));
-        const uint32_t xy = pack2<BF16>(x, y);
-        l = add_pair<BF16>(xy, l);
-        pb[2 * n + e / 4][e % 4] = xy;
+      for (int i = 0; i < kS; ++i) {
+        sn[i % NK] = mfma32<BF16>(kf[i % kAhead], qb[i / NK], i < NK ? (f32x16){} : sn[i % NK]);
+        if (i + kAhead < kS) kf[i % kAhead] = load_k(kat, i + kAhead);
+        else vf[i + kAhead - kS] = load_v(vat, i + kAhead - kS);
+#pragma unroll
+        for (int e = i * 8 * NK / kS; e < (i + 1) * 8 * NK / kS; ++e) pair(e);
+        __builtin_amdgcn_sched_barrier(0);
       }
-    // O^T += V^T P^T, 16 tokens at a time: k slot 8 half + i is token 8 (i / 4) + 4 half + i % 4, as the scores lie.
-    const uint32_t vrow = 4 * half + (lane % 16) / 4;
-    const uint32_t vbase = lds0 + 2 * kBuf + buf * kBuf + vrow * kRow + 8 * (lane & 1);
-    const uint32_t vpiece = ((lane / 16) & 1) * 2 + (lane % 4) / 2;
+    } else {
 #pragma unroll
-    for (int c = 0; c < ND; ++c)
+      for (int i = 0; i < kAhead; ++i) vf[i] = load_v(vat, i);
 #pragma unroll
-      for (int k = 0; k < 2 * NK; ++k) {
-        const uint32_t at = vbase + 16 * k * kRow + 16u * ((4 * c + vpiece) ^ swizzle_v<T>(vrow));
-        const u32x2 lo = lds_load_tr(at), hi = lds_load_tr(at + 8 * kRow);
-        o[c] = mfma32<BF16>((u32x4){lo.x, lo.y, hi.x, hi.y}, pb[k], o[c]);
-      }
+      for (int e = 0; e < 8 * NK; ++e) pair(e);
+    }
+    // O^T += V^T P^T
+    top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kO; ++i) {
+      o[i % ND] = mfma32<BF16>(vf[i % kAhead], pb[i / ND], o[i % ND]);
+      if (i + kAhead < kO) vf[i % kAhead] = load_v(vat, i + kAhead);
+#pragma unroll
+      for (int e = i * 16 * NK / kO; e < (i + 1) * 16 * NK / kO; ++e) top = fmaxf(top, sn[e / 16][e % 16]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  if (t0 < t1) {
+    f32x16 s0[NK], s1[NK];
+#pragma unroll
+    for (int n = 0; n < NK; ++n) s1[n] = (f32x16){};
+    next = place(t0);
+    stage(next, false, 0);
+    stage(next, true, 0);
+    wait_loads();
+    __syncthreads();
+    if (t0 + 1 < t1) {
+      next = place(t0 + 1);
+      stage(next, false, 1);
+    }
+#pragma unroll
+    for (int i = 0; i < kS; ++i) s0[i % NK] = mfma32<BF16>(load_k(kaddr, i), qb[i / NK], i < NK ? (f32x16){} : s0[i % NK]);
+    top = max_of<NK>(s0);
+    for (int t = t0; t < t1; t += 2) {
+      step(t, s0, s1);
+      if (t + 1 < t1) step(t + 1, s1, s0);
+    }
   }
 
   l += __shfl_xor(l, 32, kWave);
-  const bool mine = rt.row0 + 32 * wave + (int)r32 < rt.rows;
+  // (once more from the lane: not held in registers through the loop)
+  uint32_t lane2 = lane_id();
+  asm volatile("" : "+v"(lane2));
+  const int orow32 = rt.row0 + 32 * wave + (int)(lane2 % 32), half4 = 4 * (int)(lane2 / 32);
+  const bool mine = orow32 < rt.rows;
   float odd = l * 0.f;  // NaN if something is not finite
 #pragma unroll
   for (int c = 0; c < ND; ++c)
 #pragma unroll
     for (int r = 0; r < 16; ++r) odd = fmaf(o[c][r], 0.f, odd);
-  if (ballot(mine && odd != odd)) {
+  if (ballot(mine && (odd != odd || (started && l == 0.f)))) {
     redo_rows<T, BF16>(a, part, rt, h, rt.row0 + 32 * wave, 32, tl, t0, t1, split, BN);
     return;
   }
   if (!mine) return;
-  const int64_t t = rt.tok0 + tok;
+  const int otok = orow32 / a.G, ohq = h * a.G + (orow32 - otok * a.G);
+  const int64_t t = rt.tok0 + otok;
+  const bool nothing = rt.base + otok < 0;
   if (part.n_splits > 1) {
-    const int64_t orow = (int64_t)split * a.n_q * a.Hq + t * a.Hq + hq;
-    if (half == 0) part.ml[orow] = make_float2(started ? -ref[0] : -INFINITY, pos < 0 ? -1.f : l * kUnit);
-    float* dst = part.o + orow * d + 4 * half;
+    const int64_t orow = (int64_t)split * a.n_q * a.Hq + t * a.Hq + ohq;
+    if (half4 == 0) part.ml[orow] = make_float2(started ? -shift : -INFINITY, nothing ? -1.f : l);
+    float* dst = part.o + orow * d + half4;
 #pragma unroll
     for (int c = 0; c < ND; ++c)
 #pragma unroll
       for (int r = 0; r < 16; r += 4)
-        *reinterpret_cast<f32x4*>(dst + 32 * c + 2 * r) =
-            (f32x4){o[c][r], o[c][r + 1], o[c][r + 2], o[c][r + 3]} * kUnit;
+        *reinterpret_cast<f32x4*>(dst + 32 * c + 2 * r) = (f32x4){o[c][r], o[c][r + 1], o[c][r + 2], o[c][r + 3]};
   } else {
-    const float inv = pos < 0 ? 0.f : 1.f / l;
-    uint16_t* dst = a.out + t * a.out_stride + hq * d + 4 * half;
+    const float inv = nothing ? 0.f : 1.f / l;
+    uint16_t* dst = a.out + t * a.out_stride + ohq * d + half4;
 #pragma unroll
     for (int c = 0; c < ND; ++c)
 #pragma unroll
@@ -452,7 +539,7 @@ __global__ __launch_bounds__(64) void k_paged_merge(PagedAttnArgs a, PartOut par
   for (int s = 0; s < part.n_splits; ++s) {
     const float2 ml = part.ml[s * rows + row];
     if (ml.x == -INFINITY && ml.y == 0.f) continue;
-    const float w = at_least(__builtin_amdgcn_exp2f((ml.x - M) * a.scale_log2));
+    const float w = at_least(__builtin_amdgcn_exp2f(ml.x - M));
     l = fmaf(ml.y, w, l);
 #pragma unroll
     for (int c = 0; c < T; ++c) o[c] = fmaf(part.o[(s * rows + row) * d + kTile * c + lane], w, o[c]);
