@@ -1,5 +1,7 @@
 // Causal attention of the new tokens of every request over its pages (gfx950), with an
 // optional sliding window and first tokens that stay visible.
+#include <type_traits>
+
 #include "mf_device.h"
 #include "paged.h"
 
@@ -302,9 +304,8 @@ __global__ __launch_bounds__(256, T == 4 ? 1 : 2) void k_paged_chunk(PagedAttnAr
     for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(qb[c]));
   }
 
-  // Wave w stages rows BN / 4 w .. of a tile. Pages hold 16 tokens or more, so a wave's rows share one. A row that no row
-  // of q sees is replaced by one that some does: the wave's group of 16 by the nearest with such a row, the row by the nearest of
-  // the group.
+  // Wave w stages rows BN / 4 w .. of a tile. Pages hold 16 tokens or more, so a wave's rows share one; a group of 16 of which no
+  // row of q sees any is replaced by the nearest with one that some does.
   const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
   struct Place {
     int64_t at;    // element of the group's first row in k and v
@@ -336,21 +337,30 @@ __global__ __launch_bounds__(256, T == 4 ? 1 : 2) void k_paged_chunk(PagedAttnAr
   const uint32_t lane_row = lane / kLanes, row_bytes = 2u * (uint32_t)p.token_stride;
   const uint32_t lane_off = lane_row * row_bytes, piece_k = 16u * (lane % kLanes ^ swizzle_k<T>(lane_row)),
                  piece_v = 16u * (lane % kLanes ^ swizzle_v<T>(lane_row));
-  auto stage = [&](const Place& w, bool values, uint32_t buf) {
-    const uint16_t* base = (values ? p.v : p.k) + w.at;
-    const uint32_t first = (BN / 4 * wave) & 15;  // row of the group
-    const uint32_t dst = lds0 + (buf + (values ? 2 : 0)) * kBuf + BN / 4 * wave * kRow;
+  const uint32_t group_row = (BN / 4 * wave) & 15;  // the wave's first row of the group
+  auto stage_load = [&](const Place& w, bool values, uint32_t buf, int n) {
+    const uint32_t r = group_row + kRowsPerLoad * n;  // of the group, this load's first
+    // (the places' XORs are linear in the row's bits: this load's share of them)
     uint32_t piece = values ? piece_v : piece_k, off = lane_off;
     asm volatile("" : "+v"(piece), "+v"(off));
-    const bool whole = w.from <= (int)first && w.to >= (int)first + BN / 4 - 1;
+    const uint32_t at = piece ^ (16u * (values ? swizzle_v<T>(r) : swizzle_k<T>(r)));
+    load_to_lds((values ? p.v : p.k) + w.at, off + r * row_bytes + at,
+                lds0 + (buf + (values ? 2 : 0)) * kBuf + (BN / 4 * wave + kRowsPerLoad * n) * kRow);
+  };
+  auto stage = [&](const Place& w, bool values, uint32_t buf) {
 #pragma unroll
+    for (int n = 0; n < kLoads; ++n) stage_load(w, values, buf, n);
+  };
+  // Waits for this wave's loads; then zeros for values of the tile that no row of q sees (they may be what memory held: 0
+  // times that is not 0).
+  auto settle_loads = [&](const Place& w, uint32_t buf) {
+    wait_loads();
+    if (w.from <= (int)group_row && w.to >= (int)group_row + BN / 4 - 1) return;
+#pragma unroll 1
     for (int n = 0; n < kLoads; ++n) {
-      const uint32_t r = first + kRowsPerLoad * n;  // of the group, this load's first
-      // (the places' XORs are linear in the row's bits: this load's share of them)
-      const uint32_t at = piece ^ (16u * (values ? swizzle_v<T>(r) : swizzle_k<T>(r)));
-      uint32_t row = off + r * row_bytes;
-      if (!whole) row = (uint32_t)min(max((int)(r + lane_row), w.from), w.to) * row_bytes;
-      load_to_lds(base, row + at, dst + kRowsPerLoad * n * kRow);
+      const int r = (int)(group_row + kRowsPerLoad * n + lane_row);
+      const uint32_t dst = lds0 + (buf + 2) * kBuf + (BN / 4 * wave + kRowsPerLoad * n) * kRow + 16 * lane;
+      if (r < w.from || r > w.to) *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(dst) = (u32x4){0u, 0u, 0u, 0u};
     }
   };
 
@@ -374,21 +384,10 @@ __global__ __launch_bounds__(256, T == 4 ? 1 : 2) void k_paged_chunk(PagedAttnAr
     return (u32x4){lo.x, lo.y, hi.x, hi.y};
   };
 
-  // One tile: its scores are in s (top: this lane's largest), those of the next go to sn while this one's probabilities are
-  // computed, their maximum while the values are multiplied.
+  // The first half of a tile: its scores are in s, this lane's largest in top. Tokens that a row does not see, and the shift.
   float top = -INFINITY;
-  Place next = {};
-  auto step = [&](int t, f32x16 (&s)[NK], f32x16 (&sn)[NK]) {
-    const uint32_t buf = (uint32_t)(t - t0) & 1u;
-    wait_loads();
-    __syncthreads();
-    if (t + 1 < t1) stage(next, true, buf ^ 1u);
-    if (t + 2 < t1) {
-      next = place(t + 2);
-      stage(next, false, buf);
-    }
+  auto settle = [&](int t, f32x16 (&s)[NK]) {
     const int j0 = tl.start(t, BN);
-    // Tokens that a row does not see.
     if (j0 + BN - 1 > pos0 || (a.window > 0 && j0 <= pos1 - a.window && j0 + BN > a.sinks)) {
 #pragma unroll
       for (int n = 0; n < NK; ++n)
@@ -412,38 +411,44 @@ __global__ __launch_bounds__(256, T == 4 ? 1 : 2) void k_paged_chunk(PagedAttnAr
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[c][r] *= alpha;
     }
-    // Probabilities, rounded; the sum is that of the rounded ones.
-    u32x4 pb[2 * NK];
-    auto pair = [&](int i) {
-      const float x = __builtin_amdgcn_exp2f(fmaf(s[i / 8][2 * (i % 8)], a.scale_log2, shift));
-      const float y = __builtin_amdgcn_exp2f(fmaf(s[i / 8][2 * (i % 8) + 1], a.scale_log2, shift));
-      const uint32_t xy = pack2<BF16>(x, y);
-      l = add_pair<BF16>(xy, l);
-      pb[i / 4][i % 4] = xy;
-    };
+  };
+  // Probabilities 2 i and 2 i + 1 of a lane, rounded; the sum is that of the rounded ones.
+  u32x4 pb[2 * NK];
+  auto pair = [&](const f32x16 (&s)[NK], int i) {
+    const float x = __builtin_amdgcn_exp2f(fmaf(s[i / 8][2 * (i % 8)], a.scale_log2, shift));
+    const float y = __builtin_amdgcn_exp2f(fmaf(s[i / 8][2 * (i % 8) + 1], a.scale_log2, shift));
+    const uint32_t xy = pack2<BF16>(x, y);
+    l = add_pair<BF16>(xy, l);
+    pb[i / 4][i % 4] = xy;
+  };
+  // A tile with one behind it: that one's scores go to sn under the exponentials of this one's, their maximum under the product
+  // with the values; the operands of a product are read kAhead products before it.
+  Place cur = {}, next = {};  // of the tile and of the one behind it
+  auto step = [&](int t, f32x16 (&s)[NK], f32x16 (&sn)[NK]) {
+    const uint32_t buf = (uint32_t)(t - t0) & 1u;
+    settle_loads(cur, buf);
+    __syncthreads();
     uint32_t kat = kaddr + (buf ^ 1u) * kBuf, vat = vaddr + buf * kBuf;
-    asm volatile("" : "+v"(kat), "+v"(vat));  // (as in stage)
-    u32x4 vf[kAhead];
-    if (t + 1 < t1) {
-      u32x4 kf[kAhead];
+    asm volatile("" : "+v"(kat), "+v"(vat));  // (as in stage_load)
+    u32x4 kf[kAhead], vf[kAhead];
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) kf[i] = load_k(kat, i);
+    for (int i = 0; i < kAhead; ++i) kf[i] = load_k(kat, i);
+    // The next tile's values and the keys of the one after it (behind the last, that once more, for nothing) are staged a
+    // load at each of the first products.
+    cur = next;
+    if (t + 2 < t1) next = place(t + 2);
+    settle(t, s);
 #pragma unroll
-      for (int i = 0; i < kS; ++i) {
-        sn[i % NK] = mfma32<BF16>(kf[i % kAhead], qb[i / NK], i < NK ? (f32x16){} : sn[i % NK]);
-        if (i + kAhead < kS) kf[i % kAhead] = load_k(kat, i + kAhead);
-        else vf[i + kAhead - kS] = load_v(vat, i + kAhead - kS);
+    for (int i = 0; i < kS; ++i) {
+      sn[i % NK] = mfma32<BF16>(kf[i % kAhead], qb[i / NK], i < NK ? (f32x16){} : sn[i % NK]);
+      if (i + kAhead < kS) kf[i % kAhead] = load_k(kat, i + kAhead);
+      else vf[i + kAhead - kS] = load_v(vat, i + kAhead - kS);
+      if (i < kLoads) stage_load(cur, true, buf ^ 1u, i);
+      else if (i < 2 * kLoads) stage_load(next, false, buf, i - kLoads);
 #pragma unroll
-        for (int e = i * 8 * NK / kS; e < (i + 1) * 8 * NK / kS; ++e) pair(e);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) vf[i] = load_v(vat, i);
-#pragma unroll
-      for (int e = 0; e < 8 * NK; ++e) pair(e);
+      for (int e = i * 8 * NK / kS; e < (i + 1) * 8 * NK / kS; ++e) pair(s, e);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    // O^T += V^T P^T
     top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kO; ++i) {
@@ -455,13 +460,26 @@ __global__ __launch_bounds__(256, T == 4 ? 1 : 2) void k_paged_chunk(PagedAttnAr
     }
   };
 
+  // The last tile.
+  auto finish = [&](int t, f32x16 (&s)[NK]) {
+    const uint32_t buf = (uint32_t)(t - t0) & 1u;
+    settle_loads(cur, buf);
+    __syncthreads();
+    settle(t, s);
+#pragma unroll
+    for (int e = 0; e < 8 * NK; ++e) pair(s, e);
+#pragma unroll
+    for (int i = 0; i < kO; ++i) {
+      o[i % ND] = mfma32<BF16>(load_v(vaddr + buf * kBuf, i), pb[i / ND], o[i % ND]);
+      if (i % kAhead == kAhead - 1) __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
   if (t0 < t1) {
     f32x16 s0[NK], s1[NK];
-#pragma unroll
-    for (int n = 0; n < NK; ++n) s1[n] = (f32x16){};
-    next = place(t0);
-    stage(next, false, 0);
-    stage(next, true, 0);
+    cur = next = place(t0);
+    stage(cur, false, 0);
+    stage(cur, true, 0);
     wait_loads();
     __syncthreads();
     if (t0 + 1 < t1) {
@@ -469,11 +487,21 @@ __global__ __launch_bounds__(256, T == 4 ? 1 : 2) void k_paged_chunk(PagedAttnAr
       stage(next, false, 1);
     }
 #pragma unroll
-    for (int i = 0; i < kS; ++i) s0[i % NK] = mfma32<BF16>(load_k(kaddr, i), qb[i / NK], i < NK ? (f32x16){} : s0[i % NK]);
+    for (int i = 0; i < kS; ++i) {
+      s0[i % NK] = mfma32<BF16>(load_k(kaddr, i), qb[i / NK], i < NK ? (f32x16){} : s0[i % NK]);
+      if (i % kAhead == kAhead - 1) __builtin_amdgcn_sched_barrier(0);
+    }
     top = max_of<NK>(s0);
-    for (int t = t0; t < t1; t += 2) {
+    int t = t0;
+    for (; t + 2 < t1; t += 2) {
       step(t, s0, s1);
-      if (t + 1 < t1) step(t + 1, s1, s0);
+      step(t + 1, s1, s0);
+    }
+    if (t + 1 < t1) {
+      step(t, s0, s1);
+      finish(t + 1, s1);
+    } else {
+      finish(t, s0);
     }
   }
 
