@@ -9,10 +9,12 @@ selection is disabled for every kernel.
 from __future__ import annotations
 
 import argparse
+import concurrent.futures
 import os
 import shutil
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -22,6 +24,9 @@ LIB = os.path.join(HERE, "libmustafar.so")
 SOURCES = ["api.hip", "compress.hip", "attention.hip", "attention_mfma.hip", "measure.hip", "paged_api.hip", "paged.hip",
            "paged_attn.hip"]
 ARCH = "gfx950"
+# Per source: k_paged_chunk runs one wave a SIMD; left to itself the compiler then gives every matrix
+# product an AGPR result and copies the scores, which the vector units read, out of them.
+EXTRA_FLAGS = {"paged_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def hipcc() -> str:
@@ -38,12 +43,20 @@ def common_flags() -> list[str]:
 
 
 def build(verbose: bool = False) -> str:
-    tmp = LIB + ".tmp"
-    cmd = [hipcc(), *common_flags(), "-shared", "-o", tmp,
-           *[os.path.join(CSRC, s) for s in SOURCES]]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+    """Compiles every source to an object of its own, a few at a time, and links them."""
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.run(cmd, check=True)
+
+    with tempfile.TemporaryDirectory() as objects:
+        outs = [os.path.join(objects, s + ".o") for s in SOURCES]
+        cmds = [[hipcc(), *common_flags(), *EXTRA_FLAGS.get(s, []), "-c", os.path.join(CSRC, s), "-o", o]
+                for s, o in zip(SOURCES, outs)]
+        with concurrent.futures.ThreadPoolExecutor(max_workers=4) as pool:
+            list(pool.map(run, cmds))
+        tmp = LIB + ".tmp"
+        run([hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *outs])
     os.replace(tmp, LIB)
     return LIB
 
@@ -53,7 +66,7 @@ def dump_asm(out_dir: str) -> None:
     os.makedirs(out_dir, exist_ok=True)
     for s in SOURCES:
         out = os.path.join(out_dir, s.replace(".hip", f"-{ARCH}.s"))
-        cmd = [hipcc(), *common_flags(), "--cuda-device-only", "-S", "-o", out,
+        cmd = [hipcc(), *common_flags(), *EXTRA_FLAGS.get(s, []), "--cuda-device-only", "-S", "-o", out,
                os.path.join(CSRC, s)]
         subprocess.run(cmd, check=True)
 

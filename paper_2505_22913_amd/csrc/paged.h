@@ -39,20 +39,20 @@ struct PagedAttnArgs {
   void* ws;          // their results when there are several
 };
 
-// Rows (new tokens times query heads of a kv-head) of a workgroup, and the workgroups that hold n_q tokens of B requests however
-// they are divided.
-constexpr int kChunkRows = 128;
-inline int64_t paged_tiles(const PagedView& p, int G, int n_q) { return (int64_t)n_q * G / kChunkRows + p.B; }
+// Waves of a workgroup, of 32 rows (new tokens times query heads of a kv-head) each; d = 64 T.
+constexpr int chunk_waves(int T) { return T == 4 ? 4 : 8; }
+// Workgroups that hold the rows of n_q tokens of B requests however they are divided.
+inline int64_t paged_tiles(const PagedView& p, int G, int n_q) { return (int64_t)n_q * G / (32 * chunk_waves(p.d / 64)) + p.B; }
 
 // Bytes of the ranges' results: (reference, sum) and d fp32 values of every row and query head.
 inline int64_t paged_ws_bytes(const PagedView& p, int Hq, int n_q, int n_splits) {
   return n_splits <= 1 ? 0 : (int64_t)n_splits * n_q * Hq * (p.d + 2) * 4;
 }
 
-// Ranges that a call takes by itself: two workgroups a CU, each of at least four tiles.
+// Ranges that a call takes by itself: a workgroup a CU, each of at least four tiles.
 inline int paged_splits(const PagedView& p, int G, int n_q, int max_q, int64_t max_tokens) {
   const int64_t groups = paged_tiles(p, G, n_q) * p.H, tiles = max_tokens / 64 / 4;
-  const int64_t n = 512 / groups;
+  const int64_t n = 256 / groups;
   return (int)(n < 1 || tiles < 1 ? 1 : n < tiles ? n : tiles);
 }
 hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s);

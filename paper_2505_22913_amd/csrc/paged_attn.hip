@@ -112,6 +112,11 @@ struct TileList {
     }
     n = hi < 0 ? 0 : n_first + hi / BN - first + 1;
   }
+  // Tiles of the list that start at or before token j.
+  __device__ __forceinline__ int count_to(int j, int BN) const {
+    if (j < 0) return 0;
+    return j / BN < first ? min(n_first, j / BN + 1) : n_first + j / BN - first + 1;
+  }
   __device__ __forceinline__ int start(int i, int BN) const { return (i < n_first ? i : first + i - n_first) * BN; }
 };
 
@@ -211,14 +216,21 @@ __device__ __forceinline__ void redo_rows(const PagedAttnArgs& a, const PartOut&
 }
 
 // ------------------------------------------------------------------------------------------
-// k_paged_chunk: 128 rows a workgroup, 32 a wave, tiles of 64 tokens (32 at d = 256).
+// k_paged_chunk: 32 rows a wave, 8 waves a workgroup (4 at d = 256), tiles of 64 tokens (32).
 //
 // Both products have the rows as columns: S^T = K Q^T leaves a lane with scores of one row (column l % 32),
 // so the softmax's shift and sum are per lane (two lanes hold a row's tokens), and its 8-token groups,
 // rounded to the type, are the B operand of O^T = V^T P^T as they lie; V^T comes out of LDS transposed.
+//
+// X(t) is the products of tile t + 1's scores with the exponentials of tile t's between them, Y(t) the product with tile t's
+// values with the maximum of tile t + 1's scores between. X is bound by the vector units, Y by the matrix cores, and
+// waves w and w + 4 share a SIMD: the second four run half a tile late. A barrier a tile opens slot t, in which the first four do
+// X(t), Y(t) and the second Y(t - 1), X(t); both read the keys of tile t + 1, the first the values of tile t, the second those
+// of tile t - 1 (and the first of tile t's, ahead). Tiles are staged kDepth slots ahead, into buffers last read a slot before.
 // ------------------------------------------------------------------------------------------
 template <int T>
 constexpr int chunk_tile() { return T == 4 ? 32 : 64; }
+constexpr int kDepth = 2, kRingK = kDepth + 1, kRingV = kDepth + 2;
 
 // A probability is 2^kBias at the reference, which follows the largest score once that is more than 2^kSlack above it:
 // at most 2^15 (inside fp16), and fp16 keeps those down to 2^-31 of the reference. It is exp2(score * scale +
@@ -244,7 +256,8 @@ __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, u
   asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
                : "=&s"(m0) : "s"(dst), "v"(offset), "s"(base) : "memory");
 }
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(LEFT) : "memory"); }
 
 template <typename V>
 __device__ __forceinline__ V lds_load(uint32_t byte_addr) {
@@ -274,101 +287,132 @@ __device__ __forceinline__ float max_of(const f32x16 (&s)[NK]) {
 }
 
 template <int T, bool BF16>
-__global__ __launch_bounds__(256, T == 4 ? 1 : 2) void k_paged_chunk(PagedAttnArgs a, PartOut part) {
+__global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_paged_chunk(PagedAttnArgs a, PartOut part) {
+  constexpr int NW = chunk_waves(T), NQ = 1, BW = 32 * NQ, BM = NW * BW;
   constexpr int d = kTile * T, BN = chunk_tile<T>(), NK = BN / 32, NC = d / 16, ND = d / 32;
   constexpr uint32_t kRow = 2 * d, kBuf = BN * kRow;  // bytes
-  constexpr int kRowsPerLoad = 1024 / (2 * d), kLoads = BN / 4 / kRowsPerLoad;
-  extern __shared__ __align__(1024) unsigned char smem[];  // K, K, V, V
+  constexpr int kWaveRows = BN / NW, kRowsPerLoad = 1024 / (2 * d), kLoads = kWaveRows / kRowsPerLoad;
+  static_assert(kLoads * kRowsPerLoad == kWaveRows && 16 % kWaveRows == 0, "a wave's rows");
+  __shared__ __align__(1024) unsigned char smem[(kRingK + kRingV) * kBuf];  // buffers of keys, of values
   const PagedView& p = a.p;
   const int h = blockIdx.x % p.H, split = (blockIdx.x / p.H) % part.n_splits;
   const int tile = (int)(gridDim.x / (p.H * part.n_splits)) - 1 - (int)(blockIdx.x / (p.H * part.n_splits));
-  const RowTile rt = row_tile(a, tile, kChunkRows);
+  const RowTile rt = row_tile(a, tile, BM);
   if (rt.row0 >= rt.rows) return;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
   const uint32_t lane = lane_id(), r32 = lane % 32, half = lane / 32;
-  const int row = min(rt.row0 + 32 * wave + (int)r32, rt.rows - 1);
-  const int tok = row / a.G, pos = rt.base + tok;
-  const int last = min(rt.row0 + kChunkRows, rt.rows) - 1;
-  const int pos0 = rt.base + rt.row0 / a.G, pos1 = rt.base + last / a.G;
-  const TileList tl(pos0, pos1, a.window, a.sinks, BN);
-  const int t0 = (int)((int64_t)tl.n * split / part.n_splits), t1 = (int)((int64_t)tl.n * (split + 1) / part.n_splits);
+  const int wrow = rt.row0 + BW * wave;  // the wave's first row
+  const TileList tl(rt.base + rt.row0 / a.G, rt.base + (min(rt.row0 + BM, rt.rows) - 1) / a.G, a.window, a.sinks, BN);
+  const int t0 = (int)((int64_t)tl.n * split / part.n_splits);
+  const int n = (int)((int64_t)tl.n * (split + 1) / part.n_splits) - t0;  // tiles of the workgroup
+  // The wave's rows' positions, and its tiles: those behind its last position are the others'.
+  const int pos0 = rt.base + min(wrow, rt.rows - 1) / a.G, pos1 = rt.base + min(wrow + BW - 1, rt.rows - 1) / a.G;
+  const int mine = wrow >= rt.rows || pos1 < 0 ? 0 : min(n, max(tl.count_to(pos1, BN) - t0, 0));
 
-  // Q as the B operand: column = row of the wave, k = 16 c + 8 half + i.
-  u32x4 qb[NC];
-  {
+  // Tiles [clean0, clean1) of the list are seen whole by every row of the wave, [whole0, whole1) by some row of the workgroup.
+  const int clean0 = a.window > 0 ? tl.count_to(pos1 - a.window, BN) - t0 : 0, clean1 = tl.count_to(pos0 - BN + 1, BN) - t0;
+  const int whole0 = tl.count_to(tl.lo - 1, BN) - t0, whole1 = tl.count_to(tl.hi - BN + 1, BN) - t0;
+
+  // Q as the B operand: column = row of the block, k = 16 c + 8 half + i.
+  u32x4 qb[NQ][NC];
+  int pos[NQ];
+#pragma unroll
+  for (int b = 0; b < NQ; ++b) {
+    const int row = min(wrow + 32 * b + (int)r32, rt.rows - 1), tok = row / a.G;
+    pos[b] = rt.base + tok;
     const uint16_t* q = a.q + (int64_t)(rt.tok0 + tok) * a.q_stride + (h * a.G + row - tok * a.G) * d + 8 * half;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) qb[c] = *reinterpret_cast<const u32x4*>(q + 16 * c);
-    // (here: a wait for them inside the loop would be one for a tile's loads too)
-#pragma unroll
-    for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(qb[c]));
+    for (int c = 0; c < NC; ++c) qb[b][c] = *reinterpret_cast<const u32x4*>(q + 16 * c);
   }
+  // (here: a wait for them inside the loop would be one for the tiles' loads too)
+#pragma unroll
+  for (int b = 0; b < NQ; ++b)
+#pragma unroll
+    for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(qb[b][c]));
 
-  // Wave w stages rows BN / 4 w .. of a tile. Pages hold 16 tokens or more, so a wave's rows share one; a group of 16 of which no
-  // row of q sees any is replaced by the nearest with one that some does.
+  // Staging. Wave w loads rows kWaveRows w .. of a tile. Pages hold 16 tokens or more, so they share one; a group of 16 of which
+  // no row of q sees any is replaced by the nearest with one that some does. Lane i holds the offset in k and v of the rows of
+  // tile 64 m + i of the workgroup's.
   const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
-  struct Place {
-    int64_t at;    // element of the group's first row in k and v
-    int from, to;  // rows of the group that some row of q sees
-  };
-  // The pages of 64 tiles at a time, one a lane.
-  int pages = 0;
-  auto group_of = [&](int i) {
-    const int j = (tl.start(i, BN) + BN / 4 * wave) & ~15;
-    return j < tl.sinks ? j : min(max(j, tl.lo & ~15), tl.hi & ~15);
-  };
-  auto place = [&](int i) {
-    if (((i - t0) & (kWave - 1)) == 0) {
-      const int page = p.table[(int64_t)rt.b * p.max_pages + (group_of(min(i + (int)lane, t1 - 1)) >> p.log2_page)];
-      pages = (uint32_t)page < (uint32_t)p.n_pages ? page : 0;
-    }
-    const int g0 = group_of(i), page = __builtin_amdgcn_readlane(pages, (i - t0) & (kWave - 1));
-    Place w;
-    w.at = (int64_t)page * p.page_stride + (int64_t)h * p.head_stride +
-           (int64_t)(g0 & ((1 << p.log2_page) - 1)) * p.token_stride;
-    const bool first = g0 < tl.sinks;
-    w.from = first ? 0 : max(tl.lo - g0, 0);
-    w.to = min((first && tl.lo > g0 + 15 ? tl.sinks - 1 : tl.hi) - g0, 15);
-    return w;
-  };
-  // This lane's row of the wave's first load, in bytes, and its piece of the row. (Opaque in every call: kept in
-  // registers for each load of a tile, their addresses would push others into scratch, whose loads wait for a tile's.)
   constexpr uint32_t kLanes = kWave / kRowsPerLoad;  // of a row
-  const uint32_t lane_row = lane / kLanes, row_bytes = 2u * (uint32_t)p.token_stride;
+  const uint32_t group_row = (kWaveRows * wave) & 15, lane_row = lane / kLanes, row_bytes = 2u * (uint32_t)p.token_stride;
   const uint32_t lane_off = lane_row * row_bytes, piece_k = 16u * (lane % kLanes ^ swizzle_k<T>(lane_row)),
                  piece_v = 16u * (lane % kLanes ^ swizzle_v<T>(lane_row));
-  const uint32_t group_row = (BN / 4 * wave) & 15;  // the wave's first row of the group
-  auto stage_load = [&](const Place& w, bool values, uint32_t buf, int n) {
-    const uint32_t r = group_row + kRowsPerLoad * n;  // of the group, this load's first
+  uint32_t at_lo = 0, at_hi = 0;
+  auto look_up = [&](int first) __attribute__((always_inline)) {
+    int g0 = (tl.start(t0 + min(first + (int)lane, n - 1), BN) + kWaveRows * wave) & ~15;
+    if (g0 >= tl.sinks) g0 = min(max(g0, tl.lo & ~15), tl.hi & ~15);
+    int page = p.table[(int64_t)rt.b * p.max_pages + (g0 >> p.log2_page)];
+    if ((uint32_t)page >= (uint32_t)p.n_pages) page = 0;
+    const int64_t at = 2 * ((int64_t)page * p.page_stride + (int64_t)h * p.head_stride +
+                            (int64_t)((g0 & ((1 << p.log2_page) - 1)) + (int)group_row) * p.token_stride);
+    at_lo = (uint32_t)at;
+    at_hi = (uint32_t)(at >> 32);
+  };
+  auto stage_load = [&](const void* base, uint32_t piece, bool values, int buf, int i) __attribute__((always_inline)) {
     // (the places' XORs are linear in the row's bits: this load's share of them)
-    uint32_t piece = values ? piece_v : piece_k, off = lane_off;
-    asm volatile("" : "+v"(piece), "+v"(off));
-    const uint32_t at = piece ^ (16u * (values ? swizzle_v<T>(r) : swizzle_k<T>(r)));
-    load_to_lds((values ? p.v : p.k) + w.at, off + r * row_bytes + at,
-                lds0 + (buf + (values ? 2 : 0)) * kBuf + (BN / 4 * wave + kRowsPerLoad * n) * kRow);
+    const uint32_t r = kWaveRows * wave + kRowsPerLoad * i, x = 16u * (values ? swizzle_v<T>(r) : swizzle_k<T>(r));
+    load_to_lds(base, lane_off + kRowsPerLoad * i * row_bytes + (piece ^ x),
+                lds0 + (uint32_t)(buf + (values ? kRingK : 0)) * kBuf + (kWaveRows * wave + kRowsPerLoad * i) * kRow);
   };
-  auto stage = [&](const Place& w, bool values, uint32_t buf) {
+  // Where the keys of tile t (behind the last: the last, for nothing) lie; the values of the tile before lay where its keys did.
+  uint64_t k_at = 0, v_at = 0;
+  auto place = [&](int t) __attribute__((always_inline)) {
+    t = min(t, n - 1);
+    if (t % kWave == 0) look_up(t);
+    v_at = k_at;
+    k_at = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)at_hi, t % kWave) << 32 |
+           (uint32_t)__builtin_amdgcn_readlane((int)at_lo, t % kWave);
+  };
+  int k_buf = 0, v_buf = 0;  // where the next keys and values go
+  auto stage_k = [&]() __attribute__((always_inline)) {
+    uint32_t piece = piece_k;
+    asm volatile("" : "+v"(piece));  // (kept in registers for every load, the addresses would fill them)
 #pragma unroll
-    for (int n = 0; n < kLoads; ++n) stage_load(w, values, buf, n);
+    for (int i = 0; i < kLoads; ++i) stage_load(reinterpret_cast<const unsigned char*>(p.k) + k_at, piece, false, k_buf, i);
+    k_buf = k_buf + 1 == kRingK ? 0 : k_buf + 1;
   };
-  // Waits for this wave's loads; then zeros for values of the tile that no row of q sees (they may be what memory held: 0
-  // times that is not 0).
-  auto settle_loads = [&](const Place& w, uint32_t buf) {
-    wait_loads();
-    if (w.from <= (int)group_row && w.to >= (int)group_row + BN / 4 - 1) return;
+  auto stage_v = [&]() __attribute__((always_inline)) {
+    uint32_t piece = piece_v;
+    asm volatile("" : "+v"(piece));
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) stage_load(reinterpret_cast<const unsigned char*>(p.v) + v_at, piece, true, v_buf, i);
+    v_buf = v_buf + 1 == kRingV ? 0 : v_buf + 1;
+  };
+  // Slot i: the keys of tile i + 1 and the values of tile i have arrived for every wave, and nobody reads any more what slot i - 1
+  // read of them; those of slot i + kDepth are started. Values that no row of q sees are cleared (they may be what memory
+  // held: 0 times that is not 0).
+  int slot = 0;
+  auto arrive = [&]() __attribute__((always_inline)) {
+    wait_loads<2 * kLoads * (kDepth - 1)>();
+    if (slot < n && (slot < whole0 || slot >= whole1)) {
+      const int j0 = tl.start(t0 + slot, BN);
+      uint32_t zero_at = lds0 + (uint32_t)(kRingK + slot % kRingV) * kBuf + kWaveRows * wave * kRow + 16 * lane;
 #pragma unroll 1
-    for (int n = 0; n < kLoads; ++n) {
-      const int r = (int)(group_row + kRowsPerLoad * n + lane_row);
-      const uint32_t dst = lds0 + (buf + 2) * kBuf + (BN / 4 * wave + kRowsPerLoad * n) * kRow + 16 * lane;
-      if (r < w.from || r > w.to) *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(dst) = (u32x4){0u, 0u, 0u, 0u};
+      for (int i = 0; i < kLoads; ++i, zero_at += kRowsPerLoad * kRow) {
+        const int x = j0 + kWaveRows * wave + kRowsPerLoad * i + (int)lane_row;
+        if (x > tl.hi || (x < tl.lo && x >= tl.sinks))
+          *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(zero_at) = (u32x4){0u, 0u, 0u, 0u};
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    ++slot;
+    place(slot + kDepth);
+    stage_k();
+    stage_v();
   };
 
-  float l = 0.f, shift = 0.f;
-  bool started = false;  // the shift is that of a visible score
-  f32x16 o[ND];
+  const float inv_scale = 1.f / a.scale_log2;
+  float l[NQ] = {}, shift[NQ] = {}, top[NQ], limit[NQ];
 #pragma unroll
-  for (int c = 0; c < ND; ++c) o[c] = (f32x16){};
+  for (int b = 0; b < NQ; ++b) limit[b] = -INFINITY;
+  f32x16 o[NQ][ND];
+#pragma unroll
+  for (int b = 0; b < NQ; ++b)
+#pragma unroll
+    for (int c = 0; c < ND; ++c) o[b][c] = (f32x16){};
 
   // Operand i of the scores (tokens 32 (i % NK) .., channels 16 (i / NK) ..) and of the outputs (channels 32 (i % ND) .., tokens
   // 16 (i / ND) .., k slot 8 half + i being token 8 (i / 4) + 4 half + i % 4, as the scores lie). A row of LDS is a
@@ -376,172 +420,221 @@ __global__ __launch_bounds__(256, T == 4 ? 1 : 2) void k_paged_chunk(PagedAttnAr
   constexpr int kS = NK * NC, kO = 2 * NK * ND, kAhead = 4;
   const uint32_t kaddr = lds0 + r32 * kRow + 16u * (half ^ swizzle_k<T>(r32));
   const uint32_t vrow = 4 * half + (lane % 16) / 4;
-  const uint32_t vaddr = lds0 + 2 * kBuf + vrow * kRow + 16u * ((((lane / 16) & 1) * 2 + (lane % 4) / 2) ^ swizzle_v<T>(vrow)) + 8 * (lane & 1);
-  auto load_k = [&](uint32_t at, int i) { return lds_load<u32x4>((at ^ (32u * (i / NK))) + 32 * (i % NK) * kRow); };
-  auto load_v = [&](uint32_t at, int i) {
+  const uint32_t vaddr = lds0 + kRingK * kBuf + vrow * kRow + 16u * ((((lane / 16) & 1) * 2 + (lane % 4) / 2) ^ swizzle_v<T>(vrow)) + 8 * (lane & 1);
+  auto load_k = [&](uint32_t at, int i) __attribute__((always_inline)) { return lds_load<u32x4>((at ^ (32u * (i / NK))) + 32 * (i % NK) * kRow); };
+  auto load_v = [&](uint32_t at, int i) __attribute__((always_inline)) {
     const uint32_t x = (at ^ (64u * (i % ND))) + 16 * (i / ND) * kRow;
     const u32x2 lo = lds_load_tr(x), hi = lds_load_tr(x + 8 * kRow);
     return (u32x4){lo.x, lo.y, hi.x, hi.y};
   };
 
-  // The first half of a tile: its scores are in s, this lane's largest in top. Tokens that a row does not see, and the shift.
-  float top = -INFINITY;
-  auto settle = [&](int t, f32x16 (&s)[NK]) {
-    const int j0 = tl.start(t, BN);
-    if (j0 + BN - 1 > pos0 || (a.window > 0 && j0 <= pos1 - a.window && j0 + BN > a.sinks)) {
+  // The scores of a tile, this lane's largest in top, are masked and the shift follows them: limit is the largest score that
+  // it leaves alone (-inf before the first), a row's other lane has the same.
+  auto settle = [&](int t, f32x16 (&s)[NQ][NK]) __attribute__((always_inline)) {
+    if (t < clean0 || t >= clean1) {
+      const int j0 = tl.start(t0 + t, BN);
 #pragma unroll
-      for (int n = 0; n < NK; ++n)
+      for (int b = 0; b < NQ; ++b) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int j = j0 + 32 * n + 8 * (r / 4) + 4 * (int)half + r % 4;
-          if (!sees(pos, j, a.window, a.sinks)) s[n][r] = -INFINITY;
-        }
-      top = max_of<NK>(s);
+        for (int n = 0; n < NK; ++n)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int j = j0 + 32 * n + 8 * (r / 4) + 4 * (int)half + r % 4;
+            if (!sees(pos[b], j, a.window, a.sinks)) s[b][n][r] = -INFINITY;
+          }
+        top[b] = max_of<NK>(s[b]);
+      }
     }
-    top = max_halves(top);
-    const bool move = started ? fmaf(top, a.scale_log2, shift) > kBias + kSlack : top > -INFINITY;
-    if (ballot(move)) {
-      const float to = move ? fmaf(-top, a.scale_log2, kBias) : shift;
-      const float alpha = started ? __builtin_amdgcn_exp2f(to - shift) : 1.f;  // (nothing is there before the start)
-      started |= move;
-      shift = to;
-      l *= alpha;
+    bool any = false;
+#pragma unroll
+    for (int b = 0; b < NQ; ++b) any |= top[b] > limit[b];
+    if (ballot(any)) {
+#pragma unroll
+      for (int b = 0; b < NQ; ++b) {
+        top[b] = max_halves(top[b]);
+        const bool move = top[b] > limit[b], started = limit[b] > -INFINITY;
+        const float to = move ? fmaf(-top[b], a.scale_log2, kBias) : shift[b];
+        const float alpha = started ? __builtin_amdgcn_exp2f(to - shift[b]) : 1.f;  // (nothing is there before the start)
+        if (move) limit[b] = fmaf(kSlack, inv_scale, top[b]);
+        shift[b] = to;
+        l[b] *= alpha;
+#pragma unroll
+        for (int c = 0; c < ND; ++c)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[b][c][r] *= alpha;
+      }
+    }
+  };
+  // Probabilities 2 i and 2 i + 1 of a lane's row of block b, rounded; the sum is that of the rounded ones.
+  u32x4 pb[NQ][2 * NK];
+  auto exponentials = [&](f32x16 (&s)[NQ][NK], int b, int i) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      s[b][i / 8][2 * (i % 8) + e] = __builtin_amdgcn_exp2f(fmaf(s[b][i / 8][2 * (i % 8) + e], a.scale_log2, shift[b]));
+    }
+  };
+  auto round_pair = [&](const f32x16 (&s)[NQ][NK], int b, int i) __attribute__((always_inline)) {
+    const uint32_t xy = pack2<BF16>(s[b][i / 8][2 * (i % 8)], s[b][i / 8][2 * (i % 8) + 1]);
+    l[b] = add_pair<BF16>(xy, l[b]);
+    pb[b][i / 4][i % 4] = xy;
+  };
+  const bool late = NW == 8 && wave >= 4;  // (see above)
+  u32x4 kf[kAhead], vf[kAhead];
+  int kr = 1, vr = 0;  // the buffers of tile t + 1's keys and tile t's values
+  // Step t with a tile behind it. Operands are read kAhead before they are used.
+  auto step = [&](int t, f32x16 (&s)[NQ][NK], f32x16 (&sn)[NQ][NK]) __attribute__((always_inline)) {
+    if (!late) arrive();
+    uint32_t kat = kaddr + (uint32_t)kr * kBuf, vat = vaddr + (uint32_t)vr * kBuf;
+    asm volatile("" : "+v"(kat), "+v"(vat));  // (as in stage_k)
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) kf[i] = load_k(kat, i);
+#pragma unroll
+    for (int i = 0; i < kS; ++i) {
+#pragma unroll
+      for (int b = 0; b < NQ; ++b) {
+        sn[b][i % NK] = mfma32<BF16>(kf[i % kAhead], qb[b][i / NK], i < NK ? (f32x16){} : sn[b][i % NK]);
+        if (b == NQ - 1) {
+          if (i + kAhead < kS) kf[i % kAhead] = load_k(kat, i + kAhead);
+          else vf[i + kAhead - kS] = load_v(vat, i + kAhead - kS);
+        }
+#pragma unroll
+        for (int e = i * 8 * NK / kS; e < (i + 1) * 8 * NK / kS; ++e) exponentials(s, b, e);
+        // (rounded a product later, when they are there)
+#pragma unroll
+        for (int e = (i - 1) * 8 * NK / kS; i > 0 && e < i * 8 * NK / kS; ++e) round_pair(s, b, e);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < NQ; ++b) {
+#pragma unroll
+      for (int e = (kS - 1) * 8 * NK / kS; e < 8 * NK; ++e) round_pair(s, b, e);
+      top[b] = -INFINITY;
+    }
+    if (late) arrive();
+    asm volatile("" : "+v"(vat));
+#pragma unroll
+    for (int i = 0; i < kO; ++i)
+#pragma unroll
+      for (int b = 0; b < NQ; ++b) {
+        o[b][i % ND] = mfma32<BF16>(vf[i % kAhead], pb[b][i / ND], o[b][i % ND]);
+        if (b == NQ - 1 && i + kAhead < kO) vf[i % kAhead] = load_v(vat, i + kAhead);
+#pragma unroll
+        for (int e = i * 16 * NK / kO; e < (i + 1) * 16 * NK / kO; ++e) top[b] = fmaxf(top[b], sn[b][e / 16][e % 16]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    settle(t + 1, sn);
+    kr = kr + 1 == kRingK ? 0 : kr + 1;
+    vr = vr + 1 == kRingV ? 0 : vr + 1;
+  };
+  // The wave's last step.
+  auto finish = [&](f32x16 (&s)[NQ][NK]) __attribute__((always_inline)) {
+    if (!late) arrive();
+#pragma unroll
+    for (int b = 0; b < NQ; ++b)
+#pragma unroll
+      for (int e = 0; e < 8 * NK; ++e) {
+        exponentials(s, b, e);
+        round_pair(s, b, e);
+      }
+    if (late) arrive();
+    const uint32_t vat = vaddr + (uint32_t)vr * kBuf;
+#pragma unroll
+    for (int i = 0; i < kO; ++i) {
+      vf[0] = load_v(vat, i);
+#pragma unroll
+      for (int b = 0; b < NQ; ++b) o[b][i % ND] = mfma32<BF16>(vf[0], pb[b][i / ND], o[b][i % ND]);
+      if (i % kAhead == kAhead - 1) __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  if (n > 0) {
+    f32x16 s0[NQ][NK], s1[NQ][NK];
+    // The first tile's keys, then what the first kDepth slots need.
+    place(0);
+    stage_k();
+#pragma unroll 1
+    for (int i = 0; i < kDepth; ++i) {
+      place(i + 1);
+      stage_k();
+      stage_v();
+    }
+    wait_loads<2 * kLoads * kDepth>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (mine > 0) {
+#pragma unroll
+      for (int i = 0; i < kS; ++i) {
+        kf[0] = load_k(kaddr, i);
+#pragma unroll
+        for (int b = 0; b < NQ; ++b) s0[b][i % NK] = mfma32<BF16>(kf[0], qb[b][i / NK], i < NK ? (f32x16){} : s0[b][i % NK]);
+        if (i % kAhead == kAhead - 1) __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int b = 0; b < NQ; ++b) top[b] = max_of<NK>(s0[b]);
+      settle(0, s0);
+      if (late) arrive();
+      int t = 0;
+      for (; t + 2 < mine; t += 2) {
+        step(t, s0, s1);
+        step(t + 1, s1, s0);
+      }
+      if (t + 1 < mine) {
+        step(t, s0, s1);
+        finish(s1);
+      } else {
+        finish(s0);
+      }
+    }
+    // Slots of the other waves; none may end while its loads are under way.
+    while (slot <= n) arrive();
+    wait_loads<0>();
+  }
+
+  // (the rows once more from the lane: not held in registers through the loop)
+  uint32_t lane2 = lane_id();
+  asm volatile("" : "+v"(lane2));
+  const int row = wrow + (int)(lane2 % 32), half4 = 4 * (int)(lane2 / 32);
+  bool odd = false;  // something is not finite
+#pragma unroll
+  for (int b = 0; b < NQ; ++b) {
+    l[b] += __shfl_xor(l[b], 32, kWave);
+    float z = l[b] * 0.f;
+#pragma unroll
+    for (int c = 0; c < ND; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) z = fmaf(o[b][c][r], 0.f, z);
+    odd |= row + 32 * b < rt.rows && (z != z || (limit[b] > -INFINITY && l[b] == 0.f));
+  }
+  if (ballot(odd)) {
+    redo_rows<T, BF16>(a, part, rt, h, wrow, BW, tl, t0, t0 + n, split, BN);
+    return;
+  }
+#pragma unroll
+  for (int b = 0; b < NQ; ++b) {
+    if (row + 32 * b >= rt.rows) continue;
+    const int tok = (row + 32 * b) / a.G, hq = h * a.G + (row + 32 * b - tok * a.G);
+    const int64_t t = rt.tok0 + tok;
+    const bool nothing = rt.base + tok < 0;
+    if (part.n_splits > 1) {
+      const int64_t orow = (int64_t)split * a.n_q * a.Hq + t * a.Hq + hq;
+      if (half4 == 0) part.ml[orow] = make_float2(limit[b] > -INFINITY ? -shift[b] : -INFINITY, nothing ? -1.f : l[b]);
+      float* dst = part.o + orow * d + half4;
 #pragma unroll
       for (int c = 0; c < ND; ++c)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[c][r] *= alpha;
-    }
-  };
-  // Probabilities 2 i and 2 i + 1 of a lane, rounded; the sum is that of the rounded ones.
-  u32x4 pb[2 * NK];
-  auto pair = [&](const f32x16 (&s)[NK], int i) {
-    const float x = __builtin_amdgcn_exp2f(fmaf(s[i / 8][2 * (i % 8)], a.scale_log2, shift));
-    const float y = __builtin_amdgcn_exp2f(fmaf(s[i / 8][2 * (i % 8) + 1], a.scale_log2, shift));
-    const uint32_t xy = pack2<BF16>(x, y);
-    l = add_pair<BF16>(xy, l);
-    pb[i / 4][i % 4] = xy;
-  };
-  // A tile with one behind it: that one's scores go to sn under the exponentials of this one's, their maximum under the product
-  // with the values; the operands of a product are read kAhead products before it.
-  Place cur = {}, next = {};  // of the tile and of the one behind it
-  auto step = [&](int t, f32x16 (&s)[NK], f32x16 (&sn)[NK]) {
-    const uint32_t buf = (uint32_t)(t - t0) & 1u;
-    settle_loads(cur, buf);
-    __syncthreads();
-    uint32_t kat = kaddr + (buf ^ 1u) * kBuf, vat = vaddr + buf * kBuf;
-    asm volatile("" : "+v"(kat), "+v"(vat));  // (as in stage_load)
-    u32x4 kf[kAhead], vf[kAhead];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) kf[i] = load_k(kat, i);
-    // The next tile's values and the keys of the one after it (behind the last, that once more, for nothing) are staged a
-    // load at each of the first products.
-    cur = next;
-    if (t + 2 < t1) next = place(t + 2);
-    settle(t, s);
-#pragma unroll
-    for (int i = 0; i < kS; ++i) {
-      sn[i % NK] = mfma32<BF16>(kf[i % kAhead], qb[i / NK], i < NK ? (f32x16){} : sn[i % NK]);
-      if (i + kAhead < kS) kf[i % kAhead] = load_k(kat, i + kAhead);
-      else vf[i + kAhead - kS] = load_v(vat, i + kAhead - kS);
-      if (i < kLoads) stage_load(cur, true, buf ^ 1u, i);
-      else if (i < 2 * kLoads) stage_load(next, false, buf, i - kLoads);
-#pragma unroll
-      for (int e = i * 8 * NK / kS; e < (i + 1) * 8 * NK / kS; ++e) pair(s, e);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    top = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < kO; ++i) {
-      o[i % ND] = mfma32<BF16>(vf[i % kAhead], pb[i / ND], o[i % ND]);
-      if (i + kAhead < kO) vf[i % kAhead] = load_v(vat, i + kAhead);
-#pragma unroll
-      for (int e = i * 16 * NK / kO; e < (i + 1) * 16 * NK / kO; ++e) top = fmaxf(top, sn[e / 16][e % 16]);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  };
-
-  // The last tile.
-  auto finish = [&](int t, f32x16 (&s)[NK]) {
-    const uint32_t buf = (uint32_t)(t - t0) & 1u;
-    settle_loads(cur, buf);
-    __syncthreads();
-    settle(t, s);
-#pragma unroll
-    for (int e = 0; e < 8 * NK; ++e) pair(s, e);
-#pragma unroll
-    for (int i = 0; i < kO; ++i) {
-      o[i % ND] = mfma32<BF16>(load_v(vaddr + buf * kBuf, i), pb[i / ND], o[i % ND]);
-      if (i % kAhead == kAhead - 1) __builtin_amdgcn_sched_barrier(0);
-    }
-  };
-
-  if (t0 < t1) {
-    f32x16 s0[NK], s1[NK];
-    cur = next = place(t0);
-    stage(cur, false, 0);
-    stage(cur, true, 0);
-    wait_loads();
-    __syncthreads();
-    if (t0 + 1 < t1) {
-      next = place(t0 + 1);
-      stage(next, false, 1);
-    }
-#pragma unroll
-    for (int i = 0; i < kS; ++i) {
-      s0[i % NK] = mfma32<BF16>(load_k(kaddr, i), qb[i / NK], i < NK ? (f32x16){} : s0[i % NK]);
-      if (i % kAhead == kAhead - 1) __builtin_amdgcn_sched_barrier(0);
-    }
-    top = max_of<NK>(s0);
-    int t = t0;
-    for (; t + 2 < t1; t += 2) {
-      step(t, s0, s1);
-      step(t + 1, s1, s0);
-    }
-    if (t + 1 < t1) {
-      step(t, s0, s1);
-      finish(t + 1, s1);
+        for (int r = 0; r < 16; r += 4)
+          *reinterpret_cast<f32x4*>(dst + 32 * c + 2 * r) = (f32x4){o[b][c][r], o[b][c][r + 1], o[b][c][r + 2], o[b][c][r + 3]};
     } else {
-      finish(t, s0);
+      const float inv = nothing ? 0.f : 1.f / l[b];
+      uint16_t* dst = a.out + t * a.out_stride + hq * d + half4;
+#pragma unroll
+      for (int c = 0; c < ND; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+          *reinterpret_cast<u32x2*>(dst + 32 * c + 2 * r) = (u32x2){pack2<BF16>(o[b][c][r] * inv, o[b][c][r + 1] * inv),
+                                                                    pack2<BF16>(o[b][c][r + 2] * inv, o[b][c][r + 3] * inv)};
     }
-  }
-
-  l += __shfl_xor(l, 32, kWave);
-  // (once more from the lane: not held in registers through the loop)
-  uint32_t lane2 = lane_id();
-  asm volatile("" : "+v"(lane2));
-  const int orow32 = rt.row0 + 32 * wave + (int)(lane2 % 32), half4 = 4 * (int)(lane2 / 32);
-  const bool mine = orow32 < rt.rows;
-  float odd = l * 0.f;  // NaN if something is not finite
-#pragma unroll
-  for (int c = 0; c < ND; ++c)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) odd = fmaf(o[c][r], 0.f, odd);
-  if (ballot(mine && (odd != odd || (started && l == 0.f)))) {
-    redo_rows<T, BF16>(a, part, rt, h, rt.row0 + 32 * wave, 32, tl, t0, t1, split, BN);
-    return;
-  }
-  if (!mine) return;
-  const int otok = orow32 / a.G, ohq = h * a.G + (orow32 - otok * a.G);
-  const int64_t t = rt.tok0 + otok;
-  const bool nothing = rt.base + otok < 0;
-  if (part.n_splits > 1) {
-    const int64_t orow = (int64_t)split * a.n_q * a.Hq + t * a.Hq + ohq;
-    if (half4 == 0) part.ml[orow] = make_float2(started ? -shift : -INFINITY, nothing ? -1.f : l);
-    float* dst = part.o + orow * d + half4;
-#pragma unroll
-    for (int c = 0; c < ND; ++c)
-#pragma unroll
-      for (int r = 0; r < 16; r += 4)
-        *reinterpret_cast<f32x4*>(dst + 32 * c + 2 * r) = (f32x4){o[c][r], o[c][r + 1], o[c][r + 2], o[c][r + 3]};
-  } else {
-    const float inv = nothing ? 0.f : 1.f / l;
-    uint16_t* dst = a.out + t * a.out_stride + ohq * d + half4;
-#pragma unroll
-    for (int c = 0; c < ND; ++c)
-#pragma unroll
-      for (int r = 0; r < 16; r += 4)
-        *reinterpret_cast<u32x2*>(dst + 32 * c + 2 * r) =
-            (u32x2){pack2<BF16>(o[c][r] * inv, o[c][r + 1] * inv), pack2<BF16>(o[c][r + 2] * inv, o[c][r + 3] * inv)};
   }
 }
 
@@ -580,12 +673,11 @@ __global__ __launch_bounds__(64) void k_paged_merge(PagedAttnArgs a, PartOut par
 
 template <int T, bool BF16>
 static hipError_t attn_launch(const PagedAttnArgs& a, hipStream_t s) {
-  constexpr int BN = chunk_tile<T>();
   const int64_t rows = (int64_t)a.n_q * a.Hq;
   PartOut part = {(float2*)a.ws, nullptr, a.n_splits};
   part.o = (float*)(part.ml + (int64_t)a.n_splits * rows);
   const int64_t groups = paged_tiles(a.p, a.G, a.n_q) * a.p.H * a.n_splits;
-  hipLaunchKernelGGL((k_paged_chunk<T, BF16>), dim3((uint32_t)groups), dim3(256), 4 * BN * 2 * kTile * T, s, a, part);
+  hipLaunchKernelGGL((k_paged_chunk<T, BF16>), dim3((uint32_t)groups), dim3(kWave * chunk_waves(T)), 0, s, a, part);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_splits == 1) return e;
   hipLaunchKernelGGL((k_paged_merge<T, BF16>), dim3((uint32_t)rows), dim3(kWave), 0, s, a, part);
