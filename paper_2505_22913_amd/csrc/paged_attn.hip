@@ -222,15 +222,16 @@ __device__ __forceinline__ void redo_rows(const PagedAttnArgs& a, const PartOut&
 // so the softmax's shift and sum are per lane (two lanes hold a row's tokens), and its 8-token groups,
 // rounded to the type, are the B operand of O^T = V^T P^T as they lie; V^T comes out of LDS transposed.
 //
-// X(t) is the products of tile t + 1's scores with the exponentials of tile t's between them, Y(t) the product with tile t's
-// values with the maximum of tile t + 1's scores between. X is bound by the vector units, Y by the matrix cores, and
-// waves w and w + 4 share a SIMD: the second four run half a tile late. A barrier a tile opens slot t, in which the first four do
-// X(t), Y(t) and the second Y(t - 1), X(t); both read the keys of tile t + 1, the first the values of tile t, the second those
-// of tile t - 1 (and the first of tile t's, ahead). Tiles are staged kDepth slots ahead, into buffers last read a slot before.
+// Step t is X, the products of tile t + 1's scores, then Y, those with tile t's values. Between the products, fenced one by one, lies
+// what the vector units do: the exponentials of tile t in X and the first half of Y, which needs but the first half of the
+// tile, and the maximum of tile t + 1's scores in the second half. (All exponentials in X: its 16 products took 1.8 times as long
+// as Y's.) One barrier a step. Tiles are staged kDepth steps ahead (pair t: the keys of tile t + 1 and the values of
+// tile t) and arrive one step before they are needed, so that the first operands of a step are read before its barrier; they
+// go where the step before has read.
 // ------------------------------------------------------------------------------------------
 template <int T>
 constexpr int chunk_tile() { return T == 4 ? 32 : 64; }
-constexpr int kDepth = 2, kRingK = kDepth + 1, kRingV = kDepth + 2;
+constexpr int kDepth = 3, kRing = kDepth + 1;
 
 // A probability is 2^kBias at the reference, which follows the largest score once that is more than 2^kSlack above it:
 // at most 2^15 (inside fp16), and fp16 keeps those down to 2^-31 of the reference. It is exp2(score * scale +
@@ -254,7 +255,7 @@ __device__ __forceinline__ uint32_t swizzle_v(uint32_t row) {
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t dst) {
   uint32_t m0;
   asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
-               : "=&s"(m0) : "s"(dst), "v"(offset), "s"(base) : "memory");
+               : "=&s"(m0) : "s"(__builtin_amdgcn_readfirstlane((int)dst)), "v"(offset), "s"(base) : "memory");
 }
 template <int LEFT>
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(LEFT) : "memory"); }
@@ -288,12 +289,12 @@ __device__ __forceinline__ float max_of(const f32x16 (&s)[NK]) {
 
 template <int T, bool BF16>
 __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_paged_chunk(PagedAttnArgs a, PartOut part) {
-  constexpr int NW = chunk_waves(T), NQ = 1, BW = 32 * NQ, BM = NW * BW;
+  constexpr int NW = chunk_waves(T), BM = 32 * NW;
   constexpr int d = kTile * T, BN = chunk_tile<T>(), NK = BN / 32, NC = d / 16, ND = d / 32;
   constexpr uint32_t kRow = 2 * d, kBuf = BN * kRow;  // bytes
   constexpr int kWaveRows = BN / NW, kRowsPerLoad = 1024 / (2 * d), kLoads = kWaveRows / kRowsPerLoad;
   static_assert(kLoads * kRowsPerLoad == kWaveRows && 16 % kWaveRows == 0, "a wave's rows");
-  __shared__ __align__(1024) unsigned char smem[(kRingK + kRingV) * kBuf];  // buffers of keys, of values
+  __shared__ __align__(1024) unsigned char smem[(2 * kRing) * kBuf];  // buffers of keys, of values
   const PagedView& p = a.p;
   const int h = blockIdx.x % p.H, split = (blockIdx.x / p.H) % part.n_splits;
   const int tile = (int)(gridDim.x / (p.H * part.n_splits)) - 1 - (int)(blockIdx.x / (p.H * part.n_splits));
@@ -301,34 +302,26 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
   if (rt.row0 >= rt.rows) return;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
   const uint32_t lane = lane_id(), r32 = lane % 32, half = lane / 32;
-  const int wrow = rt.row0 + BW * wave;  // the wave's first row
+  const int wrow = rt.row0 + 32 * wave;  // the wave's first row
   const TileList tl(rt.base + rt.row0 / a.G, rt.base + (min(rt.row0 + BM, rt.rows) - 1) / a.G, a.window, a.sinks, BN);
   const int t0 = (int)((int64_t)tl.n * split / part.n_splits);
   const int n = (int)((int64_t)tl.n * (split + 1) / part.n_splits) - t0;  // tiles of the workgroup
   // The wave's rows' positions, and its tiles: those behind its last position are the others'.
-  const int pos0 = rt.base + min(wrow, rt.rows - 1) / a.G, pos1 = rt.base + min(wrow + BW - 1, rt.rows - 1) / a.G;
+  const int pos0 = rt.base + min(wrow, rt.rows - 1) / a.G, pos1 = rt.base + min(wrow + 31, rt.rows - 1) / a.G;
   const int mine = wrow >= rt.rows || pos1 < 0 ? 0 : min(n, max(tl.count_to(pos1, BN) - t0, 0));
 
   // Tiles [clean0, clean1) of the list are seen whole by every row of the wave, [whole0, whole1) by some row of the workgroup.
   const int clean0 = a.window > 0 ? tl.count_to(pos1 - a.window, BN) - t0 : 0, clean1 = tl.count_to(pos0 - BN + 1, BN) - t0;
   const int whole0 = tl.count_to(tl.lo - 1, BN) - t0, whole1 = tl.count_to(tl.hi - BN + 1, BN) - t0;
 
-  // Q as the B operand: column = row of the block, k = 16 c + 8 half + i.
-  u32x4 qb[NQ][NC];
-  int pos[NQ];
+  // Q as the B operand: column = row of the wave, k = 16 c + 8 half + i.
+  const int my_row = min(wrow + (int)r32, rt.rows - 1), my_tok = my_row / a.G, pos = rt.base + my_tok;
+  u32x4 qb[NC];
+  {
+    const uint16_t* q = a.q + (int64_t)(rt.tok0 + my_tok) * a.q_stride + (h * a.G + my_row - my_tok * a.G) * d + 8 * half;
 #pragma unroll
-  for (int b = 0; b < NQ; ++b) {
-    const int row = min(wrow + 32 * b + (int)r32, rt.rows - 1), tok = row / a.G;
-    pos[b] = rt.base + tok;
-    const uint16_t* q = a.q + (int64_t)(rt.tok0 + tok) * a.q_stride + (h * a.G + row - tok * a.G) * d + 8 * half;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) qb[b][c] = *reinterpret_cast<const u32x4*>(q + 16 * c);
+    for (int c = 0; c < NC; ++c) qb[c] = *reinterpret_cast<const u32x4*>(q + 16 * c);
   }
-  // (here: a wait for them inside the loop would be one for the tiles' loads too)
-#pragma unroll
-  for (int b = 0; b < NQ; ++b)
-#pragma unroll
-    for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(qb[b][c]));
 
   // Staging. Wave w loads rows kWaveRows w .. of a tile. Pages hold 16 tokens or more, so they share one; a group of 16 of which
   // no row of q sees any is replaced by the nearest with one that some does. Lane i holds the offset in k and v of the rows of
@@ -353,7 +346,7 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
     // (the places' XORs are linear in the row's bits: this load's share of them)
     const uint32_t r = kWaveRows * wave + kRowsPerLoad * i, x = 16u * (values ? swizzle_v<T>(r) : swizzle_k<T>(r));
     load_to_lds(base, lane_off + kRowsPerLoad * i * row_bytes + (piece ^ x),
-                lds0 + (uint32_t)(buf + (values ? kRingK : 0)) * kBuf + (kWaveRows * wave + kRowsPerLoad * i) * kRow);
+                lds0 + (uint32_t)(buf + (values ? kRing : 0)) * kBuf + (kWaveRows * wave + kRowsPerLoad * i) * kRow);
   };
   // Where the keys of tile t (behind the last: the last, for nothing) lie; the values of the tile before lay where its keys did.
   uint64_t k_at = 0, v_at = 0;
@@ -365,54 +358,54 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
            (uint32_t)__builtin_amdgcn_readlane((int)at_lo, t % kWave);
   };
   int k_buf = 0, v_buf = 0;  // where the next keys and values go
-  auto stage_k = [&]() __attribute__((always_inline)) {
-    uint32_t piece = piece_k;
+  // Load i of the 2 kLoads of a pair.
+  auto stage = [&](int i) __attribute__((always_inline)) {
+    uint32_t piece = i < kLoads ? piece_k : piece_v;
     asm volatile("" : "+v"(piece));  // (kept in registers for every load, the addresses would fill them)
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) stage_load(reinterpret_cast<const unsigned char*>(p.k) + k_at, piece, false, k_buf, i);
-    k_buf = k_buf + 1 == kRingK ? 0 : k_buf + 1;
+    if (i < kLoads) stage_load(reinterpret_cast<const unsigned char*>(p.k) + k_at, piece, false, k_buf, i);
+    else stage_load(reinterpret_cast<const unsigned char*>(p.v) + v_at, piece, true, v_buf, i - kLoads);
   };
-  auto stage_v = [&]() __attribute__((always_inline)) {
-    uint32_t piece = piece_v;
-    asm volatile("" : "+v"(piece));
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) stage_load(reinterpret_cast<const unsigned char*>(p.v) + v_at, piece, true, v_buf, i);
-    v_buf = v_buf + 1 == kRingV ? 0 : v_buf + 1;
+  int placed = 0;  // the pair whose loads are next
+  auto next_pair = [&]() __attribute__((always_inline)) {
+    ++placed;
+    place(placed + 1);
+    k_buf = k_buf + 1 == kRing ? 0 : k_buf + 1;
+    v_buf = v_buf + 1 == kRing ? 0 : v_buf + 1;
   };
-  // Slot i: the keys of tile i + 1 and the values of tile i have arrived for every wave, and nobody reads any more what slot i - 1
-  // read of them; those of slot i + kDepth are started. Values that no row of q sees are cleared (they may be what memory
-  // held: 0 times that is not 0).
+  auto stage_pair = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 2 * kLoads; ++i) stage(i);
+    next_pair();
+  };
+  // This wave's rows of the values of tile t, which have arrived: what no row of q sees is cleared (it may be what memory held: 0
+  // times that is not 0).
+  auto clear_values = [&](int t) __attribute__((always_inline)) {
+    if (t >= n || (t >= whole0 && t < whole1)) return;
+    const int j0 = tl.start(t0 + t, BN);
+    uint32_t zero_at = lds0 + (uint32_t)(kRing + t % kRing) * kBuf + kWaveRows * wave * kRow + 16 * lane;
+#pragma unroll 1
+    for (int i = 0; i < kLoads; ++i, zero_at += kRowsPerLoad * kRow) {
+      const int x = j0 + kWaveRows * wave + kRowsPerLoad * i + (int)lane_row;
+      if (x > tl.hi || (x < tl.lo && x >= tl.sinks))
+        *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(zero_at) = (u32x4){0u, 0u, 0u, 0u};
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  };
+  // Opens a step: the pair of the one behind it has arrived for every wave.
   int slot = 0;
   auto arrive = [&]() __attribute__((always_inline)) {
-    wait_loads<2 * kLoads * (kDepth - 1)>();
-    if (slot < n && (slot < whole0 || slot >= whole1)) {
-      const int j0 = tl.start(t0 + slot, BN);
-      uint32_t zero_at = lds0 + (uint32_t)(kRingK + slot % kRingV) * kBuf + kWaveRows * wave * kRow + 16 * lane;
-#pragma unroll 1
-      for (int i = 0; i < kLoads; ++i, zero_at += kRowsPerLoad * kRow) {
-        const int x = j0 + kWaveRows * wave + kRowsPerLoad * i + (int)lane_row;
-        if (x > tl.hi || (x < tl.lo && x >= tl.sinks))
-          *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(zero_at) = (u32x4){0u, 0u, 0u, 0u};
-      }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    }
+    wait_loads<2 * kLoads * (kDepth - 2)>();
+    ++slot;
+    clear_values(slot);
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    ++slot;
-    place(slot + kDepth);
-    stage_k();
-    stage_v();
   };
 
   const float inv_scale = 1.f / a.scale_log2;
-  float l[NQ] = {}, shift[NQ] = {}, top[NQ], limit[NQ];
+  float l = 0.f, shift = 0.f, top, limit = -INFINITY;
+  f32x16 o[ND];
 #pragma unroll
-  for (int b = 0; b < NQ; ++b) limit[b] = -INFINITY;
-  f32x16 o[NQ][ND];
-#pragma unroll
-  for (int b = 0; b < NQ; ++b)
-#pragma unroll
-    for (int c = 0; c < ND; ++c) o[b][c] = (f32x16){};
+  for (int c = 0; c < ND; ++c) o[c] = (f32x16){};
 
   // Operand i of the scores (tokens 32 (i % NK) .., channels 16 (i / NK) ..) and of the outputs (channels 32 (i % ND) .., tokens
   // 16 (i / ND) .., k slot 8 half + i being token 8 (i / 4) + 4 half + i % 4, as the scores lie). A row of LDS is a
@@ -420,7 +413,7 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
   constexpr int kS = NK * NC, kO = 2 * NK * ND, kAhead = 4;
   const uint32_t kaddr = lds0 + r32 * kRow + 16u * (half ^ swizzle_k<T>(r32));
   const uint32_t vrow = 4 * half + (lane % 16) / 4;
-  const uint32_t vaddr = lds0 + kRingK * kBuf + vrow * kRow + 16u * ((((lane / 16) & 1) * 2 + (lane % 4) / 2) ^ swizzle_v<T>(vrow)) + 8 * (lane & 1);
+  const uint32_t vaddr = lds0 + kRing * kBuf + vrow * kRow + 16u * ((((lane / 16) & 1) * 2 + (lane % 4) / 2) ^ swizzle_v<T>(vrow)) + 8 * (lane & 1);
   auto load_k = [&](uint32_t at, int i) __attribute__((always_inline)) { return lds_load<u32x4>((at ^ (32u * (i / NK))) + 32 * (i % NK) * kRow); };
   auto load_v = [&](uint32_t at, int i) __attribute__((always_inline)) {
     const uint32_t x = (at ^ (64u * (i % ND))) + 16 * (i / ND) * kRow;
@@ -430,150 +423,141 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
 
   // The scores of a tile, this lane's largest in top, are masked and the shift follows them: limit is the largest score that
   // it leaves alone (-inf before the first), a row's other lane has the same.
-  auto settle = [&](int t, f32x16 (&s)[NQ][NK]) __attribute__((always_inline)) {
+  auto settle = [&](int t, f32x16 (&s)[NK]) __attribute__((always_inline)) {
     if (t < clean0 || t >= clean1) {
-      const int j0 = tl.start(t0 + t, BN);
+      const int j0 = tl.start(t0 + t, BN), back = pos - j0 - 4 * (int)half;  // of this lane's first token of the tile
+      if (a.window == 0) {
 #pragma unroll
-      for (int b = 0; b < NQ; ++b) {
+        for (int n = 0; n < NK; ++n)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[n][r] = back < 32 * n + 8 * (r / 4) + r % 4 ? -INFINITY : s[n][r];
+      } else {
 #pragma unroll
         for (int n = 0; n < NK; ++n)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int j = j0 + 32 * n + 8 * (r / 4) + 4 * (int)half + r % 4;
-            if (!sees(pos[b], j, a.window, a.sinks)) s[b][n][r] = -INFINITY;
+            if (!sees(pos, j, a.window, a.sinks)) s[n][r] = -INFINITY;
           }
-        top[b] = max_of<NK>(s[b]);
       }
+      top = max_of<NK>(s);
     }
-    bool any = false;
+    if (ballot(top > limit)) {
+      top = max_halves(top);
+      const bool move = top > limit;
+      const float to = move ? fmaf(-top, a.scale_log2, kBias) : shift;
+      const float alpha = limit > -INFINITY ? __builtin_amdgcn_exp2f(to - shift) : 1.f;  // (nothing is there before the start)
+      if (move) limit = fmaf(kSlack, inv_scale, top);
+      shift = to;
+      l *= alpha;
 #pragma unroll
-    for (int b = 0; b < NQ; ++b) any |= top[b] > limit[b];
-    if (ballot(any)) {
+      for (int c = 0; c < ND; ++c)
 #pragma unroll
-      for (int b = 0; b < NQ; ++b) {
-        top[b] = max_halves(top[b]);
-        const bool move = top[b] > limit[b], started = limit[b] > -INFINITY;
-        const float to = move ? fmaf(-top[b], a.scale_log2, kBias) : shift[b];
-        const float alpha = started ? __builtin_amdgcn_exp2f(to - shift[b]) : 1.f;  // (nothing is there before the start)
-        if (move) limit[b] = fmaf(kSlack, inv_scale, top[b]);
-        shift[b] = to;
-        l[b] *= alpha;
-#pragma unroll
-        for (int c = 0; c < ND; ++c)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[b][c][r] *= alpha;
-      }
+        for (int r = 0; r < 16; ++r) o[c][r] *= alpha;
     }
   };
-  // Probabilities 2 i and 2 i + 1 of a lane's row of block b, rounded; the sum is that of the rounded ones.
-  u32x4 pb[NQ][2 * NK];
-  auto exponentials = [&](f32x16 (&s)[NQ][NK], int b, int i) __attribute__((always_inline)) {
+  // Probabilities 2 i and 2 i + 1 of a lane, and, when they are there, rounded: the sum is that of the rounded ones.
+  constexpr int kPairs = 8 * NK, kPairsX = kPairs * 11 / 16;
+  u32x4 pb[2 * NK];
+  auto round_pair = [&](const f32x16 (&s)[NK], int i) __attribute__((always_inline)) {
+    const uint32_t xy = pack2<BF16>(s[i / 8][2 * (i % 8)], s[i / 8][2 * (i % 8) + 1]);
+    l = add_pair<BF16>(xy, l);
+    pb[i / 4][i % 4] = xy;
+  };
+  auto pair = [&](f32x16 (&s)[NK], int i) __attribute__((always_inline)) {
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      s[b][i / 8][2 * (i % 8) + e] = __builtin_amdgcn_exp2f(fmaf(s[b][i / 8][2 * (i % 8) + e], a.scale_log2, shift[b]));
+      float x = fmaf(s[i / 8][2 * (i % 8) + e], a.scale_log2, shift);
+      s[i / 8][2 * (i % 8) + e] = __builtin_amdgcn_exp2f(x);
     }
+    if (i > 0) round_pair(s, i - 1);
   };
-  auto round_pair = [&](const f32x16 (&s)[NQ][NK], int b, int i) __attribute__((always_inline)) {
-    const uint32_t xy = pack2<BF16>(s[b][i / 8][2 * (i % 8)], s[b][i / 8][2 * (i % 8) + 1]);
-    l[b] = add_pair<BF16>(xy, l[b]);
-    pb[b][i / 4][i % 4] = xy;
-  };
-  const bool late = NW == 8 && wave >= 4;  // (see above)
   u32x4 kf[kAhead], vf[kAhead];
   int kr = 1, vr = 0;  // the buffers of tile t + 1's keys and tile t's values
-  // Step t with a tile behind it. Operands are read kAhead before they are used.
-  auto step = [&](int t, f32x16 (&s)[NQ][NK], f32x16 (&sn)[NQ][NK]) __attribute__((always_inline)) {
-    if (!late) arrive();
+  // Step t with a tile behind it. Operands are read kAhead products before they are used (the first of X in the Y before).
+  auto step = [&](int t, f32x16 (&s)[NK], f32x16 (&sn)[NK]) __attribute__((always_inline)) {
+    arrive();
     uint32_t kat = kaddr + (uint32_t)kr * kBuf, vat = vaddr + (uint32_t)vr * kBuf;
-    asm volatile("" : "+v"(kat), "+v"(vat));  // (as in stage_k)
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) kf[i] = load_k(kat, i);
+    asm volatile("" : "+v"(kat), "+v"(vat));  // (as in stage)
 #pragma unroll
     for (int i = 0; i < kS; ++i) {
+      sn[i % NK] = mfma32<BF16>(kf[i % kAhead], qb[i / NK], i < NK ? (f32x16){} : sn[i % NK]);
+      if (i < 2 * kLoads) stage(i);
+      if (i + kAhead < kS) kf[i % kAhead] = load_k(kat, i + kAhead);
+      else vf[i + kAhead - kS] = load_v(vat, i + kAhead - kS);
 #pragma unroll
-      for (int b = 0; b < NQ; ++b) {
-        sn[b][i % NK] = mfma32<BF16>(kf[i % kAhead], qb[b][i / NK], i < NK ? (f32x16){} : sn[b][i % NK]);
-        if (b == NQ - 1) {
-          if (i + kAhead < kS) kf[i % kAhead] = load_k(kat, i + kAhead);
-          else vf[i + kAhead - kS] = load_v(vat, i + kAhead - kS);
-        }
-#pragma unroll
-        for (int e = i * 8 * NK / kS; e < (i + 1) * 8 * NK / kS; ++e) exponentials(s, b, e);
-        // (rounded a product later, when they are there)
-#pragma unroll
-        for (int e = (i - 1) * 8 * NK / kS; i > 0 && e < i * 8 * NK / kS; ++e) round_pair(s, b, e);
-        __builtin_amdgcn_sched_barrier(0);
-      }
+      for (int e = i * kPairsX / kS; e < (i + 1) * kPairsX / kS; ++e) pair(s, e);
+      __builtin_amdgcn_sched_barrier(0);
     }
-#pragma unroll
-    for (int b = 0; b < NQ; ++b) {
-#pragma unroll
-      for (int e = (kS - 1) * 8 * NK / kS; e < 8 * NK; ++e) round_pair(s, b, e);
-      top[b] = -INFINITY;
-    }
-    if (late) arrive();
-    asm volatile("" : "+v"(vat));
-#pragma unroll
-    for (int i = 0; i < kO; ++i)
-#pragma unroll
-      for (int b = 0; b < NQ; ++b) {
-        o[b][i % ND] = mfma32<BF16>(vf[i % kAhead], pb[b][i / ND], o[b][i % ND]);
-        if (b == NQ - 1 && i + kAhead < kO) vf[i % kAhead] = load_v(vat, i + kAhead);
-#pragma unroll
-        for (int e = i * 16 * NK / kO; e < (i + 1) * 16 * NK / kO; ++e) top[b] = fmaxf(top[b], sn[b][e / 16][e % 16]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    settle(t + 1, sn);
-    kr = kr + 1 == kRingK ? 0 : kr + 1;
-    vr = vr + 1 == kRingV ? 0 : vr + 1;
-  };
-  // The wave's last step.
-  auto finish = [&](f32x16 (&s)[NQ][NK]) __attribute__((always_inline)) {
-    if (!late) arrive();
-#pragma unroll
-    for (int b = 0; b < NQ; ++b)
-#pragma unroll
-      for (int e = 0; e < 8 * NK; ++e) {
-        exponentials(s, b, e);
-        round_pair(s, b, e);
-      }
-    if (late) arrive();
-    const uint32_t vat = vaddr + (uint32_t)vr * kBuf;
+    next_pair();
+    kr = kr + 1 == kRing ? 0 : kr + 1;
+    vr = vr + 1 == kRing ? 0 : vr + 1;
+    uint32_t knext = kaddr + (uint32_t)kr * kBuf;
+    asm volatile("" : "+v"(vat), "+v"(knext));
+    top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kO; ++i) {
-      vf[0] = load_v(vat, i);
+      if (i == kO / 2) round_pair(s, kPairs - 1);
+      o[i % ND] = mfma32<BF16>(vf[i % kAhead], pb[i / ND], o[i % ND]);
+      if (i + kAhead < kO) vf[i % kAhead] = load_v(vat, i + kAhead);
+      else kf[i + kAhead - kO] = load_k(knext, i + kAhead - kO);
+      if (i < kO / 2) {
 #pragma unroll
-      for (int b = 0; b < NQ; ++b) o[b][i % ND] = mfma32<BF16>(vf[0], pb[b][i / ND], o[b][i % ND]);
-      if (i % kAhead == kAhead - 1) __builtin_amdgcn_sched_barrier(0);
+        for (int e = kPairsX + i * (kPairs - kPairsX) / (kO / 2); e < kPairsX + (i + 1) * (kPairs - kPairsX) / (kO / 2); ++e) pair(s, e);
+      } else {
+#pragma unroll
+        for (int e = (i - kO / 2) * 4 * kPairs / kO; e < (i - kO / 2 + 1) * 4 * kPairs / kO; ++e) top = fmaxf(top, sn[e / 16][e % 16]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    settle(t + 1, sn);
+  };
+  // The wave's last step.
+  auto finish = [&](f32x16 (&s)[NK]) __attribute__((always_inline)) {
+    arrive();
+    const uint32_t vat = vaddr + (uint32_t)vr * kBuf;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) vf[i] = load_v(vat, i);
+    stage_pair();
+#pragma unroll
+    for (int e = 0; e < kPairs; ++e) pair(s, e);
+    round_pair(s, kPairs - 1);
+#pragma unroll
+    for (int i = 0; i < kO; ++i) {
+      o[i % ND] = mfma32<BF16>(vf[i % kAhead], pb[i / ND], o[i % ND]);
+      if (i + kAhead < kO) vf[i % kAhead] = load_v(vat, i + kAhead);
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
 
   if (n > 0) {
-    f32x16 s0[NQ][NK], s1[NQ][NK];
-    // The first tile's keys, then what the first kDepth slots need.
+    f32x16 s0[NK], s1[NK];
+    // The first tile's keys, then pairs 0 .. kDepth - 1.
     place(0);
-    stage_k();
+    // (here: a wait for q inside the loop would be one for the tiles' loads too)
+#pragma unroll
+    for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(qb[c]));
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) stage(i);
+    k_buf = 1;
+    place(1);
 #pragma unroll 1
-    for (int i = 0; i < kDepth; ++i) {
-      place(i + 1);
-      stage_k();
-      stage_v();
-    }
-    wait_loads<2 * kLoads * kDepth>();
+    for (int i = 0; i < kDepth; ++i) stage_pair();
+    wait_loads<2 * kLoads * (kDepth - 1)>();
+    clear_values(0);
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     if (mine > 0) {
 #pragma unroll
+      for (int i = 0; i < kAhead; ++i) kf[i] = load_k(kaddr, i);
+#pragma unroll
       for (int i = 0; i < kS; ++i) {
-        kf[0] = load_k(kaddr, i);
-#pragma unroll
-        for (int b = 0; b < NQ; ++b) s0[b][i % NK] = mfma32<BF16>(kf[0], qb[b][i / NK], i < NK ? (f32x16){} : s0[b][i % NK]);
-        if (i % kAhead == kAhead - 1) __builtin_amdgcn_sched_barrier(0);
+        s0[i % NK] = mfma32<BF16>(kf[i % kAhead], qb[i / NK], i < NK ? (f32x16){} : s0[i % NK]);
+        kf[i % kAhead] = i + kAhead < kS ? load_k(kaddr, i + kAhead) : load_k(kaddr + kBuf, i + kAhead - kS);
+        __builtin_amdgcn_sched_barrier(0);
       }
-#pragma unroll
-      for (int b = 0; b < NQ; ++b) top[b] = max_of<NK>(s0[b]);
+      top = max_of<NK>(s0);
       settle(0, s0);
-      if (late) arrive();
       int t = 0;
       for (; t + 2 < mine; t += 2) {
         step(t, s0, s1);
@@ -586,8 +570,11 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
         finish(s0);
       }
     }
-    // Slots of the other waves; none may end while its loads are under way.
-    while (slot <= n) arrive();
+    // Steps of the other waves; none may end while its loads are under way.
+    while (slot < n) {
+      arrive();
+      stage_pair();
+    }
     wait_loads<0>();
   }
 
@@ -595,46 +582,38 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
   uint32_t lane2 = lane_id();
   asm volatile("" : "+v"(lane2));
   const int row = wrow + (int)(lane2 % 32), half4 = 4 * (int)(lane2 / 32);
-  bool odd = false;  // something is not finite
+  l += __shfl_xor(l, 32, kWave);
+  float z = l * 0.f;  // NaN if something is not finite
 #pragma unroll
-  for (int b = 0; b < NQ; ++b) {
-    l[b] += __shfl_xor(l[b], 32, kWave);
-    float z = l[b] * 0.f;
+  for (int c = 0; c < ND; ++c)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) z = fmaf(o[c][r], 0.f, z);
+  if (ballot(row < rt.rows && (z != z || (limit > -INFINITY && l == 0.f)))) {
+    redo_rows<T, BF16>(a, part, rt, h, wrow, 32, tl, t0, t0 + n, split, BN);
+    return;
+  }
+  if (row >= rt.rows) return;
+  const int tok = row / a.G, hq = h * a.G + (row - tok * a.G);
+  const int64_t t = rt.tok0 + tok;
+  const bool nothing = rt.base + tok < 0;
+  if (part.n_splits > 1) {
+    const int64_t orow = (int64_t)split * a.n_q * a.Hq + t * a.Hq + hq;
+    if (half4 == 0) part.ml[orow] = make_float2(limit > -INFINITY ? -shift : -INFINITY, nothing ? -1.f : l);
+    float* dst = part.o + orow * d + half4;
 #pragma unroll
     for (int c = 0; c < ND; ++c)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) z = fmaf(o[b][c][r], 0.f, z);
-    odd |= row + 32 * b < rt.rows && (z != z || (limit[b] > -INFINITY && l[b] == 0.f));
-  }
-  if (ballot(odd)) {
-    redo_rows<T, BF16>(a, part, rt, h, wrow, BW, tl, t0, t0 + n, split, BN);
-    return;
-  }
+      for (int r = 0; r < 16; r += 4)
+        *reinterpret_cast<f32x4*>(dst + 32 * c + 2 * r) = (f32x4){o[c][r], o[c][r + 1], o[c][r + 2], o[c][r + 3]};
+  } else {
+    const float inv = nothing ? 0.f : 1.f / l;
+    uint16_t* dst = a.out + t * a.out_stride + hq * d + half4;
 #pragma unroll
-  for (int b = 0; b < NQ; ++b) {
-    if (row + 32 * b >= rt.rows) continue;
-    const int tok = (row + 32 * b) / a.G, hq = h * a.G + (row + 32 * b - tok * a.G);
-    const int64_t t = rt.tok0 + tok;
-    const bool nothing = rt.base + tok < 0;
-    if (part.n_splits > 1) {
-      const int64_t orow = (int64_t)split * a.n_q * a.Hq + t * a.Hq + hq;
-      if (half4 == 0) part.ml[orow] = make_float2(limit[b] > -INFINITY ? -shift[b] : -INFINITY, nothing ? -1.f : l[b]);
-      float* dst = part.o + orow * d + half4;
+    for (int c = 0; c < ND; ++c)
 #pragma unroll
-      for (int c = 0; c < ND; ++c)
-#pragma unroll
-        for (int r = 0; r < 16; r += 4)
-          *reinterpret_cast<f32x4*>(dst + 32 * c + 2 * r) = (f32x4){o[b][c][r], o[b][c][r + 1], o[b][c][r + 2], o[b][c][r + 3]};
-    } else {
-      const float inv = nothing ? 0.f : 1.f / l[b];
-      uint16_t* dst = a.out + t * a.out_stride + hq * d + half4;
-#pragma unroll
-      for (int c = 0; c < ND; ++c)
-#pragma unroll
-        for (int r = 0; r < 16; r += 4)
-          *reinterpret_cast<u32x2*>(dst + 32 * c + 2 * r) = (u32x2){pack2<BF16>(o[b][c][r] * inv, o[b][c][r + 1] * inv),
-                                                                    pack2<BF16>(o[b][c][r + 2] * inv, o[b][c][r + 3] * inv)};
-    }
+      for (int r = 0; r < 16; r += 4)
+        *reinterpret_cast<u32x2*>(dst + 32 * c + 2 * r) =
+            (u32x2){pack2<BF16>(o[c][r] * inv, o[c][r + 1] * inv), pack2<BF16>(o[c][r + 2] * inv, o[c][r + 3] * inv)};
   }
 }
 
