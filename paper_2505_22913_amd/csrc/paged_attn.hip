@@ -253,9 +253,12 @@ __device__ __forceinline__ uint32_t swizzle_v(uint32_t row) {
 // compiler waits for every such load before the next transposing LDS read of any address. The load has no register
 // output; m0, its LDS address, is put back.)
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t dst) {
+  const uint64_t at = (uint64_t)base;  // (uniform; said so, whatever the compiler makes of how it came about)
+  const uint64_t sbase = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32)) << 32 |
+                         (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at);
   uint32_t m0;
   asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
-               : "=&s"(m0) : "s"(__builtin_amdgcn_readfirstlane((int)dst)), "v"(offset), "s"(base) : "memory");
+               : "=&s"(m0) : "s"(__builtin_amdgcn_readfirstlane((int)dst)), "v"(offset), "s"(sbase) : "memory");
 }
 template <int LEFT>
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(LEFT) : "memory"); }
@@ -314,14 +317,7 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
   const int clean0 = a.window > 0 ? tl.count_to(pos1 - a.window, BN) - t0 : 0, clean1 = tl.count_to(pos0 - BN + 1, BN) - t0;
   const int whole0 = tl.count_to(tl.lo - 1, BN) - t0, whole1 = tl.count_to(tl.hi - BN + 1, BN) - t0;
 
-  // Q as the B operand: column = row of the wave, k = 16 c + 8 half + i.
   const int my_row = min(wrow + (int)r32, rt.rows - 1), my_tok = my_row / a.G, pos = rt.base + my_tok;
-  u32x4 qb[NC];
-  {
-    const uint16_t* q = a.q + (int64_t)(rt.tok0 + my_tok) * a.q_stride + (h * a.G + my_row - my_tok * a.G) * d + 8 * half;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) qb[c] = *reinterpret_cast<const u32x4*>(q + 16 * c);
-  }
 
   // Staging. Wave w loads rows kWaveRows w .. of a tile. Pages hold 16 tokens or more, so they share one; a group of 16 of which
   // no row of q sees any is replaced by the nearest with one that some does. Lane i holds the offset in k and v of the rows of
@@ -472,6 +468,7 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
     }
     if (i > 0) round_pair(s, i - 1);
   };
+  u32x4 qb[NC];  // Q as the B operand: column = row of the wave, k = 16 c + 8 half + i
   u32x4 kf[kAhead], vf[kAhead];
   int kr = 1, vr = 0;  // the buffers of tile t + 1's keys and tile t's values
   // Step t with a tile behind it. Operands are read kAhead products before they are used (the first of X in the Y before).
@@ -532,18 +529,25 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
 
   if (n > 0) {
     f32x16 s0[NK], s1[NK];
-    // The first tile's keys, then pairs 0 .. kDepth - 1.
+    // Where the tiles lie; q; the first tile's keys, then pairs 0 .. kDepth - 1: all under way at once.
     place(0);
-    // (here: a wait for q inside the loop would be one for the tiles' loads too)
+    __builtin_amdgcn_sched_barrier(0);
+    {
+      const uint16_t* q = a.q + (int64_t)(rt.tok0 + my_tok) * a.q_stride + (h * a.G + my_row - my_tok * a.G) * d + 8 * half;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(qb[c]));
+      for (int c = 0; c < NC; ++c) qb[c] = *reinterpret_cast<const u32x4*>(q + 16 * c);
+    }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) stage(i);
     k_buf = 1;
     place(1);
 #pragma unroll 1
     for (int i = 0; i < kDepth; ++i) stage_pair();
-    wait_loads<2 * kLoads * (kDepth - 1)>();
+    // (q's wait is here: inside the loop it would be one for the tiles' loads too)
+    wait_loads<0>();
+#pragma unroll
+    for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(qb[c]));
     clear_values(0);
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
@@ -592,11 +596,11 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
     redo_rows<T, BF16>(a, part, rt, h, wrow, 32, tl, t0, t0 + n, split, BN);
     return;
   }
-  if (row >= rt.rows) return;
   const int tok = row / a.G, hq = h * a.G + (row - tok * a.G);
   const int64_t t = rt.tok0 + tok;
   const bool nothing = rt.base + tok < 0;
   if (part.n_splits > 1) {
+    if (row >= rt.rows) return;
     const int64_t orow = (int64_t)split * a.n_q * a.Hq + t * a.Hq + hq;
     if (half4 == 0) part.ml[orow] = make_float2(limit > -INFINITY ? -shift : -INFINITY, nothing ? -1.f : l);
     float* dst = part.o + orow * d + half4;
@@ -606,14 +610,21 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
       for (int r = 0; r < 16; r += 4)
         *reinterpret_cast<f32x4*>(dst + 32 * c + 2 * r) = (f32x4){o[c][r], o[c][r + 1], o[c][r + 2], o[c][r + 3]};
   } else {
+    // Eight channels a lane: its own four and the row's other lane's, of each 16.
     const float inv = nothing ? 0.f : 1.f / l;
-    uint16_t* dst = a.out + t * a.out_stride + hq * d + half4;
+    uint16_t* dst = a.out + t * a.out_stride + hq * d + 2 * half4;
 #pragma unroll
     for (int c = 0; c < ND; ++c)
 #pragma unroll
-      for (int r = 0; r < 16; r += 4)
-        *reinterpret_cast<u32x2*>(dst + 32 * c + 2 * r) =
-            (u32x2){pack2<BF16>(o[c][r] * inv, o[c][r + 1] * inv), pack2<BF16>(o[c][r + 2] * inv, o[c][r + 3] * inv)};
+      for (int r = 0; r < 16; r += 8) {
+        uint32_t x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = pack2<BF16>(o[c][r + 2 * e] * inv, o[c][r + 2 * e + 1] * inv);
+        const auto lo = __builtin_amdgcn_permlane32_swap(x[0], x[2], false, false);
+        const auto hi = __builtin_amdgcn_permlane32_swap(x[1], x[3], false, false);
+        if (row < rt.rows)
+          *reinterpret_cast<u32x4*>(dst + 32 * c + 2 * r) = (u32x4){(uint32_t)lo[0], (uint32_t)hi[0], (uint32_t)lo[1], (uint32_t)hi[1]};
+      }
   }
 }
 
