@@ -35,25 +35,46 @@ struct PagedAttnArgs {
   int n_q, Hq, G;
   int window, sinks;
   float scale_log2;  // score scale times log2(e)
-  int n_splits;      // ranges of a request's visible tokens
-  void* ws;          // their results when there are several
+  // Ranges of a request's visible tokens in k_paged_rows and in k_paged_chunk, 0 where that kernel is not run; mixed: the first
+  // has the requests of at most kFewRows rows, the second the others, else the one that runs has all.
+  int few, many, mixed;
+  void* ws;  // the ranges' results where there are several
 };
 
-// Waves of a workgroup, of 32 rows (new tokens times query heads of a kv-head) each; d = 64 T.
+// Rows are a request's new tokens times the query heads of a kv-head. k_paged_rows takes 16 at a time, k_paged_chunk 32 a wave and
+// 8 waves a workgroup (4 at d = 256; d = 64 T).
+constexpr int kFewRows = 16;
 constexpr int chunk_waves(int T) { return T == 4 ? 4 : 8; }
-// Workgroups that hold the rows of n_q tokens of B requests however they are divided.
-inline int64_t paged_tiles(const PagedView& p, int G, int n_q) { return (int64_t)n_q * G / (32 * chunk_waves(p.d / 64)) + p.B; }
+constexpr int chunk_rows(int T) { return 32 * chunk_waves(T); }
+// Workgroups of so many rows that hold n_q tokens of B requests however they are divided.
+inline int64_t paged_tiles(const PagedView& p, int G, int n_q, int rows) { return (int64_t)n_q * G / rows + p.B; }
 
-// Bytes of the ranges' results: (reference, sum) and d fp32 values of every row and query head.
+// Bytes of the ranges' results: two numbers and d fp32 values of every row and query head.
 inline int64_t paged_ws_bytes(const PagedView& p, int Hq, int n_q, int n_splits) {
   return n_splits <= 1 ? 0 : (int64_t)n_splits * n_q * Hq * (p.d + 2) * 4;
 }
 
-// Ranges that a call takes by itself: a workgroup a CU, each of at least four tiles.
-inline int paged_splits(const PagedView& p, int G, int n_q, int max_q, int64_t max_tokens) {
-  const int64_t groups = paged_tiles(p, G, n_q) * p.H, tiles = max_tokens / 64 / 4;
-  const int64_t n = 256 / groups;
-  return (int)(n < 1 || tiles < 1 ? 1 : n < tiles ? n : tiles);
+// Which kernels a call takes, and the ranges that it takes by itself (n_splits <= 0) for requests of up to max_q tokens that see
+// up to max_tokens.
+struct PagedPlan {
+  int few, many, mixed;
+};
+inline PagedPlan paged_kernels(const PagedView& p, int G, int n_q, int max_q, int64_t max_tokens, int n_splits) {
+  PagedPlan k = {0, 0, 0};
+  const bool all_few = (int64_t)max_q * G <= kFewRows;
+  k.mixed = !all_few && p.B > 1 && n_q < (int64_t)p.B * max_q;  // (else every request has max_q)
+  auto ranges = [&](int64_t groups, int64_t target, int64_t least) {
+    if (n_splits > 0) return n_splits;
+    const int64_t n = target / groups, most = max_tokens / least;
+    return (int)(n < 1 || most < 1 ? 1 : n < most ? n : most);
+  };
+  // few rows: about 2048 waves of at least 64 tokens; many: a workgroup a CU of at least four tiles
+  if (all_few || k.mixed) k.few = ranges((int64_t)(p.B < n_q ? p.B : n_q) * p.H, 2048, 64);
+  if (!all_few) {
+    const int T = p.d / 64;
+    k.many = ranges(((int64_t)n_q * G + chunk_rows(T) - 1) / chunk_rows(T) * p.H, 256, 256);
+  }
+  return k;
 }
 hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s);
 

@@ -148,8 +148,8 @@ size_t mustafar_paged_attn_workspace_bytes(const mustafar_pages_t* p, int Hq, in
   if (check_pages(p) != MUSTAFAR_OK || Hq < 1 || Hq % p->H != 0 || Hq / p->H > MUSTAFAR_PAGED_MAX_GROUP) return 0;
   if (n_q < 1 || max_q < 0 || max_tokens < 0 || n_splits > kMaxSplits || (int64_t)n_q * Hq >= kMaxGroups) return 0;
   const mf::PagedView v = view_of(p);
-  if (n_splits <= 0) n_splits = mf::paged_splits(v, Hq / p->H, n_q, max_q, max_tokens);
-  return (size_t)mf::paged_ws_bytes(v, Hq, n_q, n_splits);
+  const mf::PagedPlan k = mf::paged_kernels(v, Hq / p->H, n_q, max_q, max_tokens, n_splits);
+  return (size_t)mf::paged_ws_bytes(v, Hq, n_q, k.few > k.many ? k.few : k.many);
 }
 
 int mustafar_paged_attn(const void* q, int64_t q_stride, int n_q, int Hq, const mustafar_pages_t* p, const void* cu,
@@ -172,13 +172,15 @@ int mustafar_paged_attn(const void* q, int64_t q_stride, int n_q, int Hq, const 
   a.p = view_of(p);
   const size_t need = mustafar_paged_attn_workspace_bytes(p, Hq, n_q, max_q, max_tokens, n_splits);
   if (need > 0 && (!aligned(ws, 16) || ws_bytes < need)) return MUSTAFAR_EWORKSPACE;
-  if (n_splits <= 0) {
-    // (what the rows see: never more than the workspace was sized for)
-    const int64_t seen = window > 0 ? (int64_t)window + max_q + sinks : max_tokens;
-    n_splits = mf::paged_splits(a.p, Hq / p->H, n_q, max_q, seen < max_tokens ? seen : max_tokens);
-  }
-  if (mf::paged_tiles(a.p, Hq / p->H, n_q) * p->H * n_splits >= kMaxGroups) return MUSTAFAR_EINVAL;
-  a.n_splits = n_splits;
+  // (what the rows see: never more than the workspace was sized for)
+  const int64_t seen = window > 0 ? (int64_t)window + max_q + sinks : max_tokens;
+  const mf::PagedPlan k = mf::paged_kernels(a.p, Hq / p->H, n_q, max_q, seen < max_tokens ? seen : max_tokens, n_splits);
+  const int64_t tiles = k.few > 0 && !k.mixed ? mf::paged_tiles(a.p, Hq / p->H, n_q, mf::kFewRows)
+                                              : mf::paged_tiles(a.p, Hq / p->H, n_q, mf::chunk_rows(p->d / kTile));
+  if ((double)tiles * p->H * (k.few > k.many ? k.few : k.many) >= (double)kMaxGroups) return MUSTAFAR_EINVAL;
+  a.few = k.few;
+  a.many = k.many;
+  a.mixed = k.mixed;
   a.ws = ws;
   a.q = (const uint16_t*)q;
   a.out = (uint16_t*)out;

@@ -69,28 +69,37 @@ struct RowTile {
 
 __device__ __forceinline__ int first_tile(int cu, int b, int G, int BM) { return (int)((int64_t)cu * G / BM) + b; }
 
-// Two rounds of 64 entries at most, one load each.
-__device__ __forceinline__ RowTile row_tile(const PagedAttnArgs& a, int tile, int BM) {
-  const int B = a.p.B, lane = (int)lane_id();
-  const int stride = (B + kWave - 1) / kWave;
-  int b = min(lane * stride, B - 1);
-  uint64_t below = ballot(lane * stride < B && first_tile(a.cu[b], b, a.G, BM) <= tile);
-  b = (63 - __builtin_clzll(below | 1)) * stride;
-  if (stride > 1) {
-    const int c = min(b + lane, B - 1);
-    below = ballot(lane < stride && b + lane < B && first_tile(a.cu[c], c, a.G, BM) <= tile);
-    b += 63 - __builtin_clzll(below | 1);
-  }
-  b = __builtin_amdgcn_readfirstlane(b);
+__device__ __forceinline__ RowTile rows_of(const PagedAttnArgs& a, int b) {
   RowTile r;
   r.b = b;
+  r.row0 = 0;
   r.tok0 = __builtin_amdgcn_readfirstlane(a.cu[b]);
   const int nq = min(__builtin_amdgcn_readfirstlane(a.cu[b + 1]), a.n_q) - r.tok0;
   r.rows = nq * a.G;
-  r.row0 = (tile - first_tile(r.tok0, b, a.G, BM)) * BM;
   const int64_t most = (int64_t)a.p.max_pages << a.p.log2_page;
-  const int len = __builtin_amdgcn_readfirstlane((int)min((int64_t)max(a.p.state[b], 0), most));
-  r.base = len - nq;
+  r.base = __builtin_amdgcn_readfirstlane((int)min((int64_t)max(a.p.state[b], 0), most)) - nq;
+  return r;
+}
+
+// The last request b of which first(cu[b], b) <= x: two rounds of 64 entries at most, one load each.
+template <typename F>
+__device__ __forceinline__ int find_request(const PagedAttnArgs& a, int x, F first) {
+  const int B = a.p.B, lane = (int)lane_id();
+  const int stride = (B + kWave - 1) / kWave;
+  int b = min(lane * stride, B - 1);
+  uint64_t below = ballot(lane * stride < B && first(a.cu[b], b) <= x);
+  b = (63 - __builtin_clzll(below | 1)) * stride;
+  if (stride > 1) {
+    const int c = min(b + lane, B - 1);
+    below = ballot(lane < stride && b + lane < B && first(a.cu[c], c) <= x);
+    b += 63 - __builtin_clzll(below | 1);
+  }
+  return __builtin_amdgcn_readfirstlane(b);
+}
+
+__device__ __forceinline__ RowTile row_tile(const PagedAttnArgs& a, int tile, int BM) {
+  RowTile r = rows_of(a, find_request(a, tile, [&](int cu, int b) { return first_tile(cu, b, a.G, BM); }));
+  r.row0 = (tile - first_tile(r.tok0, r.b, a.G, BM)) * BM;
   return r;
 }
 
@@ -302,7 +311,7 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
   const int h = blockIdx.x % p.H, split = (blockIdx.x / p.H) % part.n_splits;
   const int tile = (int)(gridDim.x / (p.H * part.n_splits)) - 1 - (int)(blockIdx.x / (p.H * part.n_splits));
   const RowTile rt = row_tile(a, tile, BM);
-  if (rt.row0 >= rt.rows) return;
+  if (rt.row0 >= rt.rows || (a.mixed && rt.rows <= kFewRows)) return;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
   const uint32_t lane = lane_id(), r32 = lane % 32, half = lane / 32;
   const int wrow = rt.row0 + 32 * wave;  // the wave's first row
@@ -629,15 +638,243 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
 }
 
 // ------------------------------------------------------------------------------------------
-// k_paged_merge: the ranges of a row together, one wave a row.
+// k_paged_rows: at most 16 rows, one wave, tiles of 32 tokens: single tokens (and few) over a long cache.
+//
+// The loads bound it (16 KB of keys and values a tile at d = 128 for some 250 vector instructions), so nothing goes through
+// LDS: a key row's 16-byte pieces are the A operand of S = K Q^T as they are loaded (lane = token l % 16, channels 32 c +
+// 8 (l / 16)), its result (row l % 16, tokens 4 (l / 16) + e of the tile's two groups of 16) is the A operand of O = P V, and a
+// lane loads channels 4 T (l % 16) .. of those eight tokens and transposes them with byte permutes into the B operand.
 // ------------------------------------------------------------------------------------------
+constexpr int kRowsTile = 32;
+
+template <bool BF16>
+__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+  if constexpr (BF16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
+}
+
 template <int T, bool BF16>
-__global__ __launch_bounds__(64) void k_paged_merge(PagedAttnArgs a, PartOut part) {
+__global__ __launch_bounds__(kWave) void k_paged_rows(PagedAttnArgs a, PartOut part) {
+  constexpr int d = kTile * T, NC = 2 * T, NO = 4 * T, BN = kRowsTile;
+  const PagedView& p = a.p;
+  const int h = blockIdx.x % p.H, split = (blockIdx.x / p.H) % part.n_splits, tile = blockIdx.x / (p.H * part.n_splits);
+  const RowTile rt = a.mixed ? rows_of(a, tile) : row_tile(a, tile, kFewRows);
+  if (rt.row0 >= rt.rows || (a.mixed && rt.rows > kFewRows)) return;
+  const uint32_t lane = lane_id(), r16 = lane % 16, q4 = lane / 16;
+  const int row = min(rt.row0 + (int)r16, rt.rows - 1), tok = row / a.G, pos = rt.base + tok;
+  const int pos0 = rt.base + rt.row0 / a.G, pos1 = rt.base + (min(rt.row0 + kFewRows, rt.rows) - 1) / a.G;
+  const TileList tl(pos0, pos1, a.window, a.sinks, BN);
+  const int t0 = (int)((int64_t)tl.n * split / part.n_splits);
+  const int n = (int)((int64_t)tl.n * (split + 1) / part.n_splits) - t0;
+  // Tiles [clean0, clean1) are seen whole by every row, [whole0, whole1) by some.
+  const int clean0 = a.window > 0 ? tl.count_to(pos1 - a.window, BN) - t0 : 0, clean1 = tl.count_to(pos0 - BN + 1, BN) - t0;
+  const int whole0 = tl.count_to(tl.lo - 1, BN) - t0, whole1 = tl.count_to(tl.hi - BN + 1, BN) - t0;
+
+  // Lane i holds the offset in k and v of group i of 16 tokens of the 32 tiles at hand (one that no row sees is replaced by the
+  // nearest that some row does; pages hold 16 tokens or more).
+  uint32_t at_lo = 0, at_hi = 0;
+  const uint32_t row_bytes = 2u * (uint32_t)p.token_stride;
+  auto group_of = [&](int t, int g) __attribute__((always_inline)) {
+    const int g0 = tl.start(t0 + t, BN) + 16 * g;
+    return g0 < tl.sinks ? g0 : min(max(g0, tl.lo & ~15), tl.hi & ~15);
+  };
+  auto look_up = [&](int first) __attribute__((always_inline)) {
+    const int g0 = group_of(min(first + (int)lane / 2, n - 1), lane & 1);
+    int page = p.table[(int64_t)rt.b * p.max_pages + (g0 >> p.log2_page)];
+    if ((uint32_t)page >= (uint32_t)p.n_pages) page = 0;
+    const int64_t at = 2 * ((int64_t)page * p.page_stride + (int64_t)h * p.head_stride +
+                            (int64_t)(g0 & ((1 << p.log2_page) - 1)) * p.token_stride);
+    at_lo = (uint32_t)at;
+    at_hi = (uint32_t)(at >> 32);
+  };
+  auto base_of = [&](const uint16_t* x, int t, int g) __attribute__((always_inline)) {
+    const int i = (2 * t + g) % kWave;
+    return reinterpret_cast<const unsigned char*>(x) + ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)at_hi, i) << 32 |
+                                                        (uint32_t)__builtin_amdgcn_readlane((int)at_lo, i));
+  };
+  // Row r of a group of a tile at the ends of what is seen: the nearest that some row sees (the others may be what memory held,
+  // and 0 times that is not 0).
+  auto nearest = [&](int r, int t, int g) __attribute__((always_inline)) {
+    const int g0 = group_of(t, g);
+    const bool first = g0 < tl.sinks;
+    const int from = first ? 0 : tl.lo, to = first && tl.lo > g0 + 15 ? tl.sinks - 1 : tl.hi;
+    return min(max(r, from - g0), min(to - g0, 15));
+  };
+  u32x4 kr[2][NC];
+  uint32_t vr[8][2 * T];
+  auto load_keys = [&](int t) __attribute__((always_inline)) {
+    if (t % (kWave / 2) == 0) look_up(t);
+    const bool edge = t < whole0 || t >= whole1;
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      uint32_t r = r16;
+      if (edge) r = (uint32_t)nearest((int)r, t, g);
+      const unsigned char* x = base_of(p.k, t, g) + (r * row_bytes + 16u * q4);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) kr[g][c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(x + 64 * c));
+    }
+  };
+  auto load_values = [&](int t) __attribute__((always_inline)) {
+    const bool edge = t < whole0 || t >= whole1;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      uint32_t r = 4 * q4 + i % 4;
+      if (edge) r = (uint32_t)nearest((int)r, t, i / 4);
+      const unsigned char* x = base_of(p.v, t, i / 4) + (r * row_bytes + 2u * NO * r16);
+      if constexpr (T == 1) {
+        const u32x2 v = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(x));
+        vr[i][0] = v.x;
+        vr[i][1] = v.y;
+      } else {
+#pragma unroll
+        for (int m = 0; m < T / 2; ++m) {
+          const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(x) + m);
+          vr[i][4 * m] = v.x;
+          vr[i][4 * m + 1] = v.y;
+          vr[i][4 * m + 2] = v.z;
+          vr[i][4 * m + 3] = v.w;
+        }
+      }
+    }
+  };
+
+  const float inv_scale = 1.f / a.scale_log2;
+  float l = 0.f, shift = 0.f, limit = -INFINITY;
+  f32x4 o[NO];
+#pragma unroll
+  for (int c = 0; c < NO; ++c) o[c] = (f32x4){};
+  if (n > 0) {
+    load_keys(0);
+    u32x4 qb[NC];  // Q as the B operand: column = row, k = 32 c + 8 (l / 16) + i
+    {
+      const uint16_t* q = a.q + (int64_t)(rt.tok0 + tok) * a.q_stride + (h * a.G + row - tok * a.G) * d + 8 * q4;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) qb[c] = *reinterpret_cast<const u32x4*>(q + 32 * c);
+    }
+    load_values(0);
+    for (int t = 0; t < n; ++t) {
+      f32x4 s[2] = {};
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) s[g] = mfma16<BF16>(kr[g][c], qb[c], s[g]);
+      // (the values of the tile whose offsets this may replace are loaded already)
+      if (t + 1 < n) load_keys(t + 1);
+      if (t < clean0 || t >= clean1) {
+        const int j0 = tl.start(t0 + t, BN) + 4 * (int)q4;
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (!sees(pos, j0 + 16 * g + e, a.window, a.sinks)) s[g][e] = -INFINITY;
+      }
+      float top = s[0][0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) top = fmaxf(top, s[e / 4][e % 4]);
+      if (ballot(top > limit)) {
+        top = fmaxf(top, __shfl_xor(top, 16, kWave));
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        const bool move = top > limit;
+        const float to = move ? fmaf(-top, a.scale_log2, kBias) : shift;
+        const float alpha = limit > -INFINITY ? __builtin_amdgcn_exp2f(to - shift) : 1.f;
+        if (move) limit = fmaf(kSlack, inv_scale, top);
+        shift = to;
+        l *= alpha;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float ae = __shfl(alpha, (int)(4 * q4) + e, kWave);  // row 4 (l / 16) + e of the outputs
+#pragma unroll
+          for (int c = 0; c < NO; ++c) o[c][e] *= ae;
+        }
+      }
+      u32x4 pa;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[e / 2][2 * (e % 2)], a.scale_log2, shift));
+        const float y = __builtin_amdgcn_exp2f(fmaf(s[e / 2][2 * (e % 2) + 1], a.scale_log2, shift));
+        pa[e] = pack2<BF16>(x, y);
+        l = add_pair<BF16>(pa[e], l);
+      }
+#pragma unroll
+      for (int c = 0; c < NO; ++c) {
+        uint32_t y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          y[i] = __builtin_amdgcn_perm(vr[2 * i + 1][c / 2], vr[2 * i][c / 2], (c & 1) ? 0x07060302u : 0x05040100u);
+        o[c] = mfma16<BF16>(pa, (u32x4){y[0], y[1], y[2], y[3]}, o[c]);
+      }
+      if (t + 1 < n) load_values(t + 1);
+    }
+  }
+
+  l += __shfl_xor(l, 16, kWave);
+  l += __shfl_xor(l, 32, kWave);
+  float z = l * 0.f;  // NaN if something is not finite
+#pragma unroll
+  for (int c = 0; c < NO; ++c)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (rt.row0 + (int)(4 * q4) + e < rt.rows) z = fmaf(o[c][e], 0.f, z);
+  if (ballot(z != z || (rt.row0 + (int)r16 < rt.rows && limit > -INFINITY && l == 0.f))) {
+    redo_rows<T, BF16>(a, part, rt, h, rt.row0, kFewRows, tl, t0, t0 + n, split, BN);
+    return;
+  }
+  const int64_t part0 = (int64_t)split * a.n_q * a.Hq;
+  if (part.n_splits > 1 && q4 == 0 && rt.row0 + (int)r16 < rt.rows)
+    part.ml[part0 + (int64_t)(rt.tok0 + tok) * a.Hq + h * a.G + row - tok * a.G] =
+        make_float2(limit > -INFINITY ? -shift : -INFINITY, pos < 0 ? -1.f : l);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int orow = rt.row0 + (int)(4 * q4) + e, otok = orow / a.G, hq = h * a.G + orow - otok * a.G;
+    const float le = __shfl(l, (int)(4 * q4) + e, kWave);
+    if (orow >= rt.rows) continue;
+    const int64_t t = rt.tok0 + otok;
+    if (part.n_splits > 1) {
+      f32x4* dst = reinterpret_cast<f32x4*>(part.o + (part0 + t * a.Hq + hq) * d + NO * r16);
+#pragma unroll
+      for (int c = 0; c < T; ++c) dst[c] = (f32x4){o[4 * c][e], o[4 * c + 1][e], o[4 * c + 2][e], o[4 * c + 3][e]};
+    } else {
+      const float inv = rt.base + otok < 0 ? 0.f : 1.f / le;
+      u32x2* dst = reinterpret_cast<u32x2*>(a.out + t * a.out_stride + hq * d + NO * r16);
+#pragma unroll
+      for (int c = 0; c < T; ++c)
+        dst[c] = (u32x2){pack2<BF16>(o[4 * c][e] * inv, o[4 * c + 1][e] * inv), pack2<BF16>(o[4 * c + 2][e] * inv, o[4 * c + 3][e] * inv)};
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// k_paged_merge: the ranges of a row together, WAVES waves a row: wave w takes ranges w, w + WAVES, .., kMergeAhead of their
+// outputs under way at once, and LDS adds the waves up. One wave for few ranges (four rows a workgroup): 16384 rows
+// of 3 ranges at d = 128 take 11 us so and 31 with four.
+// ------------------------------------------------------------------------------------------
+constexpr int kMergeWaves = 4, kMergeAhead = 8, kMergeNarrow = 8;
+
+template <int T, bool BF16, int WAVES>
+__global__ __launch_bounds__(kMergeWaves * kWave) void k_paged_merge(PagedAttnArgs a, PartOut part, int of_few) {
   constexpr int d = kTile * T;
-  const int lane = (int)lane_id();
-  const int64_t rows = (int64_t)a.n_q * a.Hq, row = blockIdx.x;
-  const int t = (int)(row / a.Hq), hq = (int)(row - (int64_t)t * a.Hq);
-  if (t >= a.cu[a.p.B]) return;
+  __shared__ float sums[WAVES > 1 ? kMergeWaves : 1][d + 1];
+  const int lane = (int)lane_id(), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+  const int64_t rows = (int64_t)a.n_q * a.Hq, i0 = WAVES > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * kMergeWaves + wave;
+  // The row: of q and all its heads, or, where the requests of few rows have ranges of their own, the r-th of a request's and kv-head's.
+  int t, hq;
+  if (a.mixed && of_few) {
+    const int r = (int)(i0 % kFewRows), h = (int)(i0 / kFewRows % a.p.H), b = (int)(i0 / kFewRows / a.p.H);
+    if (b >= a.p.B) return;
+    const RowTile rt = rows_of(a, b);
+    if (r >= rt.rows || rt.rows > kFewRows) return;
+    t = rt.tok0 + r / a.G;
+    hq = h * a.G + r % a.G;
+  } else {
+    t = (int)(i0 / a.Hq);
+    hq = (int)(i0 - (int64_t)t * a.Hq);
+    if (i0 >= rows || t >= a.cu[a.p.B]) return;
+    if (a.mixed && rows_of(a, find_request(a, t, [](int cu, int) { return cu; })).rows <= kFewRows) return;
+  }
+  const int64_t row = (int64_t)t * a.Hq + hq;
+  const int first = WAVES > 1 ? wave : 0;
   float M = -INFINITY;
   bool nothing = false;
   for (int s = lane; s < part.n_splits; s += kWave) {
@@ -647,31 +884,86 @@ __global__ __launch_bounds__(64) void k_paged_merge(PagedAttnArgs a, PartOut par
   }
   M = wave_max(M);
   float l = 0.f, o[T] = {};
-  for (int s = 0; s < part.n_splits; ++s) {
-    const float2 ml = part.ml[s * rows + row];
-    if (ml.x == -INFINITY && ml.y == 0.f) continue;
-    const float w = at_least(__builtin_amdgcn_exp2f(ml.x - M));
-    l = fmaf(ml.y, w, l);
+  for (int s0 = 0; s0 < part.n_splits; s0 += kWave) {
+    // lane i: the weight of range s0 + i, 0 for one without any (its output is not looked at)
+    float w = 0.f;
+    if (s0 + lane < part.n_splits) {
+      const float2 ml = part.ml[(s0 + lane) * rows + row];
+      if (ml.x != -INFINITY || ml.y != 0.f) w = at_least(__builtin_amdgcn_exp2f(ml.x - M));
+      if (lane % WAVES == first && w != 0.f) l = fmaf(ml.y, w, l);
+    }
+    const int end = min(kWave, part.n_splits - s0);
+    for (int i = first; i < end; i += WAVES * kMergeAhead) {
+      float x[kMergeAhead][T], wi[kMergeAhead];
 #pragma unroll
-    for (int c = 0; c < T; ++c) o[c] = fmaf(part.o[(s * rows + row) * d + kTile * c + lane], w, o[c]);
+      for (int k = 0; k < kMergeAhead; ++k) {
+        const int j = i + k * WAVES;
+        wi[k] = j < end ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), j & (kWave - 1))) : 0.f;
+        const float* src = part.o + ((int64_t)(s0 + (j < end ? j : i)) * rows + row) * d + lane;
+#pragma unroll
+        for (int c = 0; c < T; ++c) x[k][c] = src[kTile * c];
+      }
+#pragma unroll
+      for (int k = 0; k < kMergeAhead; ++k)
+#pragma unroll
+        for (int c = 0; c < T; ++c) o[c] = wi[k] == 0.f ? o[c] : fmaf(x[k][c], wi[k], o[c]);
+    }
   }
+  l = wave_sum(l);
   const bool zero = ballot(nothing) != 0;
+  if constexpr (WAVES > 1) {
+#pragma unroll
+    for (int c = 0; c < T; ++c) sums[wave][lane + kTile * c] = o[c];
+    if (lane == 0) sums[wave][d] = l;
+    __syncthreads();
+    if (wave != 0) return;
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) {
+      l += sums[w][d];
+#pragma unroll
+      for (int c = 0; c < T; ++c) o[c] += sums[w][lane + kTile * c];
+    }
+  }
 #pragma unroll
   for (int c = 0; c < T; ++c)
     a.out[t * a.out_stride + hq * d + kTile * c + lane] = (uint16_t)pack2<BF16>(zero ? 0.f : o[c] / l, 0.f);
 }
 
 template <int T, bool BF16>
+static hipError_t merge_launch(const PagedAttnArgs& a, const PartOut& part, bool of_few, hipStream_t s) {
+  if (part.n_splits <= 1) return hipSuccess;  // (written by its kernel)
+  const int64_t rows = a.mixed && of_few ? (int64_t)a.p.B * a.p.H * kFewRows : (int64_t)a.n_q * a.Hq;
+  if (part.n_splits <= kMergeNarrow)
+    hipLaunchKernelGGL((k_paged_merge<T, BF16, 1>), dim3((uint32_t)((rows + kMergeWaves - 1) / kMergeWaves)),
+                       dim3(kMergeWaves * kWave), 0, s, a, part, (int)of_few);
+  else
+    hipLaunchKernelGGL((k_paged_merge<T, BF16, kMergeWaves>), dim3((uint32_t)rows), dim3(kMergeWaves * kWave), 0, s, a, part,
+                       (int)of_few);
+  return hipGetLastError();
+}
+
+template <int T, bool BF16>
 static hipError_t attn_launch(const PagedAttnArgs& a, hipStream_t s) {
   const int64_t rows = (int64_t)a.n_q * a.Hq;
-  PartOut part = {(float2*)a.ws, nullptr, a.n_splits};
-  part.o = (float*)(part.ml + (int64_t)a.n_splits * rows);
-  const int64_t groups = paged_tiles(a.p, a.G, a.n_q) * a.p.H * a.n_splits;
-  hipLaunchKernelGGL((k_paged_chunk<T, BF16>), dim3((uint32_t)groups), dim3(kWave * chunk_waves(T)), 0, s, a, part);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.n_splits == 1) return e;
-  hipLaunchKernelGGL((k_paged_merge<T, BF16>), dim3((uint32_t)rows), dim3(kWave), 0, s, a, part);
-  return hipGetLastError();
+  const int most = a.few > a.many ? a.few : a.many;
+  PartOut few = {(float2*)a.ws, nullptr, a.few}, many;
+  few.o = (float*)(few.ml + most * rows);
+  many = few;
+  many.n_splits = a.many;
+  hipError_t e;
+  if (a.few > 0) {
+    const int64_t tiles = a.mixed ? a.p.B : paged_tiles(a.p, a.G, a.n_q, kFewRows);
+    hipLaunchKernelGGL((k_paged_rows<T, BF16>), dim3((uint32_t)(tiles * a.p.H * a.few)), dim3(kWave), 0, s, a, few);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if (a.many > 0) {
+    const int64_t tiles = paged_tiles(a.p, a.G, a.n_q, chunk_rows(T));
+    hipLaunchKernelGGL((k_paged_chunk<T, BF16>), dim3((uint32_t)(tiles * a.p.H * a.many)), dim3(kWave * chunk_waves(T)), 0, s,
+                       a, many);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if ((e = merge_launch<T, BF16>(a, few, true, s)) != hipSuccess) return e;
+  return merge_launch<T, BF16>(a, many, false, s);
 }
 
 hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s) {
