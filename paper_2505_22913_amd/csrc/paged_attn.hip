@@ -69,36 +69,42 @@ struct RowTile {
 
 __device__ __forceinline__ int first_tile(int cu, int b, int G, int BM) { return (int)((int64_t)cu * G / BM) + b; }
 
-__device__ __forceinline__ RowTile rows_of(const PagedAttnArgs& a, int b) {
+__device__ __forceinline__ RowTile rows_at(const PagedAttnArgs& a, int b, int cu, int cu_next, int len) {
   RowTile r;
   r.b = b;
   r.row0 = 0;
-  r.tok0 = __builtin_amdgcn_readfirstlane(a.cu[b]);
-  const int nq = min(__builtin_amdgcn_readfirstlane(a.cu[b + 1]), a.n_q) - r.tok0;
+  r.tok0 = cu;
+  const int nq = min(cu_next, a.n_q) - cu;
   r.rows = nq * a.G;
-  const int64_t most = (int64_t)a.p.max_pages << a.p.log2_page;
-  r.base = __builtin_amdgcn_readfirstlane((int)min((int64_t)max(a.p.state[b], 0), most)) - nq;
+  r.base = (int)min((int64_t)max(len, 0), (int64_t)a.p.max_pages << a.p.log2_page) - nq;
   return r;
 }
 
-// The last request b of which first(cu[b], b) <= x: two rounds of 64 entries at most, one load each.
+__device__ __forceinline__ RowTile rows_of(const PagedAttnArgs& a, int b) {
+  const int cu = a.cu[b], next = a.cu[b + 1], len = a.p.state[b];
+  return rows_at(a, b, __builtin_amdgcn_readfirstlane(cu), __builtin_amdgcn_readfirstlane(next), __builtin_amdgcn_readfirstlane(len));
+}
+
+// The last request b of which first(cu[b], b) <= x, with its rows: up to 64 requests, one round of loads; else two, and its own.
 template <typename F>
-__device__ __forceinline__ int find_request(const PagedAttnArgs& a, int x, F first) {
+__device__ __forceinline__ RowTile find_rows(const PagedAttnArgs& a, int x, F first) {
   const int B = a.p.B, lane = (int)lane_id();
+  if (B <= kWave) {
+    const int b = min(lane, B - 1), cu = a.cu[b], next = a.cu[b + 1], len = a.p.state[b];
+    const int at = 63 - __builtin_clzll(ballot(lane < B && first(cu, b) <= x) | 1);
+    return rows_at(a, at, __builtin_amdgcn_readlane(cu, at), __builtin_amdgcn_readlane(next, at), __builtin_amdgcn_readlane(len, at));
+  }
   const int stride = (B + kWave - 1) / kWave;
   int b = min(lane * stride, B - 1);
   uint64_t below = ballot(lane * stride < B && first(a.cu[b], b) <= x);
   b = (63 - __builtin_clzll(below | 1)) * stride;
-  if (stride > 1) {
-    const int c = min(b + lane, B - 1);
-    below = ballot(lane < stride && b + lane < B && first(a.cu[c], c) <= x);
-    b += 63 - __builtin_clzll(below | 1);
-  }
-  return __builtin_amdgcn_readfirstlane(b);
+  const int c = min(b + lane, B - 1);
+  below = ballot(lane < stride && b + lane < B && first(a.cu[c], c) <= x);
+  return rows_of(a, __builtin_amdgcn_readfirstlane(b + 63 - (int)__builtin_clzll(below | 1)));
 }
 
 __device__ __forceinline__ RowTile row_tile(const PagedAttnArgs& a, int tile, int BM) {
-  RowTile r = rows_of(a, find_request(a, tile, [&](int cu, int b) { return first_tile(cu, b, a.G, BM); }));
+  RowTile r = find_rows(a, tile, [&](int cu, int b) { return first_tile(cu, b, a.G, BM); });
   r.row0 = (tile - first_tile(r.tok0, r.b, a.G, BM)) * BM;
   return r;
 }
@@ -871,7 +877,7 @@ __global__ __launch_bounds__(kMergeWaves * kWave) void k_paged_merge(PagedAttnAr
     t = (int)(i0 / a.Hq);
     hq = (int)(i0 - (int64_t)t * a.Hq);
     if (i0 >= rows || t >= a.cu[a.p.B]) return;
-    if (a.mixed && rows_of(a, find_request(a, t, [](int cu, int) { return cu; })).rows <= kFewRows) return;
+    if (a.mixed && find_rows(a, t, [](int cu, int) { return cu; }).rows <= kFewRows) return;
   }
   const int64_t row = (int64_t)t * a.Hq + hq;
   const int first = WAVES > 1 ? wave : 0;
