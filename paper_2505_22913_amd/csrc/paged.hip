@@ -22,9 +22,11 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // those that nobody reads, and the stack is written only above its old top.
 // In place, the lengths may be overwritten once every workgroup is done with them: the
 // last one to take a ticket (the state's last word, back at 0 afterwards) writes them.
+// A chain of memory latencies bounds it (lengths, prefix sums, table or stack, slot), so a thread has one slot until 65536:
+// 64 requests of a token each take 4.2 us, 256 with up to 512 tokens (256 workgroups) 9.3; with four slots a thread 13.1.
 // ------------------------------------------------------------------------------------------
 constexpr int kPlanThreads = 256;
-constexpr int kPlanPerGroup = 1024;  // slots a workgroup
+constexpr int kPlanPerGroup = 256;  // slots a workgroup
 enum { kPlanPages = 1, kPlanTable = 2, kPlanSlots = 4, kPlanState = 8 };
 
 struct PlanArgs {
@@ -79,6 +81,7 @@ __device__ __forceinline__ int plan_find(const uint32_t* at, int B, uint32_t i) 
 __global__ __launch_bounds__(kPlanThreads) void k_paged_plan(PlanArgs a) {
   extern __shared__ uint32_t sm[];  // cu, taken, given: [B + 1] each
   __shared__ uint32_t wsum[3][kPlanThreads / kWave];
+  __shared__ int wbits[kPlanThreads / kWave];
   __shared__ int last;
   uint32_t* cu = sm;
   uint32_t* taken = sm + a.B + 1;
@@ -108,15 +111,19 @@ __global__ __launch_bounds__(kPlanThreads) void k_paged_plan(PlanArgs a) {
   int bits = 0;
 #pragma unroll
   for (int bit = 1; bit <= kPlanState; bit *= 2)
-    if (__syncthreads_or(wrong & bit)) bits |= bit;
+    if (ballot((wrong & bit) != 0)) bits |= bit;
+  if (t % kWave == 0) wbits[wave] = bits;
+  __syncthreads();
   uint32_t total[3] = {0u, 0u, 0u};
 #pragma unroll
-  for (int w = 0; w < kPlanThreads / kWave; ++w)
+  for (int w = 0; w < kPlanThreads / kWave; ++w) {
+    bits |= wbits[w];
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
       if (w < wave) base[k] += wsum[k][w];
       total[k] += wsum[k][w];
     }
+  }
   if (!bits) {
     if (total[0] > (uint32_t)a.n_slots) bits |= kPlanSlots;
     if (total[1] > total[2] && total[1] - total[2] > (uint32_t)n_free) bits |= kPlanPages;
