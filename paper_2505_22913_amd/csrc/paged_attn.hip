@@ -852,99 +852,114 @@ __global__ __launch_bounds__(kWave) void k_paged_rows(PagedAttnArgs a, PartOut p
 }
 
 // ------------------------------------------------------------------------------------------
-// k_paged_merge: the ranges of a row together, WAVES waves a row: wave w takes ranges w, w + WAVES, .., kMergeAhead of their
-// outputs under way at once, and LDS adds the waves up. One wave for few ranges (four rows a workgroup): 16384 rows
-// of 3 ranges at d = 128 take 11 us so and 31 with four.
+// k_paged_merge: the ranges of a row together, out = sum w o / sum w l with w = 2^(m - max m).
+//
+// A stream of d / 4 lanes loads a range's outputs, four a lane, kMergeAhead ranges at once and the first ones before the weights
+// are known; OF lanes look at the weights. A row has one stream, or, where rows are few and ranges many (WIDE), the 16 / T of a
+// workgroup, each with every (16 / T)-th range, which shuffles and LDS add up. Latency bounds it: 4 us for up to 500 rows; at
+// d = 128, 16384 rows of 4 ranges take 9.4 us (3.8 TB/s; 12.5 with a wave a row). One stream a row against a workgroup a row:
+// 32 rows of 256 ranges 23.4 and 7.2 us, 512 of 16 4.8 both, 992 of 8 to 16 6.5 and 7.8, 2404 of 21 7.6 and 13.0.
 // ------------------------------------------------------------------------------------------
-constexpr int kMergeWaves = 4, kMergeAhead = 8, kMergeNarrow = 8;
+constexpr int kMergeThreads = 256, kMergeAhead = 8, kMergeWideRows = 512;
 
-template <int T, bool BF16, int WAVES>
-__global__ __launch_bounds__(kMergeWaves * kWave) void k_paged_merge(PagedAttnArgs a, PartOut part, int of_few) {
-  constexpr int d = kTile * T;
-  __shared__ float sums[WAVES > 1 ? kMergeWaves : 1][d + 1];
-  const int lane = (int)lane_id(), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
-  const int64_t rows = (int64_t)a.n_q * a.Hq, i0 = WAVES > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * kMergeWaves + wave;
+template <int T, bool BF16, int OF, bool WIDE>
+__global__ __launch_bounds__(kMergeThreads) void k_paged_merge(PagedAttnArgs a, PartOut part, int of_few) {
+  constexpr int d = kTile * T, L = 16 * T, S = kMergeThreads / L;
+  constexpr int kStep = WIDE ? S : 1;
+  const int lane = (int)lane_id(), stream = (int)threadIdx.x / L, sub = (int)threadIdx.x % L;
+  const int64_t rows = (int64_t)a.n_q * a.Hq, i0 = WIDE ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * S + stream;
   // The row: of q and all its heads, or, where the requests of few rows have ranges of their own, the r-th of a request's and kv-head's.
   int t, hq;
+  bool mine;
   if (a.mixed && of_few) {
     const int r = (int)(i0 % kFewRows), h = (int)(i0 / kFewRows % a.p.H), b = (int)(i0 / kFewRows / a.p.H);
     if (b >= a.p.B) return;
-    const RowTile rt = rows_of(a, b);
-    if (r >= rt.rows || rt.rows > kFewRows) return;
+    const RowTile rt = rows_of(a, b);  // (a wave's rows are one request's: S divides kFewRows)
+    mine = r < rt.rows && rt.rows <= kFewRows;
     t = rt.tok0 + r / a.G;
     hq = h * a.G + r % a.G;
   } else {
     t = (int)(i0 / a.Hq);
     hq = (int)(i0 - (int64_t)t * a.Hq);
-    if (i0 >= rows || t >= a.cu[a.p.B]) return;
-    if (a.mixed && find_rows(a, t, [](int cu, int) { return cu; }).rows <= kFewRows) return;
-  }
-  const int64_t row = (int64_t)t * a.Hq + hq;
-  const int first = WAVES > 1 ? wave : 0;
-  float M = -INFINITY;
-  bool nothing = false;
-  for (int s = lane; s < part.n_splits; s += kWave) {
-    const float2 ml = part.ml[s * rows + row];
-    M = fmaxf(M, ml.x);
-    nothing |= ml.y < 0.f;
-  }
-  M = wave_max(M);
-  float l = 0.f, o[T] = {};
-  for (int s0 = 0; s0 < part.n_splits; s0 += kWave) {
-    // lane i: the weight of range s0 + i, 0 for one without any (its output is not looked at)
-    float w = 0.f;
-    if (s0 + lane < part.n_splits) {
-      const float2 ml = part.ml[(s0 + lane) * rows + row];
-      if (ml.x != -INFINITY || ml.y != 0.f) w = at_least(__builtin_amdgcn_exp2f(ml.x - M));
-      if (lane % WAVES == first && w != 0.f) l = fmaf(ml.y, w, l);
+    mine = i0 < rows && t < a.cu[a.p.B];
+    if (a.mixed) {
+#pragma unroll
+      for (int k = 0; k < (WIDE ? 1 : kWave / L); ++k) {
+        const int x = __builtin_amdgcn_readlane(t, k * L);
+        const bool few = find_rows(a, x, [](int cu, int) { return cu; }).rows <= kFewRows;
+        if (x == t && few) mine = false;
+      }
     }
-    const int end = min(kWave, part.n_splits - s0);
-    for (int i = first; i < end; i += WAVES * kMergeAhead) {
-      float x[kMergeAhead][T], wi[kMergeAhead];
+  }
+  if (!mine) return;  // (all of a stream; WIDE: all of the workgroup)
+  const int64_t row = (int64_t)t * a.Hq + hq;
+  const int first = WIDE ? stream : 0, at = lane % OF;
+  f32x4 x[kMergeAhead], o = {};
+  auto load = [&](int s0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < kMergeAhead; ++k)
+      if (s0 + kStep * k < part.n_splits) x[k] = *reinterpret_cast<const f32x4*>(part.o + ((s0 + kStep * k) * rows + row) * d + 4 * sub);
+  };
+  load(first);
+  float M = -INFINITY, l = 0.f;
+  for (int s = at; s < part.n_splits; s += OF) M = fmaxf(M, part.ml[s * rows + row].x);
+#pragma unroll
+  for (int k = 1; k < OF; k *= 2) M = fmaxf(M, __shfl_xor(M, k, kWave));
+  uint64_t nothing = 0;
+  for (int s0 = 0; s0 < part.n_splits; s0 += OF) {
+    // lane i of those: the weight of range s0 + i, 0 for one without any (its output is not looked at)
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (s0 + at < part.n_splits) ml = part.ml[(s0 + at) * rows + row];
+    const float w = ml.x != -INFINITY || ml.y != 0.f ? at_least(__builtin_amdgcn_exp2f(ml.x - M)) : 0.f;
+    if (w != 0.f) l = fmaf(ml.y, w, l);
+    nothing |= ballot(ml.y < 0.f);
+    const int end = min(s0 + OF, part.n_splits);
+    for (int s = s0; s < end; s += kStep * kMergeAhead) {
 #pragma unroll
       for (int k = 0; k < kMergeAhead; ++k) {
-        const int j = i + k * WAVES;
-        wi[k] = j < end ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), j & (kWave - 1))) : 0.f;
-        const float* src = part.o + ((int64_t)(s0 + (j < end ? j : i)) * rows + row) * d + lane;
+        const int sk = s + first + kStep * k;
+        if (OF == kMergeAhead && sk >= end) break;
+        const float wk = __shfl(w, (lane & -OF) | ((sk - s0) % OF), kWave);
+        if (sk < end && wk != 0.f)
 #pragma unroll
-        for (int c = 0; c < T; ++c) x[k][c] = src[kTile * c];
+          for (int e = 0; e < 4; ++e) o[e] = fmaf(x[k][e], wk, o[e]);
       }
-#pragma unroll
-      for (int k = 0; k < kMergeAhead; ++k)
-#pragma unroll
-        for (int c = 0; c < T; ++c) o[c] = wi[k] == 0.f ? o[c] : fmaf(x[k][c], wi[k], o[c]);
+      load(s + first + kStep * kMergeAhead);
     }
   }
-  l = wave_sum(l);
-  const bool zero = ballot(nothing) != 0;
-  if constexpr (WAVES > 1) {
 #pragma unroll
-    for (int c = 0; c < T; ++c) sums[wave][lane + kTile * c] = o[c];
-    if (lane == 0) sums[wave][d] = l;
+  for (int k = 1; k < OF; k *= 2) l += __shfl_xor(l, k, kWave);
+  const bool zero = (nothing >> (lane & -OF) & (~0ull >> (kWave - OF))) != 0;
+  if constexpr (WIDE) {
+    __shared__ f32x4 sums[kMergeThreads / kWave][L];
+#pragma unroll
+    for (int k = L; k < kWave; k *= 2)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], k, kWave);
+    if (lane < L) sums[threadIdx.x / kWave][lane] = o;
     __syncthreads();
-    if (wave != 0) return;
+    if (threadIdx.x >= L) return;
+    o = sums[0][sub];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) {
-      l += sums[w][d];
-#pragma unroll
-      for (int c = 0; c < T; ++c) o[c] += sums[w][lane + kTile * c];
-    }
+    for (int w = 1; w < kMergeThreads / kWave; ++w) o += sums[w][sub];
   }
-#pragma unroll
-  for (int c = 0; c < T; ++c)
-    a.out[t * a.out_stride + hq * d + kTile * c + lane] = (uint16_t)pack2<BF16>(zero ? 0.f : o[c] / l, 0.f);
+  u32x2 y = {};
+  if (!zero) y = (u32x2){pack2<BF16>(o[0] / l, o[1] / l), pack2<BF16>(o[2] / l, o[3] / l)};
+  *reinterpret_cast<u32x2*>(a.out + t * a.out_stride + hq * d + 4 * sub) = y;
 }
 
 template <int T, bool BF16>
 static hipError_t merge_launch(const PagedAttnArgs& a, const PartOut& part, bool of_few, hipStream_t s) {
   if (part.n_splits <= 1) return hipSuccess;  // (written by its kernel)
   const int64_t rows = a.mixed && of_few ? (int64_t)a.p.B * a.p.H * kFewRows : (int64_t)a.n_q * a.Hq;
-  if (part.n_splits <= kMergeNarrow)
-    hipLaunchKernelGGL((k_paged_merge<T, BF16, 1>), dim3((uint32_t)((rows + kMergeWaves - 1) / kMergeWaves)),
-                       dim3(kMergeWaves * kWave), 0, s, a, part, (int)of_few);
+  constexpr int S = 16 / T;
+  const dim3 streams((uint32_t)((rows + S - 1) / S)), block(kMergeThreads);
+  if (part.n_splits <= kMergeAhead)
+    hipLaunchKernelGGL((k_paged_merge<T, BF16, kMergeAhead, false>), streams, block, 0, s, a, part, (int)of_few);
+  else if (rows >= kMergeWideRows)
+    hipLaunchKernelGGL((k_paged_merge<T, BF16, 16 * T, false>), streams, block, 0, s, a, part, (int)of_few);
   else
-    hipLaunchKernelGGL((k_paged_merge<T, BF16, kMergeWaves>), dim3((uint32_t)rows), dim3(kMergeWaves * kWave), 0, s, a, part,
-                       (int)of_few);
+    hipLaunchKernelGGL((k_paged_merge<T, BF16, kWave, true>), dim3((uint32_t)rows), block, 0, s, a, part, (int)of_few);
   return hipGetLastError();
 }
 
