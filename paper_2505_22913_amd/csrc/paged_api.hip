@@ -178,6 +178,7 @@ int mustafar_paged_attn(const void* q, int64_t q_stride, int n_q, int Hq, const 
   const int64_t tiles = k.few > 0 && !k.mixed ? mf::paged_tiles(a.p, Hq / p->H, n_q, mf::kFewRows)
                                               : mf::paged_tiles(a.p, Hq / p->H, n_q, mf::chunk_rows(p->d / kTile));
   if ((double)tiles * p->H * (k.few > k.many ? k.few : k.many) >= (double)kMaxGroups) return MUSTAFAR_EINVAL;
+  if (k.mixed && (double)p->B * p->H * mf::kFewRows >= (double)kMaxGroups) return MUSTAFAR_EINVAL;  // (k_paged_merge's rows)
   a.few = k.few;
   a.many = k.many;
   a.mixed = k.mixed;

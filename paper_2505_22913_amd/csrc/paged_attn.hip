@@ -109,6 +109,9 @@ __device__ __forceinline__ RowTile row_tile(const PagedAttnArgs& a, int tile, in
   return r;
 }
 
+// The newest token that a window ending at pos leaves out (-1: none; the difference may leave 32 bits).
+__device__ __forceinline__ int before(int pos, int window) { return (int)max((int64_t)pos - window, (int64_t)-1); }
+
 // The tokens that rows at positions [pos0, pos1] see between them, [0, sinks) and [lo, hi], in tiles of BN:
 // tile i of the list starts at token start(i).
 struct TileList {
@@ -117,7 +120,7 @@ struct TileList {
   int n;
   __device__ __forceinline__ TileList(int pos0, int pos1, int window, int n_sinks, int BN) {
     hi = pos1;
-    lo = window > 0 ? max(pos0 - window + 1, 0) : 0;
+    lo = window > 0 ? before(pos0, window) + 1 : 0;
     sinks = min(n_sinks, lo);
     n_first = (sinks + BN - 1) / BN;
     first = lo / BN;
@@ -329,7 +332,7 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
   const int mine = wrow >= rt.rows || pos1 < 0 ? 0 : min(n, max(tl.count_to(pos1, BN) - t0, 0));
 
   // Tiles [clean0, clean1) of the list are seen whole by every row of the wave, [whole0, whole1) by some row of the workgroup.
-  const int clean0 = a.window > 0 ? tl.count_to(pos1 - a.window, BN) - t0 : 0, clean1 = tl.count_to(pos0 - BN + 1, BN) - t0;
+  const int clean0 = a.window > 0 ? tl.count_to(before(pos1, a.window), BN) - t0 : 0, clean1 = tl.count_to(pos0 - BN + 1, BN) - t0;
   const int whole0 = tl.count_to(tl.lo - 1, BN) - t0, whole1 = tl.count_to(tl.hi - BN + 1, BN) - t0;
 
   const int my_row = min(wrow + (int)r32, rt.rows - 1), my_tok = my_row / a.G, pos = rt.base + my_tok;
@@ -675,7 +678,7 @@ __global__ __launch_bounds__(kWave) void k_paged_rows(PagedAttnArgs a, PartOut p
   const int t0 = (int)((int64_t)tl.n * split / part.n_splits);
   const int n = (int)((int64_t)tl.n * (split + 1) / part.n_splits) - t0;
   // Tiles [clean0, clean1) are seen whole by every row, [whole0, whole1) by some.
-  const int clean0 = a.window > 0 ? tl.count_to(pos1 - a.window, BN) - t0 : 0, clean1 = tl.count_to(pos0 - BN + 1, BN) - t0;
+  const int clean0 = a.window > 0 ? tl.count_to(before(pos1, a.window), BN) - t0 : 0, clean1 = tl.count_to(pos0 - BN + 1, BN) - t0;
   const int whole0 = tl.count_to(tl.lo - 1, BN) - t0, whole1 = tl.count_to(tl.hi - BN + 1, BN) - t0;
 
   // Lane i holds the offset in k and v of group i of 16 tokens of the 32 tiles at hand (one that no row sees is replaced by the

@@ -200,6 +200,76 @@ def test_windows_and_sinks(dtype, window, sinks, new):
     attend(dtype, 2, 2, 128, 32, [5, 400, 90, 130], new, window=window, sinks=sinks, seed=window)
 
 
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 40])
+@pytest.mark.parametrize("sinks", [0, 2 ** 31 - 1])
+@pytest.mark.parametrize("new", [[3, 2], [40, 100]])
+def test_a_window_longer_than_anything(window, sinks, new):
+    """Also for rows before a request's first token, whose window begins under -2^31."""
+    cache, ks, vs = fill(2, 2, 128, 16, [2, 70], torch.float16, seed=30)
+    q = torch.randn(sum(new), 4, 128, device="cuda").half()
+    got = mf.mustafar_paged_attn(q, cache, starts(new), window=window, sinks=sinks)
+    check(got, q, ks, vs, new, [2, 70], torch.float16, window, sinks, label="long window")
+
+
+@pytest.mark.parametrize("dtype,d,n_splits", [(torch.float16, 64, 0), (torch.bfloat16, 64, 20), (torch.float16, 128, 3),
+                                              (torch.bfloat16, 128, 20), (torch.float16, 256, 5), (torch.bfloat16, 256, 70)])
+@pytest.mark.parametrize("B", [20, 65, 130])
+def test_many_requests_of_single_tokens_and_a_few_chunks(dtype, d, n_splits, B):
+    """Requests of few rows and of many side by side, every way of joining their ranges."""
+    rng = random.Random(B + n_splits)
+    cached = [rng.choice([0, 1, 30, 64, 200]) for _ in range(B)]
+    new = [1] * B
+    for b, n in ((0, 0), (3, 40), (B - 2, 70), (B - 1, 5)):
+        new[b] = n
+    attend(dtype, 2, 4, d, 16, cached, new, n_splits=n_splits, seed=B)
+    attend(dtype, 2, 4, d, 16, cached, [min(n, 1) for n in new], n_splits=n_splits, seed=B)
+
+
+def test_as_many_requests_as_there_can_be():
+    B = 4096
+    rng = random.Random(1)
+    lens = [rng.choice([0, 1, 2, 5, 17]) for _ in range(B)]
+    new = [min(n, 1) for n in lens]
+    new[1], lens[1] = 33, 40
+    cache, ks, vs = fill(B, 1, 64, 16, lens, torch.float16, seed=31)
+    q = torch.randn(sum(new), 1, 64, device="cuda").half()
+    got = mf.mustafar_paged_attn(q, cache, starts(new), max_q=33)
+    check(got, q, ks, vs, new, lens, torch.float16, label="4096")
+
+
+def test_a_workspace_that_two_captured_calls_share():
+    """Two graphs of calls of different sizes with one workspace, replayed in turns with eager calls between them."""
+    dtype, made = torch.bfloat16, []
+    for i, (cached, new) in enumerate((([3000, 40], [1, 1]), ([900, 100], [60, 1]))):
+        lens = [a + b for a, b in zip(cached, new)]
+        cache, ks, vs = fill(2, 2, 128, 16, lens, dtype, seed=40 + i)
+        made.append((cache, ks, vs, lens, new, torch.randn(sum(new), 8, 128, device="cuda").to(dtype), starts(new)))
+    need = max(mf.mustafar_paged_attn_workspace_bytes(m[0], 8, sum(m[4]), max(m[4]), max(m[3])) for m in made)
+    assert need > 0
+    ws, graphs, outs = torch.empty(need, dtype=torch.uint8, device="cuda"), [], []
+
+    def call(m, out):
+        mf.mustafar_paged_attn(m[5], m[0], m[6], max_q=max(m[4]), max_tokens=max(m[3]), out=out, ws=ws)
+    for m in made:
+        out = torch.zeros_like(m[5])
+        call(m, out)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call(m, out)
+        graphs.append(graph)
+        outs.append(out)
+    for i in (0, 1, 1, 0, 0, 1):
+        outs[i].fill_(9.0)
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        m = made[i]
+        check(outs[i], m[5], m[1], m[2], m[4], m[3], dtype, label=f"graph {i}")
+        again = torch.empty_like(m[5])
+        call(m, again)
+        assert torch.equal(again, outs[i])       # every call's sums are in one order
+
+
 @pytest.mark.parametrize("n_splits", [1, 2, 3, 7, 64])
 @pytest.mark.parametrize("new,window,sinks", [([1, 1, 1], 0, 0), ([40, 1, 200], 0, 0), ([40, 1, 200], 130, 65)])
 def test_splits(n_splits, new, window, sinks):
