@@ -137,8 +137,8 @@ int mustafar_paged_gather(const mustafar_pages_t* p, const void* first, void* x_
   if (n_max < 0) return MUSTAFAR_EINVAL;
   if (n_max == 0) return MUSTAFAR_OK;
   if (!aligned(x_k, 16) || !aligned(x_v, 16) || (first && !aligned(first, 4))) return MUSTAFAR_EINVAL;
-  const double vecs = (double)p->B * p->H * n_max * (p->d / 8);
-  if (vecs / 256 >= (double)kMaxGroups) return MUSTAFAR_EINVAL;
+  const int64_t groups = ((int64_t)n_max * (p->d / 8) + 255) / 256;  // of an entry and kv-head
+  if ((double)p->B * p->H * (double)groups >= (double)kMaxGroups) return MUSTAFAR_EINVAL;
   return status_of(mf::launch_paged_gather(view_of(p), (const int32_t*)first, (uint16_t*)x_k, (uint16_t*)x_v, n_max,
                                            (hipStream_t)stream));
 }

@@ -148,6 +148,24 @@ def test_pages_are_gathered(dtype, layout, H, d, P, lens, first, n_max):
             assert bool((got[b, :, m:] == 7).all())
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_outputs_larger_than_the_caches_are_gathered(dtype):
+    B, H, d, P, n_max = 2, 8, 128, 64, 35001       # 287 MB
+    lens, first = [35100, 20], [98, 0]
+    cache = mf.PagedCache(B, H, d, 560, P, max_pages=552, dtype=dtype)
+    cache.k.normal_()
+    cache.v.normal_()
+    mf.mustafar_paged_plan(cache, ints(lens), sum(lens))
+    x = [torch.full((B, H, n_max, d), 7.0, dtype=torch.float16, device="cuda") for _ in range(2)]
+    mf.mustafar_paged_gather(cache, n_max, first=ints(first), x_k=x[0], x_v=x[1])
+    for got, pool in zip(x, (cache.k, cache.v)):
+        for b, (n, f) in enumerate(zip(lens, first)):
+            m = min(n - f, n_max)
+            pages = cache.table[b, :(n + P - 1) // P].long()
+            want = pool[pages].transpose(0, 1).reshape(H, -1, d)[:, f:f + m].half()
+            assert torch.equal(got[b, :, :m], want) and bool((got[b, :, m:] == 7).all())
+
+
 def test_bf16_values_beyond_fp16_are_gathered_as_its_largest():
     cache, _, _ = fill(1, 1, 64, 16, [16], torch.bfloat16)
     row = torch.tensor([1e5, -1e5, 3e38, float("inf"), -float("inf"), float("nan"), 65504.0, 65280.0, 1e-8, -1e-6] + [0.5] * 54)
