@@ -71,8 +71,9 @@ inline PagedPlan paged_kernels(const PagedView& p, int G, int n_q, int max_q, in
   // few rows: about 2048 waves of at least 64 tokens; many: a workgroup a CU of at least four tiles
   if (all_few || k.mixed) k.few = ranges((int64_t)(p.B < n_q ? p.B : n_q) * p.H, 2048, 64);
   if (!all_few) {
-    const int T = p.d / 64;
-    k.many = ranges(((int64_t)n_q * G + chunk_rows(T) - 1) / chunk_rows(T) * p.H, 256, 256);
+    const int rows = chunk_rows(p.d / 64);
+    auto tiles = [&](int64_t tokens) { return (tokens * G + rows - 1) / rows; };
+    k.many = ranges((k.mixed || p.B == 1 ? tiles(n_q) : p.B * tiles(max_q)) * p.H, 256, 256);
   }
   return k;
 }

@@ -58,16 +58,15 @@ __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
 // ------------------------------------------------------------------------------------------
 // Rows, tokens, tiles.
 // ------------------------------------------------------------------------------------------
-// The rows of a request are its new tokens times the G query heads of a kv-head, so that
-// a kv-head's keys are read once for all of them; a workgroup takes BM consecutive ones. Request b owns
-// workgroups (cu[b] G) / BM + b up to those of request b + 1: as many as its rows need, or one more.
+// The rows of a request are its new tokens times the G query heads of a kv-head, so that a kv-head's keys are read once for all
+// of them; a workgroup takes BM consecutive ones. Every workgroup counts the requests' tiles for itself, so that those without
+// work are the launch's last ones: spread over it, a third of them made 16 requests of 512 rows (256 workgroups for 256 CUs)
+// take two turns, 76 us for 40.
 struct RowTile {
   int b, row0, rows;  // request, first row, rows of the request (row0 >= rows: nothing to do)
   int base;           // position of the request's first new token
   int tok0;           // its row in q
 };
-
-__device__ __forceinline__ int first_tile(int cu, int b, int G, int BM) { return (int)((int64_t)cu * G / BM) + b; }
 
 __device__ __forceinline__ RowTile rows_at(const PagedAttnArgs& a, int b, int cu, int cu_next, int len) {
   RowTile r;
@@ -85,27 +84,52 @@ __device__ __forceinline__ RowTile rows_of(const PagedAttnArgs& a, int b) {
   return rows_at(a, b, __builtin_amdgcn_readfirstlane(cu), __builtin_amdgcn_readfirstlane(next), __builtin_amdgcn_readfirstlane(len));
 }
 
-// The last request b of which first(cu[b], b) <= x, with its rows: up to 64 requests, one round of loads; else two, and its own.
-template <typename F>
-__device__ __forceinline__ RowTile find_rows(const PagedAttnArgs& a, int x, F first) {
+// The request that holds row t of q: of up to 64 requests by one round of loads, else by two and its own.
+__device__ __forceinline__ RowTile request_of(const PagedAttnArgs& a, int t) {
   const int B = a.p.B, lane = (int)lane_id();
   if (B <= kWave) {
     const int b = min(lane, B - 1), cu = a.cu[b], next = a.cu[b + 1], len = a.p.state[b];
-    const int at = 63 - __builtin_clzll(ballot(lane < B && first(cu, b) <= x) | 1);
+    const int at = 63 - __builtin_clzll(ballot(lane < B && cu <= t) | 1);
     return rows_at(a, at, __builtin_amdgcn_readlane(cu, at), __builtin_amdgcn_readlane(next, at), __builtin_amdgcn_readlane(len, at));
   }
   const int stride = (B + kWave - 1) / kWave;
-  int b = min(lane * stride, B - 1);
-  uint64_t below = ballot(lane * stride < B && first(a.cu[b], b) <= x);
-  b = (63 - __builtin_clzll(below | 1)) * stride;
-  const int c = min(b + lane, B - 1);
-  below = ballot(lane < stride && b + lane < B && first(a.cu[c], c) <= x);
+  const int b = (63 - __builtin_clzll(ballot(lane * stride < B && a.cu[min(lane * stride, B - 1)] <= t) | 1)) * stride;
+  const uint64_t below = ballot(lane < stride && b + lane < B && a.cu[min(b + lane, B - 1)] <= t);
   return rows_of(a, __builtin_amdgcn_readfirstlane(b + 63 - (int)__builtin_clzll(below | 1)));
 }
 
-__device__ __forceinline__ RowTile row_tile(const PagedAttnArgs& a, int tile, int BM) {
-  RowTile r = find_rows(a, tile, [&](int cu, int b) { return first_tile(cu, b, a.G, BM); });
-  r.row0 = (tile - first_tile(r.tok0, r.b, a.G, BM)) * BM;
+// Tile `tile` of the launch: all requests' tiles (with `many`: of the requests of more than kFewRows rows) from the last one to the
+// first, so that a request's longest come first. row0 >= rows: there are not so many.
+template <int BM>
+__device__ __forceinline__ RowTile row_tile(const PagedAttnArgs& a, int tile, bool many) {
+  const int B = a.p.B, lane = (int)lane_id(), stride = (B + kWave - 1) / kWave;
+  auto tiles = [&](int b) {
+    const int rows = (min(a.cu[b + 1], a.n_q) - a.cu[b]) * a.G;
+    return rows <= (many ? kFewRows : 0) ? 0u : (uint32_t)(rows + BM - 1) / BM;
+  };
+  // Lane i: the tiles of requests stride * i ..; then the requests of the lane that has the wanted one.
+  uint32_t n = 0;
+  for (int b = lane * stride; b < min((lane + 1) * stride, B); ++b) n += tiles(b);
+  uint32_t incl = wave_incl_scan(n);
+  const uint32_t total = __builtin_amdgcn_readlane(incl, kWave - 1);
+  RowTile r;
+  if ((uint32_t)tile >= total) {
+    r.row0 = r.rows = 0;
+    return r;
+  }
+  uint32_t want = total - 1 - (uint32_t)tile;
+  int at = __builtin_popcountll(ballot(incl <= want));
+  want -= __builtin_amdgcn_readlane(incl - n, at);
+  if (stride > 1) {
+    at *= stride;
+    n = lane < stride && at + lane < B ? tiles(at + lane) : 0u;
+    incl = wave_incl_scan(n);
+    const int x = __builtin_popcountll(ballot(incl <= want));
+    want -= __builtin_amdgcn_readlane(incl - n, x);
+    at += x;
+  }
+  r = rows_of(a, at);
+  r.row0 = (int)want * BM;
   return r;
 }
 
@@ -317,10 +341,9 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
   static_assert(kLoads * kRowsPerLoad == kWaveRows && 16 % kWaveRows == 0, "a wave's rows");
   __shared__ __align__(1024) unsigned char smem[(2 * kRing) * kBuf];  // buffers of keys, of values
   const PagedView& p = a.p;
-  const int h = blockIdx.x % p.H, split = (blockIdx.x / p.H) % part.n_splits;
-  const int tile = (int)(gridDim.x / (p.H * part.n_splits)) - 1 - (int)(blockIdx.x / (p.H * part.n_splits));
-  const RowTile rt = row_tile(a, tile, BM);
-  if (rt.row0 >= rt.rows || (a.mixed && rt.rows <= kFewRows)) return;
+  const int h = blockIdx.x % p.H, split = (blockIdx.x / p.H) % part.n_splits, tile = (int)(blockIdx.x / (p.H * part.n_splits));
+  const RowTile rt = row_tile<BM>(a, tile, a.mixed != 0);
+  if (rt.row0 >= rt.rows) return;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
   const uint32_t lane = lane_id(), r32 = lane % 32, half = lane / 32;
   const int wrow = rt.row0 + 32 * wave;  // the wave's first row
@@ -346,8 +369,14 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
   const uint32_t lane_off = lane_row * row_bytes, piece_k = 16u * (lane % kLanes ^ swizzle_k<T>(lane_row)),
                  piece_v = 16u * (lane % kLanes ^ swizzle_v<T>(lane_row));
   uint32_t at_lo = 0, at_hi = 0;
+  // (the lane once more where the loop seldom comes: not held in a register through it)
+  auto lane_again = [&]() __attribute__((always_inline)) {
+    uint32_t x = lane_id();
+    asm volatile("" : "+v"(x));
+    return x;
+  };
   auto look_up = [&](int first) __attribute__((always_inline)) {
-    int g0 = (tl.start(t0 + min(first + (int)lane, n - 1), BN) + kWaveRows * wave) & ~15;
+    int g0 = (tl.start(t0 + min(first + (int)lane_again(), n - 1), BN) + kWaveRows * wave) & ~15;
     if (g0 >= tl.sinks) g0 = min(max(g0, tl.lo & ~15), tl.hi & ~15);
     int page = p.table[(int64_t)rt.b * p.max_pages + (g0 >> p.log2_page)];
     if ((uint32_t)page >= (uint32_t)p.n_pages) page = 0;
@@ -396,6 +425,7 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
   auto clear_values = [&](int t) __attribute__((always_inline)) {
     if (t >= n || (t >= whole0 && t < whole1)) return;
     const int j0 = tl.start(t0 + t, BN);
+    const uint32_t lane = lane_again(), lane_row = lane / kLanes;
     uint32_t zero_at = lds0 + (uint32_t)(kRing + t % kRing) * kBuf + kWaveRows * wave * kRow + 16 * lane;
 #pragma unroll 1
     for (int i = 0; i < kLoads; ++i, zero_at += kRowsPerLoad * kRow) {
@@ -423,8 +453,9 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
 
   // Operand i of the scores (tokens 32 (i % NK) .., channels 16 (i / NK) ..) and of the outputs (channels 32 (i % ND) .., tokens
   // 16 (i / ND) .., k slot 8 half + i being token 8 (i / 4) + 4 half + i % 4, as the scores lie). A row of LDS is a
-  // multiple of its pieces' places, so that XOR selects the piece.
-  constexpr int kS = NK * NC, kO = 2 * NK * ND, kAhead = 4;
+  // multiple of its pieces' places, so that XOR selects the piece. (kAhead products: 2 and 6 are no faster, and from 4 on
+  // registers spill at d = 128.)
+  constexpr int kS = NK * NC, kO = 2 * NK * ND, kAhead = 3;
   const uint32_t kaddr = lds0 + r32 * kRow + 16u * (half ^ swizzle_k<T>(r32));
   const uint32_t vrow = 4 * half + (lane % 16) / 4;
   const uint32_t vaddr = lds0 + kRing * kBuf + vrow * kRow + 16u * ((((lane / 16) & 1) * 2 + (lane % 4) / 2) ^ swizzle_v<T>(vrow)) + 8 * (lane & 1);
@@ -439,6 +470,7 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
   // it leaves alone (-inf before the first), a row's other lane has the same.
   auto settle = [&](int t, f32x16 (&s)[NK]) __attribute__((always_inline)) {
     if (t < clean0 || t >= clean1) {
+      const uint32_t half = lane_again() / 32;
       const int j0 = tl.start(t0 + t, BN), back = pos - j0 - 4 * (int)half;  // of this lane's first token of the tile
       if (a.window == 0) {
 #pragma unroll
@@ -530,10 +562,12 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
   // The wave's last step.
   auto finish = [&](f32x16 (&s)[NK]) __attribute__((always_inline)) {
     arrive();
-    const uint32_t vat = vaddr + (uint32_t)vr * kBuf;
+    stage_pair();
+    __builtin_amdgcn_sched_barrier(0);
+    uint32_t vat = vaddr + (uint32_t)vr * kBuf;
+    asm volatile("" : "+v"(vat));
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) vf[i] = load_v(vat, i);
-    stage_pair();
 #pragma unroll
     for (int e = 0; e < kPairs; ++e) pair(s, e);
     round_pair(s, kPairs - 1);
@@ -575,9 +609,11 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
 #pragma unroll
       for (int i = 0; i < kS; ++i) {
         s0[i % NK] = mfma32<BF16>(kf[i % kAhead], qb[i / NK], i < NK ? (f32x16){} : s0[i % NK]);
-        kf[i % kAhead] = i + kAhead < kS ? load_k(kaddr, i + kAhead) : load_k(kaddr + kBuf, i + kAhead - kS);
+        if (i + kAhead < kS) kf[i % kAhead] = load_k(kaddr, i + kAhead);
         __builtin_amdgcn_sched_barrier(0);
       }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) kf[i] = load_k(kaddr + kBuf, i);
       top = max_of<NK>(s0);
       settle(0, s0);
       int t = 0;
@@ -600,9 +636,7 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
     wait_loads<0>();
   }
 
-  // (the rows once more from the lane: not held in registers through the loop)
-  uint32_t lane2 = lane_id();
-  asm volatile("" : "+v"(lane2));
+  const uint32_t lane2 = lane_again();
   const int row = wrow + (int)(lane2 % 32), half4 = 4 * (int)(lane2 / 32);
   l += __shfl_xor(l, 32, kWave);
   float z = l * 0.f;  // NaN if something is not finite
@@ -669,7 +703,7 @@ __global__ __launch_bounds__(kWave) void k_paged_rows(PagedAttnArgs a, PartOut p
   constexpr int d = kTile * T, NC = 2 * T, NO = 4 * T, BN = kRowsTile;
   const PagedView& p = a.p;
   const int h = blockIdx.x % p.H, split = (blockIdx.x / p.H) % part.n_splits, tile = blockIdx.x / (p.H * part.n_splits);
-  const RowTile rt = a.mixed ? rows_of(a, tile) : row_tile(a, tile, kFewRows);
+  const RowTile rt = a.mixed ? rows_of(a, tile) : row_tile<kFewRows>(a, tile, false);
   if (rt.row0 >= rt.rows || (a.mixed && rt.rows > kFewRows)) return;
   const uint32_t lane = lane_id(), r16 = lane % 16, q4 = lane / 16;
   const int row = min(rt.row0 + (int)r16, rt.rows - 1), tok = row / a.G, pos = rt.base + tok;
@@ -889,7 +923,7 @@ __global__ __launch_bounds__(kMergeThreads) void k_paged_merge(PagedAttnArgs a, 
 #pragma unroll
       for (int k = 0; k < (WIDE ? 1 : kWave / L); ++k) {
         const int x = __builtin_amdgcn_readlane(t, k * L);
-        const bool few = find_rows(a, x, [](int cu, int) { return cu; }).rows <= kFewRows;
+        const bool few = request_of(a, x).rows <= kFewRows;
         if (x == t && few) mine = false;
       }
     }
