@@ -902,7 +902,8 @@ constexpr int kMergeThreads = 256, kMergeAhead = 8, kMergeWideRows = 512;
 template <int T, bool BF16, int OF, bool WIDE>
 __global__ __launch_bounds__(kMergeThreads) void k_paged_merge(PagedAttnArgs a, PartOut part, int of_few) {
   constexpr int d = kTile * T, L = 16 * T, S = kMergeThreads / L;
-  constexpr int kStep = WIDE ? S : 1;
+  constexpr int kStep = WIDE ? S : 1, kAhead = kMergeAhead < OF / kStep ? kMergeAhead : OF / kStep;
+  static_assert(OF % (kStep * kAhead) == 0, "the ranges under way are of one round of weights");
   const int lane = (int)lane_id(), stream = (int)threadIdx.x / L, sub = (int)threadIdx.x % L;
   const int64_t rows = (int64_t)a.n_q * a.Hq, i0 = WIDE ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * S + stream;
   // The row: of q and all its heads, or, where the requests of few rows have ranges of their own, the r-th of a request's and kv-head's.
@@ -931,10 +932,10 @@ __global__ __launch_bounds__(kMergeThreads) void k_paged_merge(PagedAttnArgs a, 
   if (!mine) return;  // (all of a stream; WIDE: all of the workgroup)
   const int64_t row = (int64_t)t * a.Hq + hq;
   const int first = WIDE ? stream : 0, at = lane % OF;
-  f32x4 x[kMergeAhead], o = {};
+  f32x4 x[kAhead], o = {};
   auto load = [&](int s0) __attribute__((always_inline)) {
 #pragma unroll
-    for (int k = 0; k < kMergeAhead; ++k)
+    for (int k = 0; k < kAhead; ++k)
       if (s0 + kStep * k < part.n_splits) x[k] = *reinterpret_cast<const f32x4*>(part.o + ((s0 + kStep * k) * rows + row) * d + 4 * sub);
   };
   load(first);
@@ -951,9 +952,9 @@ __global__ __launch_bounds__(kMergeThreads) void k_paged_merge(PagedAttnArgs a, 
     if (w != 0.f) l = fmaf(ml.y, w, l);
     nothing |= ballot(ml.y < 0.f);
     const int end = min(s0 + OF, part.n_splits);
-    for (int s = s0; s < end; s += kStep * kMergeAhead) {
+    for (int s = s0; s < end; s += kStep * kAhead) {
 #pragma unroll
-      for (int k = 0; k < kMergeAhead; ++k) {
+      for (int k = 0; k < kAhead; ++k) {
         const int sk = s + first + kStep * k;
         if (OF == kMergeAhead && sk >= end) break;
         const float wk = __shfl(w, (lane & -OF) | ((sk - s0) % OF), kWave);
@@ -961,7 +962,7 @@ __global__ __launch_bounds__(kMergeThreads) void k_paged_merge(PagedAttnArgs a, 
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[e] = fmaf(x[k][e], wk, o[e]);
       }
-      load(s + first + kStep * kMergeAhead);
+      load(s + first + kStep * kAhead);
     }
   }
 #pragma unroll

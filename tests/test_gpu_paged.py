@@ -243,6 +243,15 @@ def test_many_requests_of_single_tokens_and_a_few_chunks(dtype, d, n_splits, B):
     attend(dtype, 2, 4, d, 16, cached, [min(n, 1) for n in new], n_splits=n_splits, seed=B)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("n_splits", [9, 63, 65, 100, 129, 700])
+def test_more_ranges_than_a_wave_has_lanes(dtype, d, n_splits):
+    """Few rows and many (a stream a row and a workgroup a row join them)."""
+    attend(dtype, 1, 2, d, 64, [9000, 40], [1, 1], n_splits=n_splits, seed=n_splits)
+    attend(dtype, 1, 4, d, 64, [5000, 40], [150, 1], n_splits=n_splits, seed=n_splits)
+
+
 def test_as_many_requests_as_there_can_be():
     B = 4096
     rng = random.Random(1)
