@@ -68,8 +68,13 @@ inline PagedPlan paged_kernels(const PagedView& p, int G, int n_q, int max_q, in
     const int64_t n = target / groups, most = max_tokens / least;
     return (int)(n < 1 || most < 1 ? 1 : n < most ? n : most);
   };
-  // few rows: about 2048 waves of at least 64 tokens; many: a workgroup a CU of at least four tiles
-  if (all_few || k.mixed) k.few = ranges((int64_t)(p.B < n_q ? p.B : n_q) * p.H, 2048, 64);
+  // Few rows: waves of at least 64 tokens, one a SIMD (1024). With two a SIMD the long requests of a ragged batch are shared out
+  // better, but a range's output costs as much as 2 tokens a row: 16 requests of 16384 tokens on average take 115 us for 125 with
+  // lengths from nothing to twice that and 4 rows, 167 for 164 with equal lengths; of 16 rows 185 for 168. Rows of d = 256 cost
+  // twice as much (4 of 4 requests of 4096 tokens: 40 for 34).
+  const int64_t rows = (all_few ? max_q : 1) * (int64_t)G;
+  if (all_few || k.mixed) k.few = ranges((int64_t)(p.B < n_q ? p.B : n_q) * p.H, rows <= 4 && p.d < 256 ? 2048 : 1024, 64);
+  // Many: a workgroup a CU of at least 256 tokens.
   if (!all_few) {
     const int rows = chunk_rows(p.d / 64);
     auto tiles = [&](int64_t tokens) { return (tokens * G + rows - 1) / rows; };
