@@ -58,9 +58,10 @@ inline int64_t paged_ws_bytes(const PagedView& p, int Hq, int n_q, int n_splits)
 // up to max_tokens.
 struct PagedPlan {
   int few, many, mixed;
+  int most;  // at least the ranges of this and of every smaller max_tokens
 };
 inline PagedPlan paged_kernels(const PagedView& p, int G, int n_q, int max_q, int64_t max_tokens, int n_splits) {
-  PagedPlan k = {0, 0, 0};
+  PagedPlan k = {0, 0, 0, 0};
   const bool all_few = (int64_t)max_q * G <= kFewRows;
   k.mixed = !all_few && p.B > 1 && n_q < (int64_t)p.B * max_q;  // (else every request has max_q)
   auto ranges = [&](int64_t groups, int64_t target, int64_t least) {
@@ -74,11 +75,17 @@ inline PagedPlan paged_kernels(const PagedView& p, int G, int n_q, int max_q, in
   // twice as much (4 of 4 requests of 4096 tokens: 40 for 34).
   const int64_t rows = (all_few ? max_q : 1) * (int64_t)G;
   if (all_few || k.mixed) k.few = ranges((int64_t)(p.B < n_q ? p.B : n_q) * p.H, rows <= 4 && p.d < 256 ? 2048 : 1024, 64);
-  // Many: a workgroup a CU of at least 256 tokens.
+  k.most = k.few;
+  // Many: a workgroup a CU of at least 256 tokens, where the tokens that a workgroup is spared are worth what k_paged_merge costs:
+  // the launch as much as 200 tokens of a tile of rows, every range of one on a CU as much as 600. 599 tokens and 80 workgroups
+  // take 22 us and 32 in two ranges, 1024 and 128 32 and 39; 1536 and 64 41 and 37 in four, 2304 and 128 62 and 59 in two.
   if (!all_few) {
     const int rows = chunk_rows(p.d / 64);
     auto tiles = [&](int64_t tokens) { return (tokens * G + rows - 1) / rows; };
-    k.many = ranges((k.mixed || p.B == 1 ? tiles(n_q) : p.B * tiles(max_q)) * p.H, 256, 256);
+    const int64_t groups = (k.mixed || p.B == 1 ? tiles(n_q) : p.B * tiles(max_q)) * p.H;
+    k.many = ranges(groups, 256, 256);
+    k.most = k.few > k.many ? k.few : k.many;
+    if (n_splits <= 0 && max_tokens - max_tokens / k.many < 200 + 600 * groups * k.many / 256) k.many = 1;
   }
   return k;
 }
