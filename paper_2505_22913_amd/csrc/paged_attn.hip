@@ -266,10 +266,18 @@ __device__ __forceinline__ void redo_rows(const PagedAttnArgs& a, const PartOut&
 //
 // Step t is X, the products of tile t + 1's scores, then Y, those with tile t's values. Between the products, fenced one by one, lies
 // what the vector units do: the exponentials of tile t in X and the first half of Y, which needs but the first half of the
-// tile, and the maximum of tile t + 1's scores in the second half. (All exponentials in X: its 16 products took 1.8 times as long
-// as Y's.) One barrier a step. Tiles are staged kDepth steps ahead (pair t: the keys of tile t + 1 and the values of
-// tile t) and arrive one step before they are needed, so that the first operands of a step are read before its barrier; they
-// go where the step before has read.
+// tile, and the maximum of tile t + 1's scores in the second half. One barrier a step. Tiles are staged kDepth steps ahead (pair t:
+// the keys of tile t + 1 and the values of tile t) and arrive one step before they are needed, so that the first operands of a
+// step are read before its barrier; they go where the step before has read.
+//
+// The matrix units bound it: of 4 prompts of 4096 tokens with 32 heads at d = 128 (550 GFLOP of visible pairs), 537 to 565 us from
+// one card to the next (1.02 to 0.97 PFLOP/s, where a product of 8192^3 reaches 1.23 to 1.19), they are busy for 50% of the cycles and
+// the vector units for 44%, at 1.9 GHz; LDS has no conflicts. A workgroup alone on its CU (128 KB of LDS) starts
+// and ends in 9 us and takes 1.7 a tile. Tried at that size: 64 rows a wave and one wave a SIMD, 694 us where this took 592; two
+// workgroups of 4 waves a CU and tiles of 32, 586 for 543; a tile's loads all at once, 628 for 602; all exponentials in X, 573
+// for 562; all in Y, the second four waves half a tile late, other wave priorities, 4 and 6 operands ahead: no gain.
+// At d = 256 half the waves fit, and it reaches half the rate (12 requests of 27 tokens with 128 heads over
+// 2315: 178 us, 84 at the rate of d = 128).
 // ------------------------------------------------------------------------------------------
 template <int T>
 constexpr int chunk_tile() { return T == 4 ? 32 : 64; }
@@ -503,18 +511,21 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
     }
   };
   // Probabilities 2 i and 2 i + 1 of a lane, and, when they are there, rounded: the sum is that of the rounded ones.
-  constexpr int kPairs = 8 * NK, kPairsX = kPairs * 11 / 16;
+  constexpr int kPairs = 8 * NK, kPairsX = kPairs * 10 / 16;
+  static_assert(kPairsX > 4, "the first operand of Y is rounded in X");
   u32x4 pb[2 * NK];
   auto round_pair = [&](const f32x16 (&s)[NK], int i) __attribute__((always_inline)) {
-    const uint32_t xy = pack2<BF16>(s[i / 8][2 * (i % 8)], s[i / 8][2 * (i % 8) + 1]);
+    uint32_t xy = pack2<BF16>(s[i / 8][2 * (i % 8)], s[i / 8][2 * (i % 8) + 1]);
     l = add_pair<BF16>(xy, l);
+    asm volatile("" : "+v"(l), "+v"(xy));  // (here, not where it is used: the compiler would move it behind the products)
     pb[i / 4][i % 4] = xy;
   };
   auto pair = [&](f32x16 (&s)[NK], int i) __attribute__((always_inline)) {
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      float x = fmaf(s[i / 8][2 * (i % 8) + e], a.scale_log2, shift);
-      s[i / 8][2 * (i % 8) + e] = __builtin_amdgcn_exp2f(x);
+      float x = __builtin_amdgcn_exp2f(fmaf(s[i / 8][2 * (i % 8) + e], a.scale_log2, shift));
+      asm volatile("" : "+v"(x));
+      s[i / 8][2 * (i % 8) + e] = x;
     }
     if (i > 0) round_pair(s, i - 1);
   };
@@ -554,6 +565,7 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
       } else {
 #pragma unroll
         for (int e = (i - kO / 2) * 4 * kPairs / kO; e < (i - kO / 2 + 1) * 4 * kPairs / kO; ++e) top = fmaxf(top, sn[e / 16][e % 16]);
+        asm volatile("" : "+v"(top));
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -687,6 +699,11 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
 // LDS: a key row's 16-byte pieces are the A operand of S = K Q^T as they are loaded (lane = token l % 16, channels 32 c +
 // 8 (l / 16)), its result (row l % 16, tokens 4 (l / 16) + e of the tile's two groups of 16) is the A operand of O = P V, and a
 // lane loads channels 4 T (l % 16) .. of those eight tokens and transposes them with byte permutes into the B operand.
+//
+// 16 requests of up to 16384 tokens, 8 kv-heads, d = 128 (635 MB): 115 us, 5.5 TB/s, with k_paged_merge's 4.7 (k_paged_chunk: 176); one of
+// 4096 with 32: 18 (25); 32 with a window of 1024, d = 64, 8 rows: 21 (36). Rows beyond 16 would read the pages twice: 16
+// requests of 16 rows over 16384 tokens take 167 us here and 195 there, of 20 rows 194 there. The next tile's loads follow
+// the products that free their registers; twice as many registers, for two tiles: 119 us for 117.
 // ------------------------------------------------------------------------------------------
 constexpr int kRowsTile = 32;
 
