@@ -264,20 +264,20 @@ __device__ __forceinline__ void redo_rows(const PagedAttnArgs& a, const PartOut&
 // so the softmax's shift and sum are per lane (two lanes hold a row's tokens), and its 8-token groups,
 // rounded to the type, are the B operand of O^T = V^T P^T as they lie; V^T comes out of LDS transposed.
 //
-// Step t is X, the products of tile t + 1's scores, then Y, those with tile t's values. Between the products, fenced one by one, lies
-// what the vector units do: the exponentials of tile t in X and the first half of Y, which needs but the first half of the
-// tile, and the maximum of tile t + 1's scores in the second half. One barrier a step. Tiles are staged kDepth steps ahead (pair t:
-// the keys of tile t + 1 and the values of tile t) and arrive one step before they are needed, so that the first operands of a
-// step are read before its barrier; they go where the step before has read.
+// Step t is X, the products of tile t + 1's scores, then the probabilities of tile t, then Y, the products with its values, then
+// the maximum of tile t + 1's scores; the products are fenced one by one, so that the reads of their operands stay ahead of them.
+// One barrier a step. Tiles are staged kDepth steps ahead (pair t: the keys of tile t + 1 and the values of tile t) and arrive one
+// step before they are needed, so that the first operands of a step are read before its barrier; they go where the step
+// before has read.
 //
-// The matrix units bound it: of 4 prompts of 4096 tokens with 32 heads at d = 128 (550 GFLOP of visible pairs), 537 to 565 us from
-// one card to the next (1.02 to 0.97 PFLOP/s, where a product of 8192^3 reaches 1.23 to 1.19), they are busy for 50% of the cycles and
-// the vector units for 44%, at 1.9 GHz; LDS has no conflicts. A workgroup alone on its CU (128 KB of LDS) starts
-// and ends in 9 us and takes 1.7 a tile. Tried at that size: 64 rows a wave and one wave a SIMD, 694 us where this took 592; two
-// workgroups of 4 waves a CU and tiles of 32, 586 for 543; a tile's loads all at once, 628 for 602; all exponentials in X, 573
-// for 562; all in Y, the second four waves half a tile late, other wave priorities, 4 and 6 operands ahead: no gain.
-// At d = 256 half the waves fit, and it reaches half the rate (12 requests of 27 tokens with 128 heads over
-// 2315: 178 us, 84 at the rate of d = 128).
+// The matrix units bound it, at the clock that the card's power leaves them: of 4 prompts of 4096 tokens with 32 heads at d = 128
+// (550 GFLOP of visible pairs), 535 to 560 us from one card to the next (1.03 to 0.98 PFLOP/s, where a product of 8192^3 reaches
+// 1.23 to 1.19), they are busy for half of the cycles and the vector units for 44%, at 1.9 GHz of 2.4; LDS has no conflicts. One
+// prompt of 4096 with 16 heads at d = 256: 155 us, 0.89 PFLOP/s. A workgroup alone on its CU (128 KB of LDS) starts
+// and ends in 9 us and takes 1.7 a tile. Tried at the first size: the probabilities between the products of X and Y, 566 us for 548; Y
+// before X, so that one buffer of scores will do, 573 for 545, with four of the eight waves half a step later 596; 64
+// rows a wave and one wave a SIMD, 694 for 592; two workgroups of 4 waves a CU and tiles of 32, 586 for 543; a tile's loads all at
+// once, 628 for 602; other wave priorities, 4 and 6 operands ahead: no gain.
 // ------------------------------------------------------------------------------------------
 template <int T>
 constexpr int chunk_tile() { return T == 4 ? 32 : 64; }
@@ -454,7 +454,7 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
   };
 
   const float inv_scale = 1.f / a.scale_log2;
-  float l = 0.f, shift = 0.f, top, limit = -INFINITY;
+  float l = 0.f, shift = 0.f, limit = -INFINITY;
   f32x16 o[ND];
 #pragma unroll
   for (int c = 0; c < ND; ++c) o[c] = (f32x16){};
@@ -474,8 +474,8 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
     return (u32x4){lo.x, lo.y, hi.x, hi.y};
   };
 
-  // The scores of a tile, this lane's largest in top, are masked and the shift follows them: limit is the largest score that
-  // it leaves alone (-inf before the first), a row's other lane has the same.
+  // The scores of tile t are masked and the shift follows them: limit is the largest score that it leaves alone (-inf before the
+  // first), a row's other lane has the same.
   auto settle = [&](int t, f32x16 (&s)[NK]) __attribute__((always_inline)) {
     if (t < clean0 || t >= clean1) {
       const uint32_t half = lane_again() / 32;
@@ -494,8 +494,8 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
             if (!sees(pos, j, a.window, a.sinks)) s[n][r] = -INFINITY;
           }
       }
-      top = max_of<NK>(s);
     }
+    float top = max_of<NK>(s);
     if (ballot(top > limit)) {
       top = max_halves(top);
       const bool move = top > limit;
@@ -510,24 +510,22 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
         for (int r = 0; r < 16; ++r) o[c][r] *= alpha;
     }
   };
-  // Probabilities 2 i and 2 i + 1 of a lane, and, when they are there, rounded: the sum is that of the rounded ones.
-  constexpr int kPairs = 8 * NK, kPairsX = kPairs * 10 / 16;
-  static_assert(kPairsX > 4, "the first operand of Y is rounded in X");
+  // A tile's probabilities (in place of the scores), rounded one pair behind: the sum is that of the rounded ones.
   u32x4 pb[2 * NK];
-  auto round_pair = [&](const f32x16 (&s)[NK], int i) __attribute__((always_inline)) {
-    uint32_t xy = pack2<BF16>(s[i / 8][2 * (i % 8)], s[i / 8][2 * (i % 8) + 1]);
-    l = add_pair<BF16>(xy, l);
-    asm volatile("" : "+v"(l), "+v"(xy));  // (here, not where it is used: the compiler would move it behind the products)
-    pb[i / 4][i % 4] = xy;
-  };
-  auto pair = [&](f32x16 (&s)[NK], int i) __attribute__((always_inline)) {
+  auto weights = [&](f32x16 (&s)[NK]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      float x = __builtin_amdgcn_exp2f(fmaf(s[i / 8][2 * (i % 8) + e], a.scale_log2, shift));
-      asm volatile("" : "+v"(x));
-      s[i / 8][2 * (i % 8) + e] = x;
+    for (int i = 0; i <= 8 * NK; ++i) {
+      if (i < 8 * NK)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          s[i / 8][2 * (i % 8) + e] = __builtin_amdgcn_exp2f(fmaf(s[i / 8][2 * (i % 8) + e], a.scale_log2, shift));
+        }
+      if (i == 0) continue;
+      const int k = i - 1;
+      const uint32_t xy = pack2<BF16>(s[k / 8][2 * (k % 8)], s[k / 8][2 * (k % 8) + 1]);
+      l = add_pair<BF16>(xy, l);
+      pb[k / 4][k % 4] = xy;
     }
-    if (i > 0) round_pair(s, i - 1);
   };
   u32x4 qb[NC];  // Q as the B operand: column = row of the wave, k = 16 c + 8 half + i
   u32x4 kf[kAhead], vf[kAhead];
@@ -543,30 +541,19 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
       if (i < 2 * kLoads) stage(i);
       if (i + kAhead < kS) kf[i % kAhead] = load_k(kat, i + kAhead);
       else vf[i + kAhead - kS] = load_v(vat, i + kAhead - kS);
-#pragma unroll
-      for (int e = i * kPairsX / kS; e < (i + 1) * kPairsX / kS; ++e) pair(s, e);
       __builtin_amdgcn_sched_barrier(0);
     }
     next_pair();
+    weights(s);
     kr = kr + 1 == kRing ? 0 : kr + 1;
     vr = vr + 1 == kRing ? 0 : vr + 1;
     uint32_t knext = kaddr + (uint32_t)kr * kBuf;
     asm volatile("" : "+v"(vat), "+v"(knext));
-    top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kO; ++i) {
-      if (i == kO / 2) round_pair(s, kPairs - 1);
       o[i % ND] = mfma32<BF16>(vf[i % kAhead], pb[i / ND], o[i % ND]);
       if (i + kAhead < kO) vf[i % kAhead] = load_v(vat, i + kAhead);
       else kf[i + kAhead - kO] = load_k(knext, i + kAhead - kO);
-      if (i < kO / 2) {
-#pragma unroll
-        for (int e = kPairsX + i * (kPairs - kPairsX) / (kO / 2); e < kPairsX + (i + 1) * (kPairs - kPairsX) / (kO / 2); ++e) pair(s, e);
-      } else {
-#pragma unroll
-        for (int e = (i - kO / 2) * 4 * kPairs / kO; e < (i - kO / 2 + 1) * 4 * kPairs / kO; ++e) top = fmaxf(top, sn[e / 16][e % 16]);
-        asm volatile("" : "+v"(top));
-      }
       __builtin_amdgcn_sched_barrier(0);
     }
     settle(t + 1, sn);
@@ -580,9 +567,7 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
     asm volatile("" : "+v"(vat));
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) vf[i] = load_v(vat, i);
-#pragma unroll
-    for (int e = 0; e < kPairs; ++e) pair(s, e);
-    round_pair(s, kPairs - 1);
+    weights(s);
 #pragma unroll
     for (int i = 0; i < kO; ++i) {
       o[i % ND] = mfma32<BF16>(vf[i % kAhead], pb[i / ND], o[i % ND]);
@@ -626,7 +611,6 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
       }
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) kf[i] = load_k(kaddr + kBuf, i);
-      top = max_of<NK>(s0);
       settle(0, s0);
       int t = 0;
       for (; t + 2 < mine; t += 2) {
