@@ -621,7 +621,8 @@ size_t mustafar_paged_attn_workspace_bytes(const mustafar_pages_t* p, int Hq, in
  *        left as they were
  *   scale  <= 0 selects 1/sqrt(d)
  *   max_q, max_tokens  bounds of an entry's new tokens and of state[b] for the choice
- *        of kernel and split; larger ones give the same result, later
+ *        of kernel and split; wrong ones give the same result, within its roundings,
+ *        later (what a call gives is the same every time)
  *   n_splits  ranges of an entry's visible tokens processed in parallel (<= 0: by the
  *        sizes); ws: mustafar_paged_attn_workspace_bytes, 16-byte aligned
  * Only tokens that a row sees take part: others may hold infinities or NaN, and table

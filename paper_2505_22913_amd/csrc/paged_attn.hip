@@ -1006,8 +1006,8 @@ template <int T, bool BF16>
 static hipError_t attn_launch(const PagedAttnArgs& a, hipStream_t s) {
   const int64_t rows = (int64_t)a.n_q * a.Hq;
   const int most = a.few > a.many ? a.few : a.many;
-  PartOut few = {(float2*)a.ws, nullptr, a.few}, many;
-  few.o = (float*)(few.ml + most * rows);
+  PartOut few = {nullptr, (float*)a.ws, a.few}, many;
+  few.ml = (float2*)(few.o + most * rows * (64 * T));
   many = few;
   many.n_splits = a.many;
   hipError_t e;

@@ -126,3 +126,16 @@ def test_paged_host_code_is_clean_under_asan_and_ubsan(tmp_path):
     exe = str(tmp_path / "paged_harness")
     _run([HIPCC, "-fsanitize=address,undefined", "-fno-gpu-sanitize", *objs, "-o", exe])
     assert "paged harness ok" in _run([exe], env=ENV)
+
+
+def test_a_workspace_does_for_every_shorter_length(lib):
+    """A call's ranges follow what its rows see, its workspace max_tokens: more of these never need less."""
+    for kw in (dict(), dict(B=1), dict(B=64), dict(d=64, page_stride=8 * 64 * 64, head_stride=64 * 64, token_stride=64)):
+        p, st = init(**kw)
+        assert st == mf.OK
+        for Hq, n_q, max_q in ((8, 64, 1), (32, 3, 1), (32, 64, 2), (8, 300, 100), (32, 512, 512), (64, 6000, 2000), (32, 200, 60)):
+            last = 0
+            for tokens in list(range(0, 3000, 97)) + [4096, 10000, 32768, 100000, 1 << 22, 2 ** 31 - 1]:
+                need = lib.mustafar_paged_attn_workspace_bytes(ctypes.byref(p), Hq, n_q, max_q, tokens, 0)
+                assert need >= last, (kw, Hq, n_q, max_q, tokens)
+                last = need
