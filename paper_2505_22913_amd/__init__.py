@@ -659,30 +659,31 @@ class PagedCache:
 
 def _want(name, x, shape, dtype, device, dense=True):
     """Raises unless x is a tensor of this shape, type and device, contiguous if `dense`."""
-    if tuple(x.shape) != tuple(shape) or x.dtype != dtype or (dense and not x.is_contiguous()):
+    if x.shape != shape or x.dtype != dtype or (dense and not x.is_contiguous()):
         raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} expected, "
                          f"not {x.dtype} {tuple(x.shape)}")
     if x.device != device:
         raise ValueError(f"{name} is on {x.device}, the cache on {device}")
 
 
-def _paged_device(cache, *tensors):
-    """The cache's device is the current one (the launches go there) and holds every tensor."""
+def _current(cache):
+    """The cache's device has to be the current one: the launches go there."""
     import torch
     if cache.device.index != torch.cuda.current_device():
         raise ValueError(f"the cache is on {cache.device}, the current device is cuda:{torch.cuda.current_device()}")
-    for x in tensors:
-        if x is not None and x.device != cache.device:
-            raise ValueError(f"a tensor is on {x.device}, the cache on {cache.device}")
 
 
-def _rows(name, x, heads, d, dtype):
-    """Stride of the rows of x [n][heads][d], whose rows are contiguous."""
-    if x.dim() != 3 or tuple(x.shape[1:]) != (heads, d) or x.dtype != dtype:
-        raise ValueError(f"{name}: [n][{heads}][{d}] of {dtype} expected, not {tuple(x.shape)} of {x.dtype}")
-    if x.shape[0] and (x.stride(2) != 1 or (heads > 1 and x.stride(1) != d)):
+def _rows(name, x, n, heads, cache):
+    """Stride of the rows of x [n][heads][d] of the cache's type and device, whose rows are contiguous."""
+    d = cache.desc.d
+    if x.shape != (n, heads, d) or x.dtype != cache.dtype:
+        raise ValueError(f"{name}: [{n}][{heads}][{d}] of {cache.dtype} expected, not {tuple(x.shape)} of {x.dtype}")
+    if x.device != cache.device:
+        raise ValueError(f"{name} is on {x.device}, the cache on {cache.device}")
+    rows, head, channel = x.stride()
+    if n and (channel != 1 or (heads > 1 and head != d)):
         raise ValueError(f"{name}: rows of {heads} x {d} contiguous elements expected")
-    return x.stride(0) if x.shape[0] > 1 else heads * d
+    return rows if n > 1 else heads * d
 
 
 def _on_stream(stream):
@@ -700,7 +701,7 @@ def mustafar_paged_plan(cache: PagedCache, new_len, n_slots: int, keep=None, sta
     bits of a step that was refused and changed nothing."""
     import torch
     B, i32 = cache.desc.B, torch.int32
-    _paged_device(cache, new_len, keep, state_out, cu, slots, status)
+    _current(cache)
     with _on_stream(stream):
         cu = torch.empty(B + 1, dtype=i32, device=cache.device) if cu is None else cu
         slots = torch.empty(n_slots, dtype=i32, device=cache.device) if slots is None else slots
@@ -720,11 +721,9 @@ def mustafar_paged_write(cache: PagedCache, k_new, v_new, slots, stream=None) ->
     """k_new, v_new [n][H][d] (the cache's type; rows of a packed projection too) into their slots
     [n] (int32; negative: left out)."""
     import torch
-    n, H, d = int(k_new.shape[0]), cache.desc.H, cache.desc.d
-    _paged_device(cache, k_new, v_new, slots)
-    ks, vs = _rows("k_new", k_new, H, d, cache.dtype), _rows("v_new", v_new, H, d, cache.dtype)
-    if v_new.shape[0] != n:
-        raise ValueError("as many values as keys")
+    n, H = k_new.shape[0], cache.desc.H
+    _current(cache)
+    ks, vs = _rows("k_new", k_new, n, H, cache), _rows("v_new", v_new, n, H, cache)
     _want("slots", slots, (n,), torch.int32, cache.device)
     _check("mustafar_paged_write", lib().mustafar_paged_write(
         ctypes.byref(cache.desc), _dptr(k_new), ks, _dptr(v_new), vs, _dptr(slots), n, _stream(stream)))
@@ -736,7 +735,7 @@ def mustafar_paged_gather(cache: PagedCache, n_max: int, first=None, x_k=None, x
     tensors that the call makes)."""
     import torch
     shape = (cache.desc.B, cache.desc.H, int(n_max), cache.desc.d)
-    _paged_device(cache, first, x_k, x_v)
+    _current(cache)
     with _on_stream(stream):
         x_k = torch.zeros(shape, dtype=torch.float16, device=cache.device) if x_k is None else x_k
         x_v = torch.zeros(shape, dtype=torch.float16, device=cache.device) if x_v is None else x_v
@@ -763,23 +762,27 @@ def mustafar_paged_attn(q, cache: PagedCache, cu, max_q: int | None = None, max_
     and the first `sinks`. max_q and max_tokens: bounds of a request's rows and length (default: one
     row each if n_q <= B, else n_q; all that a table can hold). Returns out [n_q][Hq][d]."""
     import torch
-    n_q, Hq, d = (int(s) for s in q.shape)
+    if q.dim() != 3:
+        raise ValueError(f"q: [n_q][Hq][{cache.desc.d}] expected, not {tuple(q.shape)}")
+    n_q, Hq, d = q.shape
     B = cache.desc.B
-    _paged_device(cache, q, cu, out, ws)
+    _current(cache)
     max_q = (1 if n_q <= B else n_q) if max_q is None else max_q
     if max_tokens is None:
         max_tokens = min(cache.desc.max_pages, cache.desc.n_pages) * cache.desc.page_tokens
-    qs = _rows("q", q, Hq, cache.desc.d, cache.dtype)
+    qs = _rows("q", q, n_q, Hq, cache)
     _want("cu", cu, (B + 1,), torch.int32, cache.device)
-    need = mustafar_paged_attn_workspace_bytes(cache, Hq, n_q, max_q, max_tokens, n_splits)
-    with _on_stream(stream):
-        if out is None:
+    if ws is None:
+        need = mustafar_paged_attn_workspace_bytes(cache, Hq, n_q, max_q, max_tokens, n_splits)
+        if need > 0:
+            with _on_stream(stream):
+                ws = torch.empty(need, dtype=torch.uint8, device=cache.device)
+    elif ws.device != cache.device or not ws.is_contiguous():
+        raise ValueError(f"ws: contiguous memory on {cache.device} expected")
+    if out is None:
+        with _on_stream(stream):
             out = torch.empty((n_q, Hq, d), dtype=cache.dtype, device=cache.device)
-        if ws is None and need > 0:
-            ws = torch.empty(need, dtype=torch.uint8, device=cache.device)
-    if out.shape[0] != n_q:
-        raise ValueError("as many rows of out as of q")
-    os_ = _rows("out", out, Hq, d, cache.dtype)
+    os_ = _rows("out", out, n_q, Hq, cache)
     _check("mustafar_paged_attn", lib().mustafar_paged_attn(
         _dptr(q), qs, n_q, Hq, ctypes.byref(cache.desc), _dptr(cu), int(window), int(sinks), float(scale), _dptr(out),
         os_, int(max_q), int(max_tokens), int(n_splits), _dptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),

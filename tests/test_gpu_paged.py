@@ -541,3 +541,37 @@ def test_other_streams():
     for outs in results:
         for out, q, m in zip(outs, qs, made):
             check(out, q, m[1], m[2], [100, 30], [700, 300], dtype, label="streams")
+
+
+def test_the_binding_refuses_what_does_not_fit():
+    """Shapes, types, strides and devices are checked before anything is launched."""
+    cache, _, _ = fill(2, 2, 64, 16, [20, 30], torch.float16, seed=50)
+    state = cache.state.clone()
+    x = torch.zeros(3, 2, 64, dtype=torch.float16, device="cuda")
+    q, cu, slots = torch.zeros(2, 4, 64, dtype=torch.float16, device="cuda"), starts([1, 1]), ints([0, 1, 2])
+    plan = lambda **kw: mf.mustafar_paged_plan(**{**dict(cache=cache, new_len=ints([1, 1]), n_slots=2), **kw})  # noqa: E731
+    write = lambda **kw: mf.mustafar_paged_write(**{**dict(cache=cache, k_new=x, v_new=x, slots=slots), **kw})  # noqa: E731
+    attn = lambda **kw: mf.mustafar_paged_attn(**{**dict(q=q, cache=cache, cu=cu), **kw})  # noqa: E731
+    gather = lambda **kw: mf.mustafar_paged_gather(**{**dict(cache=cache, n_max=4), **kw})  # noqa: E731
+    bad = [(plan, dict(new_len=ints([1]))), (plan, dict(new_len=ints([1, 1]).cpu())), (plan, dict(new_len=ints([1, 1]).long())),
+           (plan, dict(keep=ints([1, 1, 1]))), (plan, dict(state_out=ints([0, 0]))), (plan, dict(slots=ints([0]))),
+           (write, dict(k_new=x.float())), (write, dict(v_new=x[:2])), (write, dict(k_new=x.cpu())), (write, dict(k_new=x[:, :1])),
+           (write, dict(k_new=x.transpose(0, 1).contiguous().transpose(0, 1))), (write, dict(slots=slots[:2])),
+           (write, dict(slots=slots.long())), (attn, dict(q=q.bfloat16())), (attn, dict(q=q[0])), (attn, dict(q=q[..., :32])),
+           (attn, dict(q=q.cpu())), (attn, dict(cu=cu[:2])), (attn, dict(cu=cu.long())), (attn, dict(out=q[:1])),
+           (attn, dict(out=q.float())), (attn, dict(out=q.cpu())), (attn, dict(ws=torch.zeros(1 << 20))),
+           (gather, dict(first=ints([0]))), (gather, dict(x_k=x)), (gather, dict(x_k=torch.zeros(2, 2, 4, 64, device="cuda")))]
+    for call, kw in bad:
+        with pytest.raises(ValueError):
+            call(**kw)
+    for call, kw in ((attn, dict(q=torch.zeros(2, 3, 64, dtype=torch.float16, device="cuda"))), (attn, dict(window=-1)),
+                     (attn, dict(n_splits=4, ws=torch.zeros(16, dtype=torch.uint8, device="cuda"))),
+                     (attn, dict(q=torch.zeros(2, 130, 64, dtype=torch.float16, device="cuda"))), (plan, dict(n_slots=-1, slots=ints([])))):
+        with pytest.raises((mf.MustafarError, ValueError)):
+            call(**kw)
+    assert torch.equal(cache.state, state)
+    for call, kw in ((attn, dict(q=q[:0], cu=starts([0, 0]))), (write, dict(k_new=x[:0], v_new=x[:0], slots=slots[:0])),
+                     (plan, dict(new_len=ints([0, 0]), n_slots=0)), (gather, dict(n_max=0))):
+        call(**kw)                                                                     # nothing to do
+    torch.cuda.synchronize()
+    assert torch.equal(cache.state, state)
