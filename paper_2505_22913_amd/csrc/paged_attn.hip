@@ -684,10 +684,10 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
 // 8 (l / 16)), its result (row l % 16, tokens 4 (l / 16) + e of the tile's two groups of 16) is the A operand of O = P V, and a
 // lane loads channels 4 T (l % 16) .. of those eight tokens and transposes them with byte permutes into the B operand.
 //
-// 16 requests of up to 16384 tokens, 8 kv-heads, d = 128 (635 MB): 115 us, 5.5 TB/s, with k_paged_merge's 4.7 (k_paged_chunk: 176); one of
-// 4096 with 32: 18 (25); 32 with a window of 1024, d = 64, 8 rows: 21 (36). Rows beyond 16 would read the pages twice: 16
-// requests of 16 rows over 16384 tokens take 167 us here and 195 there, of 20 rows 194 there. The next tile's loads follow
-// the products that free their registers; twice as many registers, for two tiles: 119 us for 117.
+// With k_paged_merge, and in parentheses k_paged_chunk instead: 16 requests of up to 16384 tokens, 8 kv-heads of 4 rows, d = 128 (634
+// MB) 115 us, 5.5 TB/s (152); one of 4096 with 32 heads 18 (20.5); 32 with a window of 1024, d = 64, 8 rows 21 (21); of 16
+// rows, 16 requests of 16384 tokens 165 (194), one 23 (22), 32 of 1024 32 (28). Rows beyond 16 would read the pages twice. The next
+// tile's loads follow the products that free their registers; with as many registers again, for two tiles: 119 us for 117.
 // ------------------------------------------------------------------------------------------
 constexpr int kRowsTile = 32;
 
