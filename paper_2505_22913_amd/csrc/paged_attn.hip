@@ -301,13 +301,13 @@ __device__ __forceinline__ uint32_t swizzle_v(uint32_t row) {
 
 // 16 bytes a lane from base + offset to LDS at dst + 16 lane; wait_loads() waits for them. (Inline: behind the builtin the
 // compiler waits for every such load before the next transposing LDS read of any address. The load has no register
-// output; m0, its LDS address, is put back.)
+// output; m0, its LDS address, is put back. Five cycles lie between a base that the vector units wrote and its use.)
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t dst) {
   const uint64_t at = (uint64_t)base;  // (uniform; said so, whatever the compiler makes of how it came about)
   const uint64_t sbase = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32)) << 32 |
                          (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at);
   uint32_t m0;
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 2\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
                : "=&s"(m0) : "s"(__builtin_amdgcn_readfirstlane((int)dst)), "v"(offset), "s"(sbase) : "memory");
 }
 template <int LEFT>
