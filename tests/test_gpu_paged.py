@@ -264,6 +264,23 @@ def test_as_many_requests_as_there_can_be():
     check(got, q, ks, vs, new, lens, torch.float16, label="4096")
 
 
+@pytest.mark.parametrize("n_splits", [0, 5, 12, 70])
+@pytest.mark.parametrize("new", [[1, 1, 1], [90, 1, 3], [40, 70, 33]])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_what_a_workspace_held_takes_no_part(d, new, n_splits):
+    """A workspace of NaN: ranges without tokens, requests shorter than there are ranges, rows that see nothing."""
+    cached = [3000, 2, 500]
+    lens = [a + b for a, b in zip(cached, new)]
+    cache, ks, vs = fill(3, 2, d, 16, lens, torch.float16, seed=60)
+    cache.state[1] = 1              # fewer tokens than rows, where there is more than one
+    lens[1], ks[1], vs[1] = 1, ks[1][:, :1], vs[1][:, :1]
+    q = torch.randn(sum(new), 8, d, device="cuda").half()
+    need = mf.mustafar_paged_attn_workspace_bytes(cache, 8, sum(new), max(new), 4000, n_splits)
+    ws = torch.full((max(need, 16),), 255, dtype=torch.uint8, device="cuda")
+    got = mf.mustafar_paged_attn(q, cache, starts(new), max_q=max(new), max_tokens=4000, n_splits=n_splits, ws=ws)
+    check(got, q, ks, vs, new, lens, torch.float16, label="workspace of NaN")
+
+
 def test_a_workspace_that_two_captured_calls_share():
     """Two graphs of calls of different sizes with one workspace, replayed in turns with eager calls between them."""
     dtype, made = torch.bfloat16, []
