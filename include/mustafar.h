@@ -627,10 +627,12 @@ size_t mustafar_paged_attn_workspace_bytes(const mustafar_pages_t* p, int Hq, in
  *        sizes); ws: mustafar_paged_attn_workspace_bytes, 16-byte aligned
  * Only tokens that a row sees take part: others may hold infinities or NaN, and table
  * entries of pages that no row sees need not be valid. (An entry outside [0, n_pages)
- * is read as page 0, and a length as at most max_pages * P.) Probabilities are
- * rounded to the cache's type for the product with the values, the softmax's maximum,
- * sum and output are held in fp32. Errors: EINVAL, EUNSUPPORTED (Hq/H over
- * MUSTAFAR_PAGED_MAX_GROUP), EWORKSPACE. */
+ * is read as page 0, and a length as at most max_pages * P.) For the product with the
+ * values a probability is the sum of two numbers of the cache's type where the call's
+ * requests have at most 16 rows a kv-head (their tokens times Hq/H: single tokens), and
+ * rounded to the type where they have more; the softmax's maximum, sum and output are
+ * held in fp32. Errors: EINVAL, EUNSUPPORTED (Hq/H over MUSTAFAR_PAGED_MAX_GROUP),
+ * EWORKSPACE. */
 int mustafar_paged_attn(const void* q, int64_t q_stride, int n_q, int Hq, const mustafar_pages_t* p,
                         const void* cu, int window, int sinks, float scale, void* out,
                         int64_t out_stride, int max_q, int max_tokens, int n_splits, void* ws,

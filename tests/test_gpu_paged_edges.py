@@ -1,0 +1,78 @@
+"""Paged attention's weights, ranges and page look-ups where they can go wrong, with inputs whose scores
+are exact in fp32: what is left of a weight's error is its exponential's and its roundings'."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+import paper_2505_22913_amd as mf
+from tests.gpu_common import announce
+from tests.paged_common import fill, starts
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = [torch.float16, torch.bfloat16]
+
+
+def half_step(x, dtype):
+    """Half the distance of the type's numbers at |x| (float64)."""
+    eps = torch.finfo(dtype).eps
+    least = torch.finfo(dtype).tiny
+    return torch.exp2(torch.floor(torch.log2(x.abs().clamp(min=least)))) * eps / 2
+
+
+def exact_scores(q, k, scale):
+    """The scores of q [n][Hq][d] and k [H][L][d] whose entries are small whole numbers, float64 [Hq][n][L]."""
+    G = q.shape[1] // k.shape[0]
+    return q.double().transpose(0, 1) @ k.double().repeat_interleave(G, 0).transpose(1, 2) * scale
+
+
+def softmax_of(score, v, sees):
+    """Output and the weights' mean of |v|, float64 [n][Hq][d]."""
+    G = score.shape[0] // v.shape[0]
+    p = torch.softmax(score.masked_fill(~sees, -torch.inf), -1)
+    v = v.double().repeat_interleave(G, 0)
+    return (p @ v).transpose(0, 1), (p @ v.abs()).transpose(0, 1)
+
+
+def causal(n, L, device):
+    return torch.arange(L, device=device)[None] <= torch.arange(L - n, L, device=device)[:, None]
+
+
+# ---- the weights' precision ----------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("H,G", [(4, 1), (2, 4), (1, 16)])
+@pytest.mark.parametrize("n_splits", [1, 5])
+def test_single_tokens_weights_are_not_rounded_to_the_type(dtype, d, H, G, n_splits):
+    """Tokens whose output is off by no more than its own rounding and what 2 parts of the type leave of the weights.
+
+    q and k are whole numbers up to 3, so every score is exact in fp32. A weight 2^x, x up to 60 in magnitude, is off by
+    ln 2 (2^-18 + 60 2^-24) from x's last rounding and the scale's, 2^-22 from the exponential, and from its two parts by u^2
+    (u = half a step of the type; of fp16 also 2^-25 where the reference's is 2^7). The sums over the tokens add (n + 32) 2^-24, and the
+    normalised weights are off by twice all that."""
+    L, n = 700, 1
+    scale = 2.0 ** -5
+    announce(f"weights {dtype} d={d} H={H} G={G} splits={n_splits}")
+    cache, ks, vs = fill(3, H, d, 16, [L, 33, 1], dtype, seed=d + G)
+    g = torch.Generator().manual_seed(d)
+    for b, m in enumerate((L, 33, 1)):
+        ks[b] = torch.randint(-3, 4, (H, m, d), generator=g).to(dtype)
+        for i in range((m + 15) // 16):
+            at = ks[b][:, 16 * i:16 * i + 16]
+            cache.k[int(cache.table[b, i]), :, :at.shape[1]] = at.cuda()
+    q = torch.randint(-3, 4, (3, H * G, d), generator=g).to(dtype)
+    got = mf.mustafar_paged_attn(q.cuda(), cache, starts([1, 1, 1]), scale=scale, n_splits=n_splits).double().cpu()
+    u = torch.finfo(dtype).eps / 2
+    for b, m in enumerate((L, 33, 1)):
+        score = exact_scores(q[b:b + 1], ks[b], scale)
+        assert float(score.abs().max()) < 40 * 0.69
+        want, mean = softmax_of(score, vs[b], causal(n, m, "cpu"))
+        rel = 0.6932 * (2.0 ** -18 + 60 * 2.0 ** -24) + 2.0 ** -22 + u * u + (m + 32) * 2.0 ** -24
+        least = m * 2.0 ** -32 * float(vs[b].abs().max()) if dtype == torch.float16 else 0.0
+        tol = half_step(want, dtype) + 2 * rel * mean * (1 + u) + 2 * least
+        err = (got[b:b + 1] - want).abs()
+        worst = float((err / tol).max())
+        over = float(((err - half_step(want, dtype)) / (mean * u)).max())
+        announce(f"  request {b}: {worst:.2f} of its bound; beyond the output's rounding {over:.4f} u mean |v|")
+        assert worst <= 1, f"request {b}: an element is {worst:.2f} of its bound off"
