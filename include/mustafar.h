@@ -555,7 +555,9 @@ int mustafar_paged_init(mustafar_pages_t* p, void* k, void* v, void* table, void
 #define MUSTAFAR_PLAN_PAGES 1  /* too few free pages                                  */
 #define MUSTAFAR_PLAN_TABLE 2  /* an entry would need more than max_pages pages       */
 #define MUSTAFAR_PLAN_SLOTS 4  /* more than n_slots new tokens                        */
-#define MUSTAFAR_PLAN_STATE 8  /* a negative new_len, or a state that is none         */
+#define MUSTAFAR_PLAN_STATE 8  /* a negative new_len, or a state that is none: a length
+                                * that is negative or longer than a table, or more free
+                                * pages and pages of entries than n_pages             */
 
 /* One step's block tables, slots and sequence starts from the entries' lengths.
  * Entry b holds len = p->state[b] tokens in ceil(len / P) pages; the step keeps the

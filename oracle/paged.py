@@ -30,7 +30,7 @@ class PagePlan:
         lens = [k + a for k, a in zip(kept, new)]
         pages = [(n + P - 1) // P for n in lens]
         status = 0
-        if any(a < 0 for a in new):
+        if any(a < 0 for a in new) or sum(len(t) for t in self.tables) + len(self.stack) > self.n_pages:
             status |= 8
         if any(a >= 0 and n > self.max_pages for a, n in zip(new, pages)):
             status |= 2

@@ -604,7 +604,8 @@ class PagedCache:
     (the requests' lengths, the free pages, a word of the library's) and free [n_pages] (the
     stack of free pages), int32. Tensors that are given are used as they are (k and v in any
     order of pages, heads and tokens whose channels are contiguous); the others are made, for an
-    empty cache. max_pages: pages of the longest request (default: all).
+    empty cache: a state that holds tokens comes with its table and its stack. max_pages: pages of the
+    longest request (default: all).
     """
 
     def __init__(self, B: int, H: int, d: int, n_pages: int, page_tokens: int = 64, max_pages: int | None = None,

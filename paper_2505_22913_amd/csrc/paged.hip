@@ -80,7 +80,7 @@ __device__ __forceinline__ int plan_find(const uint32_t* at, int B, uint32_t i) 
 
 __global__ __launch_bounds__(kPlanThreads) void k_paged_plan(PlanArgs a) {
   extern __shared__ uint32_t sm[];  // cu, taken, given: [B + 1] each
-  __shared__ uint32_t wsum[3][kPlanThreads / kWave];
+  __shared__ uint32_t wsum[4][kPlanThreads / kWave];
   __shared__ int wbits[kPlanThreads / kWave];
   __shared__ int last;
   uint32_t* cu = sm;
@@ -90,20 +90,21 @@ __global__ __launch_bounds__(kPlanThreads) void k_paged_plan(PlanArgs a) {
   const int per = (a.B + kPlanThreads - 1) / kPlanThreads;
   const int n_free = a.state[a.B];
 
-  uint32_t sum[3] = {0u, 0u, 0u};
+  uint32_t sum[4] = {0u, 0u, 0u, 0u};  // new tokens, pages taken, given up, held
   int wrong = n_free < 0 || n_free > a.n_pages ? kPlanState : 0;
   for (int b = t * per; b < min(a.B, (t + 1) * per); ++b) {
     const PlanEntry e = plan_entry(a, b);
     const int w = plan_wrong(a, e);
     wrong |= w;
+    if (!(w & kPlanState)) sum[3] += (uint32_t)e.ob;
     if (w) continue;
     sum[0] += (uint32_t)e.add;
     sum[1] += (uint32_t)max(e.nb - e.ob, 0);
     sum[2] += (uint32_t)max(e.ob - e.nb, 0);
   }
-  uint32_t base[3];
+  uint32_t base[4];
 #pragma unroll
-  for (int k = 0; k < 3; ++k) {
+  for (int k = 0; k < 4; ++k) {
     const uint32_t incl = wave_incl_scan(sum[k]);
     if (t % kWave == kWave - 1) wsum[k][wave] = incl;
     base[k] = incl - sum[k];
@@ -114,16 +115,18 @@ __global__ __launch_bounds__(kPlanThreads) void k_paged_plan(PlanArgs a) {
     if (ballot((wrong & bit) != 0)) bits |= bit;
   if (t % kWave == 0) wbits[wave] = bits;
   __syncthreads();
-  uint32_t total[3] = {0u, 0u, 0u};
+  uint32_t total[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
   for (int w = 0; w < kPlanThreads / kWave; ++w) {
     bits |= wbits[w];
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
+    for (int k = 0; k < 4; ++k) {
       if (w < wave) base[k] += wsum[k][w];
       total[k] += wsum[k][w];
     }
   }
+  // (no page is held twice, so that the pages given up have room on the stack)
+  if ((int64_t)total[3] + n_free > a.n_pages) bits |= kPlanState;
   if (!bits) {
     if (total[0] > (uint32_t)a.n_slots) bits |= kPlanSlots;
     if (total[1] > total[2] && total[1] - total[2] > (uint32_t)n_free) bits |= kPlanPages;

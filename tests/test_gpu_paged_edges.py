@@ -6,6 +6,7 @@ import pytest
 import torch
 
 import paper_2505_22913_amd as mf
+from oracle.paged import PagePlan, Refused
 from tests.gpu_common import announce
 from tests.paged_common import fill, starts
 
@@ -76,3 +77,32 @@ def test_single_tokens_weights_are_not_rounded_to_the_type(dtype, d, H, G, n_spl
         over = float(((err - half_step(want, dtype)) / (mean * u)).max())
         announce(f"  request {b}: {worst:.2f} of its bound; beyond the output's rounding {over:.4f} u mean |v|")
         assert worst <= 1, f"request {b}: an element is {worst:.2f} of its bound off"
+
+
+# ---- plans ---------------------------------------------------------------------------------------
+@pytest.mark.parametrize("n_slots", [4, 5000])
+@pytest.mark.parametrize("lens,n_free,keep,new", [
+    ([64, 30], 30, [0, 0], [0, 0]),             # every page is on the stack and six of them are in tables: nothing may go on it
+    ([64, 30], 25, [0, 30], [0, 1]),            # one page too many
+    ([64, 30], 30, None, [1, 1]),               # nothing is given up, but what is taken is held already
+    ([480, 16], 0, [0, 0], [1, 1]),
+])
+def test_a_plan_of_more_pages_than_there_are_is_refused(lens, n_free, keep, new, n_slots):
+    """A state whose tables and stack hold more pages than the pool has: the stack has no room for those given up."""
+    n_pages, guard = 30, 64
+    free = torch.full((n_pages + guard,), -7, dtype=torch.int32, device="cuda")
+    free[:n_pages] = torch.arange(n_pages - 1, -1, -1, device="cuda")
+    cache = mf.PagedCache(2, 1, 64, n_pages, 16, max_pages=40, free=free[:n_pages],
+                          state=torch.tensor(lens + [n_free, 0], dtype=torch.int32, device="cuda"))
+    before = [x.clone() for x in (free, cache.table, cache.state)]
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    status = ints([0])
+    cu, slots = mf.mustafar_paged_plan(cache, ints(new), n_slots, keep=None if keep is None else ints(keep), status=status)
+    assert status.tolist() == [mf.PLAN_STATE] and cu.tolist() == [0, 0, 0] and bool((slots == -1).all())
+    for x, y in zip(before, (free, cache.table, cache.state)):
+        assert torch.equal(x, y)
+    plan = PagePlan(2, 16, n_pages, 40)
+    plan.lens, plan.tables, plan.stack = lens, [list(range((n + 15) // 16)) for n in lens], list(range(n_free))
+    with pytest.raises(Refused) as e:
+        plan.step(new, keep, n_slots)
+    assert e.value.args == (mf.PLAN_STATE,)
