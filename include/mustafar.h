@@ -603,7 +603,11 @@ int mustafar_paged_gather(const mustafar_pages_t* p, const void* first, void* x_
                           int n_max, void* stream);
 
 /* Device workspace of mustafar_paged_attn for these sizes (0: none needed). n_splits
- * <= 0 sizes for the split that such a call takes. 0 for invalid arguments. */
+ * <= 0 sizes for the split that such a call takes: never more than 393216 * (d + 2)
+ * bytes (51 MB at d = 128), whatever the sizes, and never less for more max_tokens. A
+ * smaller n_q or max_q may need more (its ranges are more): a workspace for steps of
+ * several sizes has the most that one of them needs, or that bound. 0 for invalid
+ * arguments. */
 size_t mustafar_paged_attn_workspace_bytes(const mustafar_pages_t* p, int Hq, int n_q, int max_q,
                                            int max_tokens, int n_splits);
 

@@ -38,6 +38,9 @@ struct PagedAttnArgs {
   // Ranges of a request's visible tokens in k_paged_rows and in k_paged_chunk, 0 where that kernel is not run; mixed: the first
   // has the requests of at most kFewRows rows, the second the others, else the one that runs has all.
   int few, many, mixed;
+  // Rows of a range's results in k_paged_rows: of q and all its heads, or, by_entry, kFewRows of every entry and kv-head.
+  int64_t few_rows;
+  int by_entry;
   void* ws;  // the ranges' results where there are several
 };
 
@@ -49,21 +52,30 @@ constexpr int chunk_rows(int T) { return 32 * chunk_waves(T); }
 // Workgroups of so many rows that hold n_q tokens of B requests however they are divided.
 inline int64_t paged_tiles(const PagedView& p, int G, int n_q, int rows) { return (int64_t)n_q * G / rows + p.B; }
 
-// Bytes of the ranges' results: two numbers and d fp32 values of every row and query head.
-inline int64_t paged_ws_bytes(const PagedView& p, int Hq, int n_q, int n_splits) {
-  return n_splits <= 1 ? 0 : (int64_t)n_splits * n_q * Hq * (p.d + 2) * 4;
-}
-
 // Which kernels a call takes, and the ranges that it takes by itself (n_splits <= 0) for requests of up to max_q tokens that see
 // up to max_tokens.
 struct PagedPlan {
   int few, many, mixed;
-  int most;  // at least the ranges of this and of every smaller max_tokens
+  int most_many;  // at least the ranges `many` of this and of every smaller max_tokens (`few` are that themselves)
+  int64_t few_rows;
+  int by_entry;
 };
+
+// Results of the ranges of both kernels: two numbers and d fp32 values of every row. By themselves calls take at most 16 * 2048 and
+// 256 * 256 such rows (ranges times rows; the launch's waves and workgroups times theirs), whatever the batch.
+inline int64_t paged_parts(int64_t rows, int ranges) { return ranges > 1 ? rows * ranges : 0; }
+inline int64_t paged_ws_bytes(const PagedView& p, int64_t rows, const PagedPlan& k) {
+  return (paged_parts(k.few_rows, k.few) + paged_parts(rows, k.most_many)) * (p.d + 2) * 4;
+}
+
 inline PagedPlan paged_kernels(const PagedView& p, int G, int n_q, int max_q, int64_t max_tokens, int n_splits) {
-  PagedPlan k = {0, 0, 0, 0};
+  PagedPlan k = {0, 0, 0, 0, 0, 0};
   const bool all_few = (int64_t)max_q * G <= kFewRows;
-  k.mixed = !all_few && p.B > 1 && n_q < (int64_t)p.B * max_q;  // (else every request has max_q)
+  const bool uneven = p.B > 1 && n_q < (int64_t)p.B * max_q;  // (else every request has max_q)
+  k.mixed = !all_few && uneven && G <= kFewRows;
+  const int64_t q_rows = (int64_t)n_q * G * p.H, entry_rows = (int64_t)p.B * p.H * kFewRows;
+  k.by_entry = k.mixed && entry_rows < q_rows;
+  k.few_rows = k.by_entry ? entry_rows : q_rows;
   auto ranges = [&](int64_t groups, int64_t target, int64_t least) {
     if (n_splits > 0) return n_splits;
     const int64_t n = target / groups, most = max_tokens / least;
@@ -74,17 +86,19 @@ inline PagedPlan paged_kernels(const PagedView& p, int G, int n_q, int max_q, in
   // lengths from nothing to twice that and 4 rows, 167 for 164 with equal lengths; of 16 rows 185 for 168. Rows of d = 256 cost
   // twice as much (4 of 4 requests of 4096 tokens: 40 for 34).
   const int64_t rows = (all_few ? max_q : 1) * (int64_t)G;
-  if (all_few || k.mixed) k.few = ranges((int64_t)(p.B < n_q ? p.B : n_q) * p.H, rows <= 4 && p.d < 256 ? 2048 : 1024, 64);
-  k.most = k.few;
+  auto tiles = [&](int64_t tokens, int rows) { return (tokens * G + rows - 1) / rows; };
+  if (all_few || k.mixed) {
+    const int64_t requests = p.B < n_q ? p.B : n_q, full = all_few ? tiles(n_q, kFewRows) : 0;  // (more than the requests if max_q is too small)
+    k.few = ranges((requests > full ? requests : full) * p.H, rows <= 4 && p.d < 256 ? 2048 : 1024, 64);
+  }
   // Many: a workgroup a CU of at least 256 tokens, where the tokens that a workgroup is spared are worth what k_paged_merge costs:
   // the launch as much as 200 tokens of a tile of rows, every range of one on a CU as much as 600. 599 tokens and 80 workgroups
   // take 22 us and 32 in two ranges, 1024 and 128 32 and 39; 1536 and 64 41 and 37 in four, 2304 and 128 62 and 59 in two.
   if (!all_few) {
     const int rows = chunk_rows(p.d / 64);
-    auto tiles = [&](int64_t tokens) { return (tokens * G + rows - 1) / rows; };
-    const int64_t groups = (k.mixed || p.B == 1 ? tiles(n_q) : p.B * tiles(max_q)) * p.H;
-    k.many = ranges(groups, 256, 256);
-    k.most = k.few > k.many ? k.few : k.many;
+    const int64_t full = tiles(n_q, rows), even = uneven || p.B == 1 ? 0 : p.B * tiles(max_q, rows);
+    const int64_t groups = (even > full ? even : full) * p.H;
+    k.many = k.most_many = ranges(groups, 256, 256);
     if (n_splits <= 0 && max_tokens - max_tokens / k.many < 200 + 600 * groups * k.many / 256) k.many = 1;
   }
   return k;

@@ -149,7 +149,7 @@ size_t mustafar_paged_attn_workspace_bytes(const mustafar_pages_t* p, int Hq, in
   if (n_q < 1 || max_q < 0 || max_tokens < 0 || n_splits > kMaxSplits || (int64_t)n_q * Hq >= kMaxGroups) return 0;
   const mf::PagedView v = view_of(p);
   const mf::PagedPlan k = mf::paged_kernels(v, Hq / p->H, n_q, max_q, max_tokens, n_splits);
-  return (size_t)mf::paged_ws_bytes(v, Hq, n_q, k.most);
+  return (size_t)mf::paged_ws_bytes(v, (int64_t)n_q * Hq, k);
 }
 
 int mustafar_paged_attn(const void* q, int64_t q_stride, int n_q, int Hq, const mustafar_pages_t* p, const void* cu,
@@ -182,6 +182,8 @@ int mustafar_paged_attn(const void* q, int64_t q_stride, int n_q, int Hq, const 
   a.few = k.few;
   a.many = k.many;
   a.mixed = k.mixed;
+  a.few_rows = k.few_rows;
+  a.by_entry = k.by_entry;
   a.ws = ws;
   a.q = (const uint16_t*)q;
   a.out = (uint16_t*)out;

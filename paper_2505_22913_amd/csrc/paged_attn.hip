@@ -233,10 +233,19 @@ __device__ __forceinline__ RowState<T> one_row(const PagedAttnArgs& a, int b, in
 // (-inf if it has none), their sum (-1 for a row that sees nothing at all) and the weighted values.
 // ------------------------------------------------------------------------------------------
 struct PartOut {
-  float2* ml;  // [n_splits][n_q * Hq]
-  float* o;    // [n_splits][n_q * Hq][d]
+  float2* ml;  // [n_splits][rows]
+  float* o;    // [n_splits][rows][d]
+  int64_t rows;
+  int by_entry;
   int n_splits;
 };
+
+// Row r of a request and kv-head among a range's.
+__device__ __forceinline__ int64_t part_row(const PagedAttnArgs& a, const PartOut& part, const RowTile& rt, int h, int r) {
+  if (part.by_entry) return ((int64_t)rt.b * a.p.H + h) * kFewRows + r;
+  const int tok = r / a.G;
+  return (int64_t)(rt.tok0 + tok) * a.Hq + h * a.G + r - tok * a.G;
+}
 
 template <int T, bool BF16>
 __device__ __forceinline__ void redo_rows(const PagedAttnArgs& a, const PartOut& part, const RowTile& rt, int h, int first_row,
@@ -247,7 +256,7 @@ __device__ __forceinline__ void redo_rows(const PagedAttnArgs& a, const PartOut&
     const int tok = r / a.G, hq = h * a.G + (r - tok * a.G), t = rt.tok0 + tok, pos = rt.base + tok;
     const RowState<T> s = one_row<T, BF16>(a, rt.b, h, a.q + t * a.q_stride + hq * d, pos, tl, t0, t1, BN);
     if (part.n_splits > 1) {
-      const int64_t row = (int64_t)split * a.n_q * a.Hq + (int64_t)t * a.Hq + hq;
+      const int64_t row = split * part.rows + part_row(a, part, rt, h, r);
       if (lane == 0) part.ml[row] = make_float2(s.m * a.scale_log2, pos < 0 ? -1.f : s.l);
       for (int c = 0; c < T; ++c) part.o[row * d + kTile * c + lane] = s.o[c];
     } else {
@@ -874,9 +883,8 @@ __global__ __launch_bounds__(kWave) void k_paged_rows(PagedAttnArgs a, PartOut p
     redo_rows<T, BF16>(a, part, rt, h, rt.row0, kFewRows, tl, t0, t0 + n, split, BN);
     return;
   }
-  const int64_t part0 = (int64_t)split * a.n_q * a.Hq;
   if (part.n_splits > 1 && q4 == 0 && rt.row0 + (int)r16 < rt.rows)
-    part.ml[part0 + (int64_t)(rt.tok0 + tok) * a.Hq + h * a.G + row - tok * a.G] =
+    part.ml[split * part.rows + part_row(a, part, rt, h, row)] =
         make_float2(limit > -INFINITY ? -shift : -INFINITY, pos < 0 ? -1.f : l);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -885,7 +893,7 @@ __global__ __launch_bounds__(kWave) void k_paged_rows(PagedAttnArgs a, PartOut p
     if (orow >= rt.rows) continue;
     const int64_t t = rt.tok0 + otok;
     if (part.n_splits > 1) {
-      f32x4* dst = reinterpret_cast<f32x4*>(part.o + (part0 + t * a.Hq + hq) * d + NO * r16);
+      f32x4* dst = reinterpret_cast<f32x4*>(part.o + (split * part.rows + part_row(a, part, rt, h, orow)) * d + NO * r16);
 #pragma unroll
       for (int c = 0; c < T; ++c) dst[c] = (f32x4){o[4 * c][e], o[4 * c + 1][e], o[4 * c + 2][e], o[4 * c + 3][e]};
     } else {
@@ -915,7 +923,7 @@ __global__ __launch_bounds__(kMergeThreads) void k_paged_merge(PagedAttnArgs a, 
   constexpr int kStep = WIDE ? S : 1, kAhead = kMergeAhead < OF / kStep ? kMergeAhead : OF / kStep;
   static_assert(OF % (kStep * kAhead) == 0, "the ranges under way are of one round of weights");
   const int lane = (int)lane_id(), stream = (int)threadIdx.x / L, sub = (int)threadIdx.x % L;
-  const int64_t rows = (int64_t)a.n_q * a.Hq, i0 = WIDE ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * S + stream;
+  const int64_t rows = part.rows, i0 = WIDE ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * S + stream;
   // The row: of q and all its heads, or, where the requests of few rows have ranges of their own, the r-th of a request's and kv-head's.
   int t, hq;
   bool mine;
@@ -929,7 +937,7 @@ __global__ __launch_bounds__(kMergeThreads) void k_paged_merge(PagedAttnArgs a, 
   } else {
     t = (int)(i0 / a.Hq);
     hq = (int)(i0 - (int64_t)t * a.Hq);
-    mine = i0 < rows && t < a.cu[a.p.B];
+    mine = i0 < (int64_t)a.n_q * a.Hq && t < a.cu[a.p.B];
     if (a.mixed) {
 #pragma unroll
       for (int k = 0; k < (WIDE ? 1 : kWave / L); ++k) {
@@ -940,7 +948,7 @@ __global__ __launch_bounds__(kMergeThreads) void k_paged_merge(PagedAttnArgs a, 
     }
   }
   if (!mine) return;  // (all of a stream; WIDE: all of the workgroup)
-  const int64_t row = (int64_t)t * a.Hq + hq;
+  const int64_t row = part.by_entry ? i0 : (int64_t)t * a.Hq + hq;
   const int first = WIDE ? stream : 0, at = lane % OF;
   f32x4 x[kAhead], o = {};
   auto load = [&](int s0) __attribute__((always_inline)) {
@@ -1013,12 +1021,11 @@ static hipError_t merge_launch(const PagedAttnArgs& a, const PartOut& part, bool
 
 template <int T, bool BF16>
 static hipError_t attn_launch(const PagedAttnArgs& a, hipStream_t s) {
-  const int64_t rows = (int64_t)a.n_q * a.Hq;
-  const int most = a.few > a.many ? a.few : a.many;
-  PartOut few = {nullptr, (float*)a.ws, a.few}, many;
-  few.ml = (float2*)(few.o + most * rows * (64 * T));
-  many = few;
-  many.n_splits = a.many;
+  // (all outputs first, aligned as they are accessed)
+  const int64_t rows = (int64_t)a.n_q * a.Hq, n_few = paged_parts(a.few_rows, a.few), n_many = paged_parts(rows, a.many);
+  float* const o = (float*)a.ws;
+  float2* const ml = (float2*)(o + (n_few + n_many) * (64 * T));
+  const PartOut few = {ml, o, a.few_rows, a.by_entry, a.few}, many = {ml + n_few, o + n_few * (64 * T), rows, 0, a.many};
   hipError_t e;
   if (a.few > 0) {
     const int64_t tiles = a.mixed ? a.p.B : paged_tiles(a.p, a.G, a.n_q, kFewRows);

@@ -8,7 +8,7 @@ import torch
 import paper_2505_22913_amd as mf
 from oracle.paged import PagePlan, Refused
 from tests.gpu_common import announce
-from tests.paged_common import fill, starts
+from tests.paged_common import check, fill, starts
 
 pytestmark = pytest.mark.gpu
 
@@ -106,3 +106,30 @@ def test_a_plan_of_more_pages_than_there_are_is_refused(lens, n_free, keep, new,
     with pytest.raises(Refused) as e:
         plan.step(new, keep, n_slots)
     assert e.value.args == (mf.PLAN_STATE,)
+
+
+# ---- the workspace of calls of both kinds -----------------------------------------------------------
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("new", [[1, 300, 0, 2], [1, 1, 1, 6], [1] * 30 + [9]])
+@pytest.mark.parametrize("n_splits", [0, 2, 9, 70])
+@pytest.mark.parametrize("bad", [None, float("inf")])
+def test_ranges_of_single_tokens_lie_inside_the_workspace(dtype, d, new, n_splits, bad):
+    """Single tokens beside chunks, few rows of which make the entries' rows the smaller ones or q's: a workspace of
+    exactly what is asked for, of NaN, between guards; with a value that every row sees infinite in two requests."""
+    cached = [(700, 50, 3, 90)[b % 4] for b in range(len(new))]
+    lens = [a + b for a, b in zip(cached, new)]
+    announce(f"workspace {dtype} d={d} new={new} splits={n_splits} bad={bad}")
+    cache, ks, vs = fill(len(new), 2, d, 16, lens, dtype, seed=70)
+    if bad is not None:
+        for b in (0, 1):
+            cache.v[int(cache.table[b, 0]), 1, 2, 7] = bad
+            vs[b][1, 2, 7] = bad
+    g = torch.Generator().manual_seed(71)
+    q = torch.randn(sum(new), 8, d, generator=g).to(dtype).cuda()
+    need = mf.mustafar_paged_attn_workspace_bytes(cache, 8, sum(new), max(new), 900, n_splits)
+    assert need > 0
+    whole = torch.full((need + 512,), 255, dtype=torch.uint8, device="cuda")
+    got = mf.mustafar_paged_attn(q, cache, starts(new), max_q=max(new), max_tokens=900, n_splits=n_splits, ws=whole[256:256 + need])
+    check(got, q, ks, vs, new, lens, dtype, label="workspace")
+    assert bool((whole[:256] == 255).all()) and bool((whole[256 + need:] == 255).all())

@@ -139,3 +139,38 @@ def test_a_workspace_does_for_every_shorter_length(lib):
                 need = lib.mustafar_paged_attn_workspace_bytes(ctypes.byref(p), Hq, n_q, max_q, tokens, 0)
                 assert need >= last, (kw, Hq, n_q, max_q, tokens)
                 last = need
+
+
+def pages(**kw):
+    d, H = kw.get("d", 128), kw.get("H", 8)
+    p, st = init(**{"d": d, "H": H, "page_stride": H * 64 * d, "head_stride": 64 * d, "token_stride": d, "n_pages": 1 << 20,
+                    "max_pages": 1 << 15, **kw})
+    assert st == mf.OK
+    return p
+
+
+def need(p, Hq, n_q, max_q, max_tokens, n_splits=0):
+    return mf.lib().mustafar_paged_attn_workspace_bytes(ctypes.byref(p), Hq, n_q, max_q, max_tokens, n_splits)
+
+
+@pytest.mark.parametrize("B,H,Hq,n_q,max_q,tokens", [
+    (2, 8, 32, 8193, 8192, 32768), (2, 1, 8, 8193, 8192, 131072), (2, 8, 32, 513, 512, 16384), (2, 8, 32, 16385, 16384, 32768),
+    (4, 32, 32, 16384, 16384, 4096), (2, 1, 1, 100001, 100000, 200000), (64, 8, 32, 9000, 8192, 131072)])
+def test_a_long_chunk_beside_single_tokens_needs_a_small_workspace(lib, B, H, Hq, n_q, max_q, tokens):
+    """Single tokens' ranges are paid for by the rows that single tokens can have, not by the chunk's."""
+    for d in (64, 128, 256):
+        assert need(pages(B=B, H=H, d=d), Hq, n_q, max_q, tokens) <= 60 << 20, d
+
+
+def test_no_call_needs_more_than_the_launches_rows(lib):
+    """With the split that calls take by themselves: at most 16 * 2048 + 256 * 256 rows, as the header says."""
+    sizes = [1, 2, 3, 7, 16, 17, 63, 64, 65, 200, 512, 1000, 4096, 5000, 30000, 200000]
+    for d, rows in ((64, 98304), (128, 98304), (256, 98304)):
+        most = 0
+        for B in (1, 2, 3, 17, 64, 500, 4096):
+            for H, G in ((1, 1), (1, 64), (2, 3), (8, 4), (8, 16), (8, 17), (32, 1)):
+                p = pages(B=B, H=H, d=d)
+                for n_q in sizes:
+                    for max_q in [0] + sizes:
+                        most = max(most, need(p, H * G, n_q, max_q, 2 ** 21))
+        assert 1 << 24 <= most <= rows * (d + 2) * 4
