@@ -598,7 +598,7 @@ int mustafar_paged_write(const mustafar_pages_t* p, const void* k_new, int64_t k
  * first[b] + j (first: int32 device [B], NULL: 0) for the tokens it holds; rows behind
  * the last are left as they were. bf16 is rounded to the nearest fp16, magnitudes
  * over 65504 to 65504 (the compression takes finite inputs), NaN stays NaN. Errors:
- * EINVAL (n_max < 0, pointers, alignment). */
+ * EINVAL (n_max < 0, pointers, alignment, outputs of 2^32 pieces of 16 bytes or more). */
 int mustafar_paged_gather(const mustafar_pages_t* p, const void* first, void* x_k, void* x_v,
                           int n_max, void* stream);
 
@@ -637,8 +637,8 @@ size_t mustafar_paged_attn_workspace_bytes(const mustafar_pages_t* p, int Hq, in
  * values a probability is the sum of two numbers of the cache's type where the call's
  * requests have at most 16 rows a kv-head (their tokens times Hq/H: single tokens), and
  * rounded to the type where they have more; the softmax's maximum, sum and output are
- * held in fp32. Errors: EINVAL, EUNSUPPORTED (Hq/H over MUSTAFAR_PAGED_MAX_GROUP),
- * EWORKSPACE. */
+ * held in fp32. Errors: EINVAL (also: sizes and n_splits that make a launch of 2^32
+ * threads), EUNSUPPORTED (Hq/H over MUSTAFAR_PAGED_MAX_GROUP), EWORKSPACE. */
 int mustafar_paged_attn(const void* q, int64_t q_stride, int n_q, int Hq, const mustafar_pages_t* p,
                         const void* cu, int window, int sinks, float scale, void* out,
                         int64_t out_stride, int max_q, int max_tokens, int n_splits, void* ws,

@@ -46,9 +46,12 @@ struct PagedAttnArgs {
 
 // Rows are a request's new tokens times the query heads of a kv-head. k_paged_rows takes 16 at a time, k_paged_chunk 32 a wave and
 // 8 waves a workgroup (4 at d = 256; d = 64 T).
-constexpr int kFewRows = 16;
+constexpr int kFewRows = 16, kWaveSize = 64;
 constexpr int chunk_waves(int T) { return T == 4 ? 4 : 8; }
 constexpr int chunk_rows(int T) { return 32 * chunk_waves(T); }
+// Workgroups of k_paged_merge with a stream of 16 T lanes a row.
+constexpr int kMergeThreads = 256;
+inline int64_t merge_groups(int64_t rows, int T) { return (rows * 16 * T + kMergeThreads - 1) / kMergeThreads; }
 // Workgroups of so many rows that hold n_q tokens of B requests however they are divided.
 inline int64_t paged_tiles(const PagedView& p, int G, int n_q, int rows) { return (int64_t)n_q * G / rows + p.B; }
 

@@ -232,10 +232,16 @@ __global__ __launch_bounds__(256) void k_paged_write(PagedView p, const uint16_t
 
 hipError_t launch_paged_write(const PagedView& p, const uint16_t* k_new, int64_t k_stride, const uint16_t* v_new,
                               int64_t v_stride, const int32_t* slots, int n_new, hipStream_t s) {
-  const int64_t n_vec = (int64_t)n_new * p.H * (p.d / 8);
-  hipLaunchKernelGGL(k_paged_write, dim3((uint32_t)((n_vec + 255) / 256)), dim3(256), 0, s, p, k_new, k_stride, v_new,
-                     v_stride, slots, n_vec);
-  return hipGetLastError();
+  // (a launch has less than 2^32 threads)
+  const int64_t row = p.H * (p.d / 8), most = (((int64_t)1 << 32) - 512) / row;
+  for (int64_t t = 0; t < n_new; t += most) {
+    const int64_t n_vec = (n_new - t < most ? n_new - t : most) * row;
+    hipLaunchKernelGGL(k_paged_write, dim3((uint32_t)((n_vec + 255) / 256)), dim3(256), 0, s, p, k_new + t * k_stride, k_stride,
+                       v_new + t * v_stride, v_stride, slots + t, n_vec);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 // ------------------------------------------------------------------------------------------

@@ -9,10 +9,13 @@
 namespace {
 
 constexpr int kTile = MUSTAFAR_TILE;
-constexpr int64_t kMaxGroups = 0x7fffffff;  // workgroups of a launch
+constexpr int64_t kMaxRows = 0x7fffffff;
 constexpr int kMaxSplits = 1 << 16;
 
 bool aligned(const void* p, uintptr_t a) { return p && ((uintptr_t)p % a) == 0; }
+
+// A launch has less than 2^32 threads.
+bool launches(double groups, int threads) { return groups * threads < 4294967296.0; }
 
 int status_of(hipError_t e) { return e == hipSuccess ? MUSTAFAR_OK : MUSTAFAR_ELAUNCH; }
 
@@ -126,7 +129,6 @@ int mustafar_paged_write(const mustafar_pages_t* p, const void* k_new, int64_t k
   if (k_stride < row || v_stride < row || k_stride % 8 != 0 || v_stride % 8 != 0 || k_stride > (int64_t)1 << 31 ||
       v_stride > (int64_t)1 << 31)
     return MUSTAFAR_EINVAL;
-  if ((int64_t)n_new * (row / 8) / 256 >= kMaxGroups) return MUSTAFAR_EINVAL;
   return status_of(mf::launch_paged_write(view_of(p), (const uint16_t*)k_new, k_stride, (const uint16_t*)v_new,
                                           v_stride, (const int32_t*)slots, n_new, (hipStream_t)stream));
 }
@@ -138,7 +140,7 @@ int mustafar_paged_gather(const mustafar_pages_t* p, const void* first, void* x_
   if (n_max == 0) return MUSTAFAR_OK;
   if (!aligned(x_k, 16) || !aligned(x_v, 16) || (first && !aligned(first, 4))) return MUSTAFAR_EINVAL;
   const int64_t groups = ((int64_t)n_max * (p->d / 8) + 255) / 256;  // of an entry and kv-head
-  if ((double)p->B * p->H * (double)groups >= (double)kMaxGroups) return MUSTAFAR_EINVAL;
+  if (!launches((double)p->B * p->H * (double)groups, 256)) return MUSTAFAR_EINVAL;
   return status_of(mf::launch_paged_gather(view_of(p), (const int32_t*)first, (uint16_t*)x_k, (uint16_t*)x_v, n_max,
                                            (hipStream_t)stream));
 }
@@ -146,7 +148,7 @@ int mustafar_paged_gather(const mustafar_pages_t* p, const void* first, void* x_
 size_t mustafar_paged_attn_workspace_bytes(const mustafar_pages_t* p, int Hq, int n_q, int max_q, int max_tokens,
                                            int n_splits) {
   if (check_pages(p) != MUSTAFAR_OK || Hq < 1 || Hq % p->H != 0 || Hq / p->H > MUSTAFAR_PAGED_MAX_GROUP) return 0;
-  if (n_q < 1 || max_q < 0 || max_tokens < 0 || n_splits > kMaxSplits || (int64_t)n_q * Hq >= kMaxGroups) return 0;
+  if (n_q < 1 || max_q < 0 || max_tokens < 0 || n_splits > kMaxSplits || (int64_t)n_q * Hq >= kMaxRows) return 0;
   const mf::PagedView v = view_of(p);
   const mf::PagedPlan k = mf::paged_kernels(v, Hq / p->H, n_q, max_q, max_tokens, n_splits);
   return (size_t)mf::paged_ws_bytes(v, (int64_t)n_q * Hq, k);
@@ -166,7 +168,7 @@ int mustafar_paged_attn(const void* q, int64_t q_stride, int n_q, int Hq, const 
   if (q_stride < row || out_stride < row || q_stride % 8 != 0 || out_stride % 8 != 0 || q_stride > (int64_t)1 << 31 ||
       out_stride > (int64_t)1 << 31)
     return MUSTAFAR_EINVAL;
-  if ((int64_t)n_q * Hq >= kMaxGroups) return MUSTAFAR_EINVAL;
+  if ((int64_t)n_q * Hq >= kMaxRows) return MUSTAFAR_EINVAL;
   if (n_splits > kMaxSplits) return MUSTAFAR_EINVAL;
   mf::PagedAttnArgs a;
   a.p = view_of(p);
@@ -175,10 +177,15 @@ int mustafar_paged_attn(const void* q, int64_t q_stride, int n_q, int Hq, const 
   // (what the rows see: never more than the workspace was sized for)
   const int64_t seen = window > 0 ? (int64_t)window + max_q + sinks : max_tokens;
   const mf::PagedPlan k = mf::paged_kernels(a.p, Hq / p->H, n_q, max_q, seen < max_tokens ? seen : max_tokens, n_splits);
-  const int64_t tiles = k.few > 0 && !k.mixed ? mf::paged_tiles(a.p, Hq / p->H, n_q, mf::kFewRows)
-                                              : mf::paged_tiles(a.p, Hq / p->H, n_q, mf::chunk_rows(p->d / kTile));
-  if ((double)tiles * p->H * (k.few > k.many ? k.few : k.many) >= (double)kMaxGroups) return MUSTAFAR_EINVAL;
-  if (k.mixed && (double)p->B * p->H * mf::kFewRows >= (double)kMaxGroups) return MUSTAFAR_EINVAL;  // (k_paged_merge's rows)
+  const int T = p->d / kTile;
+  const int64_t q_rows = (int64_t)n_q * Hq, few_rows = k.mixed ? (int64_t)p->B * p->H * mf::kFewRows : q_rows;
+  const int64_t few = k.mixed ? p->B : mf::paged_tiles(a.p, Hq / p->H, n_q, mf::kFewRows);
+  const int64_t many = mf::paged_tiles(a.p, Hq / p->H, n_q, mf::chunk_rows(T));
+  if (!launches((double)few * p->H * k.few, mf::kWaveSize) || !launches((double)many * p->H * k.many, mf::kWaveSize * mf::chunk_waves(T)))
+    return MUSTAFAR_EINVAL;
+  if ((k.few > 1 && !launches((double)mf::merge_groups(few_rows, T), mf::kMergeThreads)) ||
+      (k.many > 1 && !launches((double)mf::merge_groups(q_rows, T), mf::kMergeThreads)))
+    return MUSTAFAR_EINVAL;
   a.few = k.few;
   a.many = k.many;
   a.mixed = k.mixed;

@@ -915,7 +915,7 @@ __global__ __launch_bounds__(kWave) void k_paged_rows(PagedAttnArgs a, PartOut p
 // d = 128, 16384 rows of 4 ranges take 9.4 us (3.8 TB/s; 12.5 with a wave a row). One stream a row against a workgroup a row:
 // 32 rows of 256 ranges 23.4 and 7.2 us, 512 of 16 4.8 both, 992 of 8 to 16 6.5 and 7.8, 2404 of 21 7.6 and 13.0.
 // ------------------------------------------------------------------------------------------
-constexpr int kMergeThreads = 256, kMergeAhead = 8, kMergeWideRows = 512;
+constexpr int kMergeAhead = 8, kMergeWideRows = 512;
 
 template <int T, bool BF16, int OF, bool WIDE>
 __global__ __launch_bounds__(kMergeThreads) void k_paged_merge(PagedAttnArgs a, PartOut part, int of_few) {
@@ -1008,8 +1008,7 @@ template <int T, bool BF16>
 static hipError_t merge_launch(const PagedAttnArgs& a, const PartOut& part, bool of_few, hipStream_t s) {
   if (part.n_splits <= 1) return hipSuccess;  // (written by its kernel)
   const int64_t rows = a.mixed && of_few ? (int64_t)a.p.B * a.p.H * kFewRows : (int64_t)a.n_q * a.Hq;
-  constexpr int S = 16 / T;
-  const dim3 streams((uint32_t)((rows + S - 1) / S)), block(kMergeThreads);
+  const dim3 streams((uint32_t)merge_groups(rows, T)), block(kMergeThreads);
   if (part.n_splits <= kMergeAhead)
     hipLaunchKernelGGL((k_paged_merge<T, BF16, kMergeAhead, false>), streams, block, 0, s, a, part, (int)of_few);
   else if (rows >= kMergeWideRows)

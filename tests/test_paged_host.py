@@ -174,3 +174,17 @@ def test_no_call_needs_more_than_the_launches_rows(lib):
                     for max_q in [0] + sizes:
                         most = max(most, need(p, H * G, n_q, max_q, 2 ** 21))
         assert 1 << 24 <= most <= rows * (d + 2) * 4
+
+
+@needs_toolchain
+def test_launches_of_too_many_threads_are_refused(tmp_path):
+    """Against stubs of the launchers, so that what is accepted launches nothing."""
+    objs = []
+    for src in (os.path.join(CSRC, "paged_api.hip"), os.path.join(SAN, "paged_stubs.hip")):
+        objs.append(str(tmp_path / (os.path.basename(src) + ".o")))
+        _run([HIPCC, "--offload-arch=gfx950", "-O1", "-std=c++17", f"-I{HEADER}", f"-I{CSRC}", "-c", src, "-o", objs[-1]])
+    objs.append(str(tmp_path / "limits.o"))
+    _run([CLANG, "-O1", f"-I{HEADER}", "-c", os.path.join(SAN, "paged_limits.c"), "-o", objs[-1]])
+    exe = str(tmp_path / "paged_limits")
+    _run([HIPCC, *objs, "-o", exe])
+    assert "paged limits ok" in _run([exe], env=ENV)
