@@ -166,13 +166,6 @@ __device__ __forceinline__ bool sees(int pos, int j, int window, int n_sinks) {
   return j <= pos && (window == 0 || j > pos - window || j < n_sinks);
 }
 
-__device__ __forceinline__ int page_of(const PagedView& p, int b, int j) {
-  // (through the scalar cache: uniform, and nothing in the launch writes the table)
-  const auto* t = (const __attribute__((address_space(4))) int32_t*)(p.table + (int64_t)b * p.max_pages);
-  const int page = t[j >> p.log2_page];
-  return (uint32_t)page < (uint32_t)p.n_pages ? page : 0;
-}
-
 // ------------------------------------------------------------------------------------------
 // A row by itself, one wave: every product in fp32 on the vector units, and nothing of a token that
 // the row does not see. The kernels below come here with the rows of a wave whose result is not
