@@ -605,7 +605,8 @@ class PagedCache:
     stack of free pages), int32. Tensors that are given are used as they are (k and v in any
     order of pages, heads and tokens whose channels are contiguous); the others are made, for an
     empty cache: a state that holds tokens comes with its table and its stack. max_pages: pages of the
-    longest request (default: all).
+    longest request (default: all). status [1] (int32): 0, or why the newest plan that was not
+    given a status of its own was refused.
     """
 
     def __init__(self, B: int, H: int, d: int, n_pages: int, page_tokens: int = 64, max_pages: int | None = None,
@@ -639,6 +640,7 @@ class PagedCache:
         _want("v", v, tuple(k.shape), dtype, k.device, dense=False)
         self.k, self.v, self.table, self.state, self.free = k, v, table, state, free
         self.dtype, self.device = dtype, k.device
+        self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
         self.desc = pages_t()
         _check("mustafar_paged_init", lib().mustafar_paged_init(
             ctypes.byref(self.desc), _dptr(k), _dptr(v), _dptr(table), _dptr(state), _dptr(free), B, H, d,
@@ -698,15 +700,17 @@ def mustafar_paged_plan(cache: PagedCache, new_len, n_slots: int, keep=None, sta
                         status=None, stream=None):
     """A step's pages, sequence starts and slots: new_len [B] (int32, device) new tokens behind the
     first keep [B] of every request (None: all it holds). Returns cu [B + 1] and slots [n_slots]. The
-    cache's state advances in place, or is written to state_out [B + 2]. status [1] is 0, or PLAN_
-    bits of a step that was refused and changed nothing."""
+    cache's state advances in place, or is written to state_out [B + 2]. status [1] (None: cache.status) is
+    0, or the PLAN_ bits of a step that was refused: it changed nothing, cu is 0 and slots are -1, so that the
+    step's write and attention leave everything as it is. Too few free pages are such a step; look at the
+    status before the results."""
     import torch
     B, i32 = cache.desc.B, torch.int32
     _current(cache)
     with _on_stream(stream):
         cu = torch.empty(B + 1, dtype=i32, device=cache.device) if cu is None else cu
         slots = torch.empty(n_slots, dtype=i32, device=cache.device) if slots is None else slots
-        status = torch.empty(1, dtype=i32, device=cache.device) if status is None else status
+    status = cache.status if status is None else status
     state_out = cache.state if state_out is None else state_out
     for name, x, n in (("new_len", new_len, B), ("keep", keep, B), ("state_out", state_out, B + 2), ("cu", cu, B + 1),
                        ("slots", slots, n_slots), ("status", status, 1)):
@@ -761,7 +765,9 @@ def mustafar_paged_attn(q, cache: PagedCache, cu, max_q: int | None = None, max_
     """Causal attention of q [n_q][Hq][d] (the cache's type; rows of a packed projection too), the last
     cu[b+1] - cu[b] tokens of every request b, over its pages; window > 0: the newest `window` tokens
     and the first `sinks`. max_q and max_tokens: bounds of a request's rows and length (default: one
-    row each if n_q <= B, else n_q; all that a table can hold). Returns out [n_q][Hq][d]."""
+    row each if n_q <= B, else n_q; all that a table can hold); with bounds near the truth calls are faster.
+    Returns out [n_q][Hq][d]; rows from cu[B] on (all of a refused plan's) are left as they were, 0 in a tensor that
+    the call makes."""
     import torch
     if q.dim() != 3:
         raise ValueError(f"q: [n_q][Hq][{cache.desc.d}] expected, not {tuple(q.shape)}")
@@ -782,7 +788,7 @@ def mustafar_paged_attn(q, cache: PagedCache, cu, max_q: int | None = None, max_
         raise ValueError(f"ws: contiguous memory on {cache.device} expected")
     if out is None:
         with _on_stream(stream):
-            out = torch.empty((n_q, Hq, d), dtype=cache.dtype, device=cache.device)
+            out = torch.zeros((n_q, Hq, d), dtype=cache.dtype, device=cache.device)
     os_ = _rows("out", out, n_q, Hq, cache)
     _check("mustafar_paged_attn", lib().mustafar_paged_attn(
         _dptr(q), qs, n_q, Hq, ctypes.byref(cache.desc), _dptr(cu), int(window), int(sinks), float(scale), _dptr(out),

@@ -133,3 +133,44 @@ def test_ranges_of_single_tokens_lie_inside_the_workspace(dtype, d, new, n_split
     got = mf.mustafar_paged_attn(q, cache, starts(new), max_q=max(new), max_tokens=900, n_splits=n_splits, ws=whole[256:256 + need])
     check(got, q, ks, vs, new, lens, dtype, label="workspace")
     assert bool((whole[:256] == 255).all()) and bool((whole[256 + need:] == 255).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("new", [[1, 1], [200, 90]])
+def test_a_refused_step_is_told_and_gives_no_memory_of_others(dtype, new):
+    """Too few pages: the cache's status says so, the write leaves the pages as they are and attention's output is 0;
+    after pages have been given back the same step is taken, and the status is 0 again."""
+    lens, d = [48, 64], 128
+    cache, ks, vs = fill(2, 2, d, 16, lens, dtype, seed=80, spare=0, max_pages=40)
+    assert cache.status.tolist() == [0]
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    n = sum(new)
+    x = torch.randn(n, 2, d, device="cuda").to(dtype)
+    q = torch.randn(n, 8, d, device="cuda").to(dtype)
+    before = [t.clone() for t in (cache.k, cache.v, cache.state, cache.table)]
+    cu, slots = mf.mustafar_paged_plan(cache, ints([1, 1] if new == [1, 1] else new), n)
+    mf.mustafar_paged_write(cache, x, x, slots)
+    for _ in range(4):
+        dirty = [torch.full_like(q, float("nan")) for _ in range(8)]     # what the allocator hands out next
+        torch.cuda.synchronize()
+        del dirty
+        out = mf.mustafar_paged_attn(q, cache, cu, max_q=max(new), max_tokens=300)
+        assert bool((out == 0).all())
+    assert cache.status.tolist() == [mf.PLAN_PAGES]
+    for t, y in zip(before, (cache.k, cache.v, cache.state, cache.table)):
+        assert torch.equal(t, y)
+    mf.mustafar_paged_plan(cache, ints([0, 0]), 0, keep=ints([48, 10]))
+    assert cache.status.tolist() == [0]
+    cu, slots = mf.mustafar_paged_plan(cache, ints([1, 0]), 3)           # padded: rows behind the last are 0 too
+    assert cache.status.tolist() == [0] and cu.tolist() == [0, 1, 1]
+    mf.mustafar_paged_write(cache, x[:1].expand(3, 2, d).contiguous(), x[:1].expand(3, 2, d).contiguous(), slots)
+    dirty = torch.full((3, 8, d), float("nan"), dtype=dtype, device="cuda")
+    del dirty
+    out = mf.mustafar_paged_attn(q[:1].expand(3, 8, d).contiguous(), cache, cu, max_q=1, max_tokens=300)
+    new_k = [torch.cat([t[0], x[:1].cpu().transpose(0, 1)], 1) for t in (ks, vs)]
+    check(out[:1], q[:1], [new_k[0]], [new_k[1]], [1], [49], dtype, label="padded")
+    assert bool((out[1:] == 0).all())
+    torch.cuda.synchronize()
+    own = ints([5])
+    mf.mustafar_paged_plan(cache, ints([1000, 0]), 2000, status=own)     # a status of the call's own
+    assert own.tolist() == [mf.PLAN_TABLE] and cache.status.tolist() == [0]
