@@ -9,6 +9,7 @@ import paper_2505_22913_amd as mf
 from oracle.paged import PagePlan, Refused
 from tests.gpu_common import announce
 from tests.paged_common import check, fill, starts
+from tests.test_gpu_paged import attend
 
 pytestmark = pytest.mark.gpu
 
@@ -174,3 +175,112 @@ def test_a_refused_step_is_told_and_gives_no_memory_of_others(dtype, new):
     own = ints([5])
     mf.mustafar_paged_plan(cache, ints([1000, 0]), 2000, status=own)     # a status of the call's own
     assert own.tolist() == [mf.PLAN_TABLE] and cache.status.tolist() == [0]
+
+
+# ---- ranges longer than what a wave looks up at once -------------------------------------------------
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("n_splits", [1, 2])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (3000, 1100), (1500, 4)])
+def test_single_tokens_over_ranges_of_many_pages(dtype, d, n_splits, window, sinks):
+    """Offsets of 32 tiles of 32 tokens are looked up at once, and again behind them (and behind the sinks')."""
+    attend(dtype, 1, 2, d, 16, [1022, 1023, 1024, 1054, 2111, 4999], [1] * 6, window=window, sinks=sinks, n_splits=n_splits, seed=90)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("n_splits", [1, 2])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (5000, 4300), (4500, 4)])
+def test_chunks_over_ranges_of_many_pages(dtype, d, n_splits, window, sinks):
+    """Offsets of 64 tiles of 64 tokens (32 at d = 256) are looked up at once."""
+    attend(dtype, 1, 4, d, 16, [2047, 4095, 4097, 9000], [20, 9, 33, 40], window=window, sinks=sinks, n_splits=n_splits, seed=91)
+
+
+# ---- the weights' range, and large scores --------------------------------------------------------------
+def set_tokens(cache, which, b, x):
+    """The tokens x [H][L][d] of request b into its pages."""
+    P = cache.page_tokens
+    pool = getattr(cache, which)
+    for i in range((x.shape[1] + P - 1) // P):
+        at = x[:, i * P:(i + 1) * P]
+        pool[int(cache.table[b, i]), :, :at.shape[1]] = at.cuda()
+
+
+def tight(got, q, k, v, scale, dtype, one_part, label, least=0.0):
+    """got [n][Hq][d] against float64 where scores are exact in fp32: as in the first test above, with the type's own rounding
+    of a weight where it has one part, and `least` for those of its errors that the weight does not scale."""
+    n, L, u = q.shape[0], k.shape[1], torch.finfo(dtype).eps / 2
+    want, mean = softmax_of(exact_scores(q, k, scale), v, causal(n, L, "cpu"))
+    rel = (u if one_part else u * u) + 0.6932 * (2.0 ** -18 + 60 * 2.0 ** -24) + 2.0 ** -22 + (L + 32) * 2.0 ** -24
+    tol = half_step(want, dtype) + 2 * rel * mean * (1 + u) + 2 * least
+    worst = float(((got.double().cpu() - want).abs() / tol).max())
+    announce(f"  {label}: {worst:.2f} of its bound")
+    assert worst <= 1, f"{label}: an element is {worst:.2f} of its bound off"
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n", [1, 40])
+@pytest.mark.parametrize("n_splits", [0, 1])
+@pytest.mark.parametrize("late", [False, True])
+def test_one_token_26_log2_units_above_the_others(dtype, n, n_splits, late):
+    """A token of value 0 whose score is 18 above that of 60000 others: the output is what the others' weights make,
+    each 2^-26 of the largest and under fp16's normal numbers. A weight in fp16 is off by up to 2^-25 where the largest is at least
+    2^7, 2^-32 of it, whatever the weight."""
+    L, d = 60001, 64
+    announce(f"peak {dtype} n={n} splits={n_splits} late={late}")
+    cache, ks, vs = fill(1, 1, d, 64, [L], dtype, seed=92)
+    k, v = torch.zeros_like(ks[0]), (512 + 64 * vs[0].float()).to(dtype)
+    j = L - n - 3 if late else 2
+    k[0, j], v[0, j] = 2.25, 0.0
+    set_tokens(cache, "k", 0, k)
+    set_tokens(cache, "v", 0, v)
+    q = torch.ones(n, 2, d, dtype=dtype)
+    got = mf.mustafar_paged_attn(q.cuda(), cache, starts([n]), n_splits=n_splits, scale=0.125)
+    least = L * 2.0 ** -32 * float(v.abs().max()) if dtype == torch.float16 else 0.0
+    tight(got, q, k, v, 0.125, dtype, n > 1, "peak", least)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("n", [1, 70])
+@pytest.mark.parametrize("n_splits", [1, 5])
+@pytest.mark.parametrize("high", [16.0, 16384.0])
+def test_scores_that_are_large_and_differ_little(dtype, d, n, n_splits, high):
+    """Scores of 2^10 or 2^20 with differences of tens, times 2^-5: a common rounding of the softmax's shift takes no part in the
+    weights' ratios."""
+    L, H, G = 500, 2, 4
+    announce(f"large scores {dtype} d={d} n={n} splits={n_splits} high={high}")
+    cache, _, vs = fill(1, H, d, 16, [L], dtype, seed=93)
+    g = torch.Generator().manual_seed(94)
+    k, q = torch.randint(-3, 4, (H, L, d), generator=g).to(dtype), torch.randint(-3, 4, (n, H * G, d), generator=g).to(dtype)
+    k[..., 3], q[..., 3] = high, 64.0
+    assert float(exact_scores(q, k, 2.0 ** -5).std(-1).max()) < 5
+    set_tokens(cache, "k", 0, k)
+    got = mf.mustafar_paged_attn(q.cuda(), cache, starts([n]), n_splits=n_splits, scale=2.0 ** -5)
+    least = L * 2.0 ** -32 * float(vs[0].abs().max()) if dtype == torch.float16 else 0.0
+    tight(got, q, k, vs[0], 2.0 ** -5, dtype, n * G > 16, "large scores", least)
+
+
+# ---- several layers ------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_layers_share_a_steps_table_state_and_stack(dtype):
+    """A cache a layer with keys and values of its own; one plan a step, taken on one of them, places every layer's."""
+    B, H, G, d, P = 2, 2, 2, 64, 16
+    first = mf.PagedCache(B, H, d, 24, P, max_pages=12, dtype=dtype)
+    layers = [first] + [mf.PagedCache(B, H, d, 24, P, dtype=dtype, table=first.table, state=first.state, free=first.free)
+                        for _ in range(2)]
+    held = [[[], []] for _ in layers]
+    lens = [0, 0]
+    for step, new in enumerate(([40, 17], [1, 1], [30, 1])):
+        n = sum(new)
+        cu, slots = mf.mustafar_paged_plan(first, torch.tensor(new, dtype=torch.int32, device="cuda"), n)
+        lens = [a + b for a, b in zip(lens, new)]
+        assert all(c.lens.tolist() == lens for c in layers)
+        for layer, (cache, h) in enumerate(zip(layers, held)):
+            x = torch.randn(n, (G + 2) * H, d, device="cuda").to(dtype)
+            mf.mustafar_paged_write(cache, x[:, G * H:G * H + H], x[:, G * H + H:], slots)
+            h[0].append(x[:, G * H:G * H + H].split(new))
+            h[1].append(x[:, G * H + H:].split(new))
+            out = mf.mustafar_paged_attn(x[:, :G * H], cache, cu, max_q=max(new), max_tokens=max(lens))
+            ks, vs = ([torch.cat([p[b] for p in part]).transpose(0, 1) for b in range(B)] for part in h)
+            check(out, x[:, :G * H], ks, vs, new, lens, dtype, label=f"step {step} layer {layer}")
