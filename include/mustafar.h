@@ -522,7 +522,9 @@ int mustafar_window_step_grouped(mustafar_window_t* w, mustafar_ccache_t* Kc, mu
  *             once, left 0 by every call)
  *   free_pages [n_pages] int32: a stack of free pages, the top at index count - 1
  * All are device memory of the caller, who sets them for an empty cache (lengths 0,
- * n_pages free pages, every page on the stack; tables need no setting). */
+ * n_pages free pages, every page on the stack; tables need no setting). A model has a
+ * cache a layer: keys and values of its own, and the same table, state and stack, so
+ * that one plan a step, of any of them, is every layer's. */
 enum mustafar_type { MUSTAFAR_FP16 = 0, MUSTAFAR_BF16 = 1 };
 
 #define MUSTAFAR_PAGED_MAX_BATCH 4096       /* entries of a paged cache               */

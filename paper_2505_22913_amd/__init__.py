@@ -606,7 +606,8 @@ class PagedCache:
     order of pages, heads and tokens whose channels are contiguous); the others are made, for an
     empty cache: a state that holds tokens comes with its table and its stack. max_pages: pages of the
     longest request (default: all). status [1] (int32): 0, or why the newest plan that was not
-    given a status of its own was refused.
+    given a status of its own was refused. A model has a cache a layer, each with k and v of its own and
+    the first one's table, state and free, and a step one plan, taken on the first.
     """
 
     def __init__(self, B: int, H: int, d: int, n_pages: int, page_tokens: int = 64, max_pages: int | None = None,
