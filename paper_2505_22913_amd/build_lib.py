@@ -24,8 +24,8 @@ LIB = os.path.join(HERE, "libmustafar.so")
 SOURCES = ["api.hip", "compress.hip", "attention.hip", "attention_mfma.hip", "measure.hip", "paged_api.hip", "paged.hip",
            "paged_attn.hip"]
 ARCH = "gfx950"
-# Per source: k_paged_chunk runs one wave a SIMD; left to itself the compiler then gives every matrix
-# product an AGPR result and copies the scores, which the vector units read, out of them.
+# Per source: k_paged_chunk runs two waves a SIMD, one at d = 256; left to itself the compiler gives every
+# matrix product an AGPR result and copies the scores, which the vector units read, out of them.
 EXTRA_FLAGS = {"paged_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 

@@ -170,7 +170,9 @@ __device__ __forceinline__ bool sees(int pos, int j, int window, int n_sinks) {
 // A row by itself, one wave: every product in fp32 on the vector units, and nothing of a token that
 // the row does not see. The kernels below come here with the rows of a wave whose result is not
 // finite: their matrix products take whole tiles, so that a value that is not finite reaches
-// the rows that do not see it (0 times infinity).
+// the rows that do not see it (0 times infinity). Latency bounds it, a row of 4096 tokens takes more than a millisecond: a
+// prompt of 4096 with 32 heads, 170 us, takes 29 ms where every row of one head sees an infinity, 46 where those of all do, 42
+// where only the last row does.
 // ------------------------------------------------------------------------------------------
 // The least weight of a visible token: an infinite value that one sees stays infinite
 // where its probability is under fp32's range (0 times infinity would be NaN).
@@ -272,10 +274,11 @@ __device__ __forceinline__ void redo_rows(const PagedAttnArgs& a, const PartOut&
 // step before they are needed, so that the first operands of a step are read before its barrier; they go where the step
 // before has read.
 //
-// The matrix units bound it, at the clock that the card's power leaves them: of 4 prompts of 4096 tokens with 32 heads at d = 128
-// (550 GFLOP of visible pairs), 535 to 560 us from one card to the next (1.03 to 0.98 PFLOP/s, where a product of 8192^3 reaches
-// 1.23 to 1.19), they are busy for half of the cycles and the vector units for 44%, at 1.9 GHz of 2.4; LDS has no conflicts. One
-// prompt of 4096 with 16 heads at d = 256: 155 us, 0.89 PFLOP/s. A workgroup alone on its CU (128 KB of LDS) starts
+// The matrix units and the vector units bound it, hardly ever at once: of 4 prompts of 4096 tokens with 32 heads at d = 128 (550 GFLOP
+// of visible pairs), 535 to 570 us from one card to the next (1.03 to 0.96 PFLOP/s, where a product of 8192^3 reaches 1.23 to
+// 1.19), the first are busy for half of the cycles and the second for 45%, at the 1.9 GHz of 2.4 that the card's power leaves
+// them; LDS has no conflicts. The same with d = 64: 358 us, 0.77 PFLOP/s. One prompt of 4096 with 16 heads at d = 256: 155 to 167 us,
+// 0.89 to 0.82 PFLOP/s. A workgroup alone on its CU (128 KB of LDS) starts
 // and ends in 9 us and takes 1.7 a tile. Tried at the first size: the probabilities between the products of X and Y, 566 us for 548; Y
 // before X, so that one buffer of scores will do, 573 for 545, with four of the eight waves half a step later 596; 64
 // rows a wave and one wave a SIMD, 694 for 592; two workgroups of 4 waves a CU and tiles of 32, 586 for 543; a tile's loads all at
@@ -694,8 +697,8 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
 // calls below, both forms in turn on one card. Rounded to the type they made bf16 outputs' error 1.4 times their own rounding's.
 //
 // With k_paged_merge, and in parentheses k_paged_chunk instead: 16 requests of up to 16384 tokens, 8 kv-heads of 4 rows, d = 128 (634
-// MB) 115 us, 5.5 TB/s (152); one of 4096 with 32 heads 18 (20.5); 32 with a window of 1024, d = 64, 8 rows 21 (21); of 16
-// rows, 16 requests of 16384 tokens 165 (194), one 23 (22), 32 of 1024 32 (28). Rows beyond 16 would read the pages twice. The next
+// MB) 116 us, 5.5 TB/s (152); one of 4096 with 32 heads 18.4 (20.5); 32 with a window of 1024, d = 64, 8 rows 21.5 (21); of 16
+// rows, 16 requests of 16384 tokens 166 (194), one 23.6 (22), 32 of 1024 32.6 (28). Rows beyond 16 would read the pages twice. The next
 // tile's loads follow the products that free their registers; with as many registers again, for two tiles: 119 us for 117.
 // ------------------------------------------------------------------------------------------
 constexpr int kRowsTile = 32;
