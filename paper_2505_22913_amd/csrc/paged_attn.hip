@@ -687,7 +687,7 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
 // ------------------------------------------------------------------------------------------
 // k_paged_rows: at most 16 rows, one wave, tiles of 32 tokens: single tokens (and few) over a long cache.
 //
-// The loads bound it (16 KB of keys and values a tile at d = 128 for some 250 vector instructions), so nothing goes through
+// The loads bound it (16 KB of keys and values a tile at d = 128 for some 180 vector instructions), so nothing goes through
 // LDS: a key row's 16-byte pieces are the A operand of S = K Q^T as they are loaded (lane = token l % 16, channels 32 c +
 // 8 (l / 16)), its result (row l % 16, tokens 4 (l / 16) + e of the tile's two groups of 16) is the A operand of O = P V, and a
 // lane loads channels 4 T (l % 16) .. of those eight tokens and transposes them with byte permutes into the B operand.
