@@ -291,9 +291,11 @@ constexpr int kDepth = 3, kRing = kDepth + 1;
 // A probability is 2^kBias at the reference, which follows the largest score once that is more than 2^kSlack above it:
 // at most 2^15 (inside fp16), and fp16 keeps those down to 2^-31 of the reference. It is exp2(score * scale +
 // shift) with shift = kBias - reference * scale rounded: one shift for all weights of a row, so its rounding is a
-// factor of them all. (Scores of 2^23 and more, where that factor leaves fp16, give infinities or zeros, and
-// the row is done by itself.)
+// factor of them all: under kFar at most 2 (fp16, whose small weights it must not lose) and 2^8 (bf16, for the
+// least weight of k_paged_merge's ranges). Rows with larger shifts are done by themselves.
 constexpr float kBias = 7.f, kSlack = 8.f;
+template <bool BF16>
+constexpr float kFar = BF16 ? 0x1p28f : 0x1p25f;
 
 // 16-byte pieces of a row are stored at their place XOR these, so that the lanes of a read (K: one piece of
 // many rows; V: 32 or 64 bytes of four rows) find them in different banks.
@@ -648,7 +650,7 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
   for (int c = 0; c < ND; ++c)
 #pragma unroll
     for (int r = 0; r < 16; ++r) z = fmaf(o[c][r], 0.f, z);
-  if (ballot(row < rt.rows && (z != z || (limit > -INFINITY && l == 0.f)))) {
+  if (ballot(row < rt.rows && (z != z || fabsf(shift) >= kFar<BF16>))) {
     redo_rows<T, BF16>(a, part, rt, h, wrow, 32, tl, t0, t0 + n, split, BN);
     return;
   }
@@ -875,7 +877,7 @@ __global__ __launch_bounds__(kWave) void k_paged_rows(PagedAttnArgs a, PartOut p
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (rt.row0 + (int)(4 * q4) + e < rt.rows) z = fmaf(o[c][e], 0.f, z);
-  if (ballot(z != z || (rt.row0 + (int)r16 < rt.rows && limit > -INFINITY && l == 0.f))) {
+  if (ballot(z != z || (rt.row0 + (int)r16 < rt.rows && fabsf(shift) >= kFar<BF16>))) {
     redo_rows<T, BF16>(a, part, rt, h, rt.row0, kFewRows, tl, t0, t0 + n, split, BN);
     return;
   }

@@ -284,3 +284,27 @@ def test_layers_share_a_steps_table_state_and_stack(dtype):
             out = mf.mustafar_paged_attn(x[:, :G * H], cache, cu, max_q=max(new), max_tokens=max(lens))
             ks, vs = ([torch.cat([p[b] for p in part]).transpose(0, 1) for b in range(B)] for part in h)
             check(out, x[:, :G * H], ks, vs, new, lens, dtype, label=f"step {step} layer {layer}")
+
+
+# ---- scores that the softmax's shift cannot follow closely ------------------------------------------------
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("n", [1, 20])
+@pytest.mark.parametrize("n_splits", [1, 3])
+@pytest.mark.parametrize("bits", [24, 26, 28, 30])
+def test_scores_whose_shift_rounds_by_many_bits(dtype, d, n, n_splits, bits):
+    """One token far above the others, with scores of 2^24 to 2^30 in which the shift's own rounding is a factor
+    of up to 2^64: the output is that token's value, which has the type already."""
+    H, G, L = 4, 4, 150
+    announce(f"shift {dtype} d={d} n={n} splits={n_splits} bits={bits}")
+    cache, ks, vs = fill(1, H, d, 16, [L], dtype, seed=95)
+    k = torch.full_like(ks[0], -64.0)
+    for h in range(H):
+        k[h, 3 + 29 * h] = 64.0
+    set_tokens(cache, "k", 0, k)
+    g = torch.Generator().manual_seed(96)
+    q = (128 + torch.randint(0, 128, (n, H * G, 1), generator=g)).expand(n, H * G, d).to(dtype)     # scores: whole numbers
+    got = mf.mustafar_paged_attn(q.contiguous().cuda(), cache, starts([n]), n_splits=n_splits, scale=2.0 ** bits / (128 * 64 * d))
+    for h in range(H):
+        want = vs[0][h, 3 + 29 * h].expand(n, G, d)
+        assert torch.equal(got[:, h * G:(h + 1) * G].cpu(), want), f"kv-head {h}"
