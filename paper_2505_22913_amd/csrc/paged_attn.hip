@@ -252,8 +252,11 @@ __device__ __forceinline__ void redo_rows(const PagedAttnArgs& a, const PartOut&
     const RowState<T> s = one_row<T, BF16>(a, rt.b, h, a.q + t * a.q_stride + hq * d, pos, tl, t0, t1, BN);
     if (part.n_splits > 1) {
       const int64_t row = split * part.rows + part_row(a, part, rt, h, r);
-      if (lane == 0) part.ml[row] = make_float2(s.m * a.scale_log2, pos < 0 ? -1.f : s.l);
-      for (int c = 0; c < T; ++c) part.o[row * d + kTile * c + lane] = s.o[c];
+      // (what the maximum's rounding leaves goes into the sums: other ranges' are multiples of 2^m with theirs. Beyond 2^27 scores
+      // of fp32 differ by more than 2^8 or not at all.)
+      const float m = s.m * a.scale_log2, f = __builtin_amdgcn_exp2f(fminf(fmaxf(fmaf(s.m, a.scale_log2, -m), -8.f), 8.f));
+      if (lane == 0) part.ml[row] = make_float2(m, pos < 0 ? -1.f : s.l * f);
+      for (int c = 0; c < T; ++c) part.o[row * d + kTile * c + lane] = s.o[c] * f;
     } else {
       for (int c = 0; c < T; ++c)
         a.out[t * a.out_stride + hq * d + kTile * c + lane] = (uint16_t)pack2<BF16>(pos < 0 ? 0.f : s.o[c] / s.l, 0.f);

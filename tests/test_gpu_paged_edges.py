@@ -308,3 +308,36 @@ def test_scores_whose_shift_rounds_by_many_bits(dtype, d, n, n_splits, bits):
     for h in range(H):
         want = vs[0][h, 3 + 29 * h].expand(n, G, d)
         assert torch.equal(got[:, h * G:(h + 1) * G].cpu(), want), f"kv-head {h}"
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("n", [1, 70])
+@pytest.mark.parametrize("n_splits", [1, 5])
+def test_a_range_with_an_infinity_beside_others_at_large_scores(dtype, d, n, n_splits):
+    """One channel of one token's value is infinite, so that the rows of its range are done by themselves; scores of 2^20
+    times 2^-5 differ by tens, and the other channels get every range's share as closely as without it."""
+    L, H, G = 500, 2, 4
+    announce(f"infinity at large scores {dtype} d={d} n={n} splits={n_splits}")
+    cache, _, vs = fill(1, H, d, 16, [L], dtype, seed=97)
+    g = torch.Generator().manual_seed(98)
+    k, q = torch.randint(-3, 4, (H, L, d), generator=g).to(dtype), torch.randint(-3, 4, (n, H * G, d), generator=g).to(dtype)
+    k[..., 3], q[..., 3] = 16384.0, (64 + torch.arange(H * G) % 7).to(dtype)
+    set_tokens(cache, "k", 0, k)
+    v = vs[0].clone()
+    v[:, 250, 5] = float("inf")
+    set_tokens(cache, "v", 0, v)
+    got = mf.mustafar_paged_attn(q.cuda(), cache, starts([n]), n_splits=n_splits, scale=2.0 ** -5)
+    assert bool((got[..., 5] == float("inf")).all())
+    keep = [c for c in range(d) if c != 5]
+    score = exact_scores(q, k, 2.0 ** -5)
+    want, mean = softmax_of(score, vs[0], causal(n, L, "cpu"))
+    u = torch.finfo(dtype).eps / 2
+    rel = u + 0.6932 * (2.0 ** -18 + 60 * 2.0 ** -24) + 2.0 ** -22 + (L + 32) * 2.0 ** -24
+    if n * G <= 16:
+        rel -= u - u * u
+    least = L * 2.0 ** -32 * float(vs[0].abs().max()) if dtype == torch.float16 else 0.0
+    tol = half_step(want, dtype) + 2 * rel * mean * (1 + u) + 2 * least
+    worst = float(((got.double().cpu() - want).abs() / tol)[..., keep].max())
+    announce(f"  {worst:.2f} of its bound")
+    assert worst <= 1, f"an element is {worst:.2f} of its bound off"
