@@ -690,6 +690,11 @@ def _rows(name, x, n, heads, cache):
     return rows if n > 1 else heads * d
 
 
+def _int32(x) -> int:
+    """A number of tokens as the C call takes it: behind 32 bits it would see another, and no cache holds more."""
+    return max(-1, min(int(x), 0x7fffffff))
+
+
 def _on_stream(stream):
     """Allocations of a call go to the stream that it works on."""
     import contextlib
@@ -756,8 +761,8 @@ def mustafar_paged_gather(cache: PagedCache, n_max: int, first=None, x_k=None, x
 
 def mustafar_paged_attn_workspace_bytes(cache: PagedCache, Hq: int, n_q: int, max_q: int, max_tokens: int,
                                         n_splits: int = 0) -> int:
-    return lib().mustafar_paged_attn_workspace_bytes(ctypes.byref(cache.desc), int(Hq), int(n_q), int(max_q),
-                                                     int(max_tokens), int(n_splits))
+    return lib().mustafar_paged_attn_workspace_bytes(ctypes.byref(cache.desc), int(Hq), int(n_q), _int32(max_q),
+                                                     _int32(max_tokens), int(n_splits))
 
 
 def mustafar_paged_attn(q, cache: PagedCache, cu, max_q: int | None = None, max_tokens: int | None = None,
@@ -778,6 +783,7 @@ def mustafar_paged_attn(q, cache: PagedCache, cu, max_q: int | None = None, max_
     max_q = (1 if n_q <= B else n_q) if max_q is None else max_q
     if max_tokens is None:
         max_tokens = min(cache.desc.max_pages, cache.desc.n_pages) * cache.desc.page_tokens
+    max_q, max_tokens, window, sinks = _int32(max_q), _int32(max_tokens), _int32(window), _int32(sinks)
     qs = _rows("q", q, n_q, Hq, cache)
     _want("cu", cu, (B + 1,), torch.int32, cache.device)
     if ws is None:
@@ -792,8 +798,8 @@ def mustafar_paged_attn(q, cache: PagedCache, cu, max_q: int | None = None, max_
             out = torch.zeros((n_q, Hq, d), dtype=cache.dtype, device=cache.device)
     os_ = _rows("out", out, n_q, Hq, cache)
     _check("mustafar_paged_attn", lib().mustafar_paged_attn(
-        _dptr(q), qs, n_q, Hq, ctypes.byref(cache.desc), _dptr(cu), int(window), int(sinks), float(scale), _dptr(out),
-        os_, int(max_q), int(max_tokens), int(n_splits), _dptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
+        _dptr(q), qs, n_q, Hq, ctypes.byref(cache.desc), _dptr(cu), window, sinks, float(scale), _dptr(out),
+        os_, max_q, max_tokens, int(n_splits), _dptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
         _stream(stream)))
     return out
 

@@ -341,3 +341,18 @@ def test_a_range_with_an_infinity_beside_others_at_large_scores(dtype, d, n, n_s
     worst = float(((got.double().cpu() - want).abs() / tol)[..., keep].max())
     announce(f"  {worst:.2f} of its bound")
     assert worst <= 1, f"an element is {worst:.2f} of its bound off"
+
+
+# ---- the binding's numbers -----------------------------------------------------------------------------
+@pytest.mark.parametrize("new", [[1, 1], [40, 3]])
+@pytest.mark.parametrize("more", [5, 1 << 31, -3, 5 - (1 << 32)])
+def test_bounds_and_windows_beyond_32_bits(new, more):
+    """A window, first tokens or bounds of 2^32 and some are more than any cache holds, not `some`; negative ones are refused."""
+    big = (1 << 32) + more if more > 0 else more
+    args = (torch.float16, 2, 2, 64, 16, [300, 20], new)
+    for kw in (dict(window=big), dict(window=7, sinks=big), dict(max_q=big), dict(max_tokens=big)):
+        if more < 0:
+            with pytest.raises(mf.MustafarError):
+                attend(*args, **kw)
+        else:
+            attend(*args, **kw)
