@@ -516,7 +516,7 @@ int mustafar_window_step_grouped(mustafar_window_t* w, mustafar_ccache_t* Kc, mu
  *             h * head_stride + o * token_stride (strides in elements, multiples of
  *             8: [n_pages][H][P][d] and [n_pages][P][H][d] are both pages)
  *   table     [B][max_pages] int32: page i of entry b holds its tokens
- *             i * P .. i * P + P - 1, P = page_tokens
+ *             i * P .. i * P + P - 1, P = page_tokens; a page is one entry's
  *   state     [B + 2] int32: the tokens that each entry holds, the number of free
  *             pages, and a word that mustafar_paged_plan uses (zeroed by the caller
  *             once, left 0 by every call)
