@@ -356,3 +356,37 @@ def test_bounds_and_windows_beyond_32_bits(new, more):
                 attend(*args, **kw)
         else:
             attend(*args, **kw)
+
+
+# ---- captured ------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("new", [[1, 1], [90, 1]])
+def test_a_captured_call_that_makes_its_own_tensors_replays(dtype, new):
+    """Plan, write and attention without status, output and workspace of the caller's, in one graph: every replay gives what eager
+    calls on a second cache give, and 0 in the padded rows, with eager work between the replays."""
+    B, H, G, d, n = 2, 2, 4, 128, sum(new) + 3
+    caches = [fill(B, H, d, 16, [300, 40], dtype, seed=99, spare=60, max_pages=64)[0] for _ in range(2)]
+    lens = torch.tensor(new, dtype=torch.int32, device="cuda")
+    rows = [torch.randn(n, (G + 2) * H, d, device="cuda").to(dtype) for _ in range(4)]
+    x = rows[0].clone()
+
+    def step(cache, x):
+        cu, slots = mf.mustafar_paged_plan(cache, lens, n)
+        mf.mustafar_paged_write(cache, x[:, H * G:H * (G + 1)], x[:, H * (G + 1):], slots)
+        return mf.mustafar_paged_attn(x[:, :H * G], cache, cu, max_q=max(new), max_tokens=900)
+
+    state = caches[0].state.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(caches[0], x)
+    assert torch.equal(caches[0].state, state)
+    for r in range(4):
+        x.copy_(rows[r])
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        want = step(caches[1], rows[r])
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and bool((got[-3:] == 0).all()), r
+        assert all(c.status.tolist() == [0] for c in caches) and torch.equal(caches[0].state, caches[1].state)
