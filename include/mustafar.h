@@ -525,7 +525,10 @@ int mustafar_window_step_grouped(mustafar_window_t* w, mustafar_ccache_t* Kc, mu
  * n_pages free pages, every page on the stack; tables need no setting). A model has a
  * cache a layer: keys and values of its own, and the same table, state and stack, so
  * that one plan a step, of any of them, is every layer's. */
-enum mustafar_type { MUSTAFAR_FP16 = 0, MUSTAFAR_BF16 = 1 };
+enum mustafar_type {
+    MUSTAFAR_FP16 = 0, MUSTAFAR_BF16 = 1,
+    MUSTAFAR_E4M3 = 2, MUSTAFAR_INT8 = 3    /* codes of the paged cache of 8 bits, below */
+};
 
 #define MUSTAFAR_PAGED_MAX_BATCH 4096       /* entries of a paged cache               */
 #define MUSTAFAR_PAGED_MAX_STEP (1 << 19)   /* slots of a step, and pages of an entry */
@@ -541,7 +544,7 @@ typedef struct mustafar_pages {
     int32_t page_tokens;      /* 16 to 1024, a power of two                        */
     int32_t n_pages;          /* n_pages * page_tokens < 2^31                      */
     int32_t max_pages;        /* of an entry                                       */
-    int32_t type;             /* mustafar_type of k and v                          */
+    int32_t type;             /* mustafar_type of k and v (FP16 or BF16)           */
     int64_t page_stride, head_stride, token_stride;
 } mustafar_pages_t;
 
@@ -647,6 +650,132 @@ int mustafar_paged_attn(const void* q, int64_t q_stride, int n_q, int Hq, const 
                         const void* cu, int window, int sinks, float scale, void* out,
                         int64_t out_stride, int max_q, int max_tokens, int n_splits, void* ws,
                         size_t ws_bytes, void* stream);
+
+/* THE PAGED CACHE IN 8 BITS. As the paged dense cache, with half its bytes: a value is
+ * code * 2^(scale - 127), one scale byte for block_tokens tokens of a kv-head's keys and
+ * one for their values, so that every value that is held is one of the 16-bit type and
+ * the products of the attention take it as it is.
+ *   pages     the descriptor of the dense cache, where k and v are codes (one byte an
+ *             element: strides and the addresses are multiples of 16 bytes, and a page
+ *             is under 2^30) and type says which:
+ *               MUSTAFAR_E4M3  8-bit floating point, 4 bits of exponent, 3 of mantissa,
+ *                              no infinities, magnitudes up to 448
+ *               MUSTAFAR_INT8  -127 to 127
+ *             mustafar_paged_plan and mustafar_rope take &p->pages; the dense cache's
+ *             other calls refuse it
+ *   k_scale, v_scale  [n_pages][H][page_tokens / block_tokens] bytes: 127 + the exponent
+ *   type      MUSTAFAR_FP16 or MUSTAFAR_BF16, of the tokens that are written, of queries
+ *             and outputs
+ * A block is quantised with the least exponent that takes its largest magnitude to a code
+ * (448 or 127), but at least -110, in fp16 -15 (e4m3) and -24 (int8: no smaller step is
+ * needed for any fp16 value). Codes are rounded to nearest, ties to even. Magnitudes over
+ * the largest that can be held, infinities among them, are held as it: 61440 (e4m3) and
+ * 65024 (int8) in fp16, 240 * 2^120 and 127 * 2^121 in bf16. NaN stays NaN in e4m3 and is
+ * held as 0 in int8; it does not count for the exponent. Tables, state and stack are set
+ * as those of the dense cache; codes and scales need no setting. */
+typedef struct mustafar_pages8 {
+    mustafar_pages_t pages;
+    uint8_t* k_scale;
+    uint8_t* v_scale;
+    int32_t type;             /* mustafar_type of tokens, queries and outputs      */
+    int32_t block_tokens;     /* 16, 32 or 64, at most page_tokens                 */
+} mustafar_pages8_t;
+
+/* Fills *p for caller-allocated buffers (host only; touches no buffer). code:
+ * MUSTAFAR_E4M3 or MUSTAFAR_INT8. Errors: EINVAL (as mustafar_paged_init). */
+int mustafar_paged8_init(mustafar_pages8_t* p, void* k, void* v, void* k_scale, void* v_scale,
+                         void* table, void* state, void* free_pages, int B, int H, int d,
+                         int page_tokens, int n_pages, int max_pages, int type, int code,
+                         int block_tokens, int64_t page_stride, int64_t head_stride,
+                         int64_t token_stride);
+
+/* Quantises the keys and values of a planned step into the entries' pages. cu [B + 1]
+ * (int32 device, ascending from 0: mustafar_paged_plan's) divides the n_new rows of k_new
+ * and v_new among the entries; the rows of entry b are its last cu[b+1] - cu[b] tokens, as
+ * in mustafar_paged_attn. Rows from cu[B] on, rows before an entry's first token and tokens
+ * whose page is outside [0, n_pages) are left out. k_new, v_new: p->type, layout as for
+ * mustafar_paged_write.
+ * A block of which no earlier token is left takes its exponent from the new tokens alone.
+ * One that holds earlier tokens keeps its exponent or, if the new ones need a larger one,
+ * gets theirs: the earlier codes are then rounded once more, to the new step (exact for
+ * e4m3 values of at least 2^-6 steps; what an int8 value is off after any number of such
+ * steps is under one of the last step, half of it for each at the step it was made). The
+ * same step written again gives the same codes. Errors: EINVAL. */
+int mustafar_paged8_write(const mustafar_pages8_t* p, const void* k_new, int64_t k_stride,
+                          const void* v_new, int64_t v_stride, const void* cu, int n_new,
+                          void* stream);
+
+/* As mustafar_paged_gather: the entries' tokens as dense fp16 tensors. Values of a bf16
+ * cache are rounded to the nearest fp16, magnitudes over 65504 to 65504. */
+int mustafar_paged8_gather(const mustafar_pages8_t* p, const void* first, void* x_k, void* x_v,
+                           int n_max, void* stream);
+
+/* As mustafar_paged_attn_workspace_bytes, with the same bound. */
+size_t mustafar_paged8_attn_workspace_bytes(const mustafar_pages8_t* p, int Hq, int n_q, int max_q,
+                                            int max_tokens, int n_splits);
+
+/* As mustafar_paged_attn, over the values that the codes stand for (q and out of
+ * p->type); all that is said there holds here. Tokens that no row sees may hold any codes
+ * and their blocks any scales. */
+int mustafar_paged8_attn(const void* q, int64_t q_stride, int n_q, int Hq,
+                         const mustafar_pages8_t* p, const void* cu, int window, int sinks,
+                         float scale, void* out, int64_t out_stride, int max_q, int max_tokens,
+                         int n_splits, void* ws, size_t ws_bytes, void* stream);
+
+/* ROTARY POSITIONS, of queries and keys before keys are cached. Pair i of a head's first
+ * rot channels, (x_a, x_b), at position p becomes
+ *   m * (x_a cos(p r_i) - x_b sin(p r_i),  x_a sin(p r_i) + x_b cos(p r_i))
+ * with the rates r_i (radians per position) and the magnitude m; the head's other channels
+ * stay as they are. */
+enum mustafar_rope_layout {
+    MUSTAFAR_ROPE_HALF = 0,         /* pair i: channels i and i + rot / 2 */
+    MUSTAFAR_ROPE_INTERLEAVED = 1   /* pair i: channels 2 i and 2 i + 1   */
+};
+enum mustafar_rope_scaling {
+    MUSTAFAR_ROPE_PLAIN = 0,    /* r_i = base^(-2 i / rot)                                    */
+    MUSTAFAR_ROPE_LINEAR = 1,   /* r_i / factor: positions of a context `factor` times as long */
+    MUSTAFAR_ROPE_BASE = 2,     /* base * factor^(rot / (rot - 2)): r_0 stays, the last is
+                                 * divided by factor (rot > 2)                               */
+    MUSTAFAR_ROPE_TURNS = 3     /* r_i (g + (1 - g) / factor) with g = (n - low) / (high - low)
+                                 * within [0, 1], n = original_len r_i / (2 pi) the turns that
+                                 * the pair makes in original_len tokens: pairs of `high`
+                                 * turns and more stay, those of `low` and fewer are divided */
+};
+#define MUSTAFAR_ROPE_MAX_D 512
+
+typedef struct mustafar_rotation {
+    const double* rates;      /* device [rot / 2], 8-byte aligned                  */
+    int32_t rot;              /* rotated channels, even, 2 to d                    */
+    int32_t layout;           /* mustafar_rope_layout                              */
+    float magnitude;          /* m                                                 */
+} mustafar_rotation_t;
+
+/* rates [rot / 2] (HOST memory) of a mustafar_rotation. factor > 0 (not looked at in
+ * PLAIN), original_len > 0 and low < high in TURNS alone. Errors: EINVAL (also rot < 2 or
+ * odd or over MUSTAFAR_ROPE_MAX_D, a base or factor that is not finite and over 0, rates
+ * that are not finite). */
+int mustafar_rope_rates(double* rates, int rot, double base, int scaling, double factor,
+                        double original_len, double low_turns, double high_turns);
+
+/* Rotates the n rows of q (Hq heads) and of k (H heads): fp16 or bf16 (type), d channels a
+ * head (a multiple of 8, at most MUSTAFAR_ROPE_MAX_D), row t's heads * d elements at
+ * t * stride, 16-byte aligned, strides multiples of 8 (a packed projection is read in
+ * place). One of q and k may be NULL with 0 heads. Angles are reduced in 64 bits, so that far
+ * positions are as exact as near ones; the rotation is in fp32, rounded once.
+ *   positions  int32 device [n], any sign; or NULL: row t is a new token of the entry b of
+ *        a planned step whose range of cu [B + 1] holds t, at position state[b] -
+ *        cu[b+1] + t (p: its pages, of any type), and rows from cu[B] on are left as
+ *        they were. With positions, p and cu are NULL
+ *   inverse  nonzero: rotates back (angles negated), still times the magnitude: what the
+ *        rotation's transpose makes of a gradient
+ *   out_q, out_k  the same type and layout with strides of their own: q (k) itself with
+ *        its stride, or memory that overlaps none of the inputs
+ * Errors: EINVAL. */
+int mustafar_rope(const mustafar_rotation_t* r, const void* q, int64_t q_stride, int Hq,
+                  const void* k, int64_t k_stride, int H, int d, int n, int type,
+                  const void* positions, const mustafar_pages_t* p, const void* cu, int inverse,
+                  void* out_q, int64_t out_q_stride, void* out_k, int64_t out_k_stride,
+                  void* stream);
 
 /* Static message for a status code. */
 const char* mustafar_strerror(int status);

@@ -69,10 +69,24 @@ class pages_t(ctypes.Structure):
                 ("token_stride", ctypes.c_int64)]
 
 
+class pages8_t(ctypes.Structure):
+    """Mirror of ``mustafar_pages8_t``."""
+    _fields_ = [("pages", pages_t), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("type", ctypes.c_int32), ("block_tokens", ctypes.c_int32)]
+
+
+class rotation_t(ctypes.Structure):
+    """Mirror of ``mustafar_rotation_t``."""
+    _fields_ = [("rates", ctypes.c_void_p), ("rot", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("magnitude", ctypes.c_float)]
+
+
 PRUNE_MAGNITUDE, PRUNE_2_4, PRUNE_OUTPUT_AWARE = 0, 1, 2
 PRUNE_CHANNEL, PRUNE_CHANNEL_OUTPUT_AWARE = 3, 4
 ATTN_SPARSE, ATTN_DENSE = 0, 1
-FP16, BF16 = 0, 1
+FP16, BF16, E4M3, INT8 = 0, 1, 2, 3
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "turns": 3}
 PLAN_PAGES, PLAN_TABLE, PLAN_SLOTS, PLAN_STATE = 1, 2, 4, 8   # status bits of mustafar_paged_plan
 GROUP = 32  # tokens per group of per-channel value pruning
 
@@ -179,6 +193,22 @@ _SIGS = {
                                            ctypes.c_int, ctypes.c_float, ctypes.c_void_p, ctypes.c_int64,
                                            ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_void_p,
                                            ctypes.c_size_t, ctypes.c_void_p]),
+    "mustafar_paged8_init": (ctypes.c_int, [ctypes.POINTER(pages8_t)] + [ctypes.c_void_p] * 7 + [ctypes.c_int] * 9
+                             + [ctypes.c_int64] * 3),
+    "mustafar_paged8_write": (ctypes.c_int, [ctypes.POINTER(pages8_t), ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                             ctypes.c_int64, ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p]),
+    "mustafar_paged8_gather": (ctypes.c_int, [ctypes.POINTER(pages8_t)] + [ctypes.c_void_p] * 3
+                               + [ctypes.c_int, ctypes.c_void_p]),
+    "mustafar_paged8_attn_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(pages8_t)] + [ctypes.c_int] * 5),
+    "mustafar_paged8_attn": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_int,
+                                            ctypes.POINTER(pages8_t), ctypes.c_void_p, ctypes.c_int, ctypes.c_int,
+                                            ctypes.c_float, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_int,
+                                            ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "mustafar_rope_rates": (ctypes.c_int, [ctypes.POINTER(ctypes.c_double), ctypes.c_int, ctypes.c_double, ctypes.c_int]
+                            + [ctypes.c_double] * 4),
+    "mustafar_rope": (ctypes.c_int, [ctypes.POINTER(rotation_t)] + [ctypes.c_void_p, ctypes.c_int64, ctypes.c_int] * 2
+                      + [ctypes.c_int] * 3 + [ctypes.c_void_p, ctypes.POINTER(pages_t), ctypes.c_void_p, ctypes.c_int]
+                      + [ctypes.c_void_p, ctypes.c_int64] * 2 + [ctypes.c_void_p]),
     "mustafar_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     "mustafar_stream_read_sink_bytes": (ctypes.c_size_t, []),
     "mustafar_stream_read": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p,
@@ -624,20 +654,12 @@ class PagedCache:
             k = torch.zeros((n_pages, H, page_tokens, d), dtype=dtype, device=device)
         if v is None:
             v = torch.zeros_like(k)
-        if table is None:
-            table = torch.zeros((B, max_pages), dtype=torch.int32, device=device)
-        if state is None:
-            state = torch.zeros(B + 2, dtype=torch.int32, device=device)
-            state[B] = n_pages
-        if free is None:
-            free = torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device)
+        table, state, free = _page_state(B, n_pages, max_pages, k.device, table, state, free)
         for name, x in (("k", k), ("v", v)):
             if tuple(x.shape) != (n_pages, H, page_tokens, d) or x.dtype != dtype or x.stride(3) != 1:
                 raise ValueError(f"{name}: [{n_pages}][{H}][{page_tokens}][{d}] of {dtype} with contiguous channels expected")
         if k.stride() != v.stride():
             raise ValueError("k and v have the same strides")
-        for name, x, shape in (("table", table, (B, max_pages)), ("state", state, (B + 2,)), ("free", free, (n_pages,))):
-            _want(name, x, shape, torch.int32, k.device)
         _want("v", v, tuple(k.shape), dtype, k.device, dense=False)
         self.k, self.v, self.table, self.state, self.free = k, v, table, state, free
         self.dtype, self.device = dtype, k.device
@@ -670,20 +692,38 @@ def _want(name, x, shape, dtype, device, dense=True):
         raise ValueError(f"{name} is on {x.device}, the cache on {device}")
 
 
-def _current(cache):
+def _page_state(B, n_pages, max_pages, device, table, state, free):
+    """The tables, the state and the stack that are given, or those of an empty cache."""
+    import torch
+    if table is None:
+        table = torch.zeros((B, max_pages), dtype=torch.int32, device=device)
+    if state is None:
+        state = torch.zeros(B + 2, dtype=torch.int32, device=device)
+        state[B] = n_pages
+    if free is None:
+        free = torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device)
+    for name, x, shape in (("table", table, (B, max_pages)), ("state", state, (B + 2,)), ("free", free, (n_pages,))):
+        _want(name, x, shape, torch.int32, device)
+    return table, state, free
+
+
+def _current(cache, what="the cache is"):
     """The cache's device has to be the current one: the launches go there."""
     import torch
     if cache.device.index != torch.cuda.current_device():
-        raise ValueError(f"the cache is on {cache.device}, the current device is cuda:{torch.cuda.current_device()}")
+        raise ValueError(f"{what} on {cache.device}, the current device is cuda:{torch.cuda.current_device()}")
 
 
 def _rows(name, x, n, heads, cache):
     """Stride of the rows of x [n][heads][d] of the cache's type and device, whose rows are contiguous."""
-    d = cache.desc.d
-    if x.shape != (n, heads, d) or x.dtype != cache.dtype:
-        raise ValueError(f"{name}: [{n}][{heads}][{d}] of {cache.dtype} expected, not {tuple(x.shape)} of {x.dtype}")
-    if x.device != cache.device:
-        raise ValueError(f"{name} is on {x.device}, the cache on {cache.device}")
+    return _row_stride(name, x, n, heads, cache.desc.d, cache.dtype, cache.device)
+
+
+def _row_stride(name, x, n, heads, d, dtype, device):
+    if x.shape != (n, heads, d) or x.dtype != dtype:
+        raise ValueError(f"{name}: [{n}][{heads}][{d}] of {dtype} expected, not {tuple(x.shape)} of {x.dtype}")
+    if x.device != device:
+        raise ValueError(f"{name} is on {x.device}, the cache on {device}")
     rows, head, channel = x.stride()
     if n and (channel != 1 or (heads > 1 and head != d)):
         raise ValueError(f"{name}: rows of {heads} x {d} contiguous elements expected")
@@ -744,9 +784,13 @@ def mustafar_paged_gather(cache: PagedCache, n_max: int, first=None, x_k=None, x
     """The requests' tokens first[b] (int32 [B], None: 0) .. as dense fp16 x_k, x_v [B][H][n_max][d], the
     input of mustafar_window_prefill; rows behind a request's last are left as they were (0 in
     tensors that the call makes)."""
+    _current(cache)
+    return _gather("mustafar_paged_gather", cache, cache.desc, n_max, first, x_k, x_v, stream)
+
+
+def _gather(fn, cache, desc, n_max, first, x_k, x_v, stream):
     import torch
     shape = (cache.desc.B, cache.desc.H, int(n_max), cache.desc.d)
-    _current(cache)
     with _on_stream(stream):
         x_k = torch.zeros(shape, dtype=torch.float16, device=cache.device) if x_k is None else x_k
         x_v = torch.zeros(shape, dtype=torch.float16, device=cache.device) if x_v is None else x_v
@@ -754,8 +798,8 @@ def mustafar_paged_gather(cache: PagedCache, n_max: int, first=None, x_k=None, x
     _want("x_v", x_v, shape, torch.float16, cache.device)
     if first is not None:
         _want("first", first, (shape[0],), torch.int32, cache.device)
-    _check("mustafar_paged_gather", lib().mustafar_paged_gather(
-        ctypes.byref(cache.desc), _dptr(first), _dptr(x_k), _dptr(x_v), shape[2], _stream(stream)))
+    _check(fn, getattr(lib(), fn)(
+        ctypes.byref(desc), _dptr(first), _dptr(x_k), _dptr(x_v), shape[2], _stream(stream)))
     return x_k, x_v
 
 
@@ -774,12 +818,17 @@ def mustafar_paged_attn(q, cache: PagedCache, cu, max_q: int | None = None, max_
     row each if n_q <= B, else n_q; all that a table can hold); with bounds near the truth calls are faster.
     Returns out [n_q][Hq][d]; rows from cu[B] on (all of a refused plan's) are left as they were, 0 in a tensor that
     the call makes."""
+    _current(cache)
+    return _paged_attn("mustafar_paged_attn", mustafar_paged_attn_workspace_bytes, q, cache, cache.desc, cu, max_q, max_tokens,
+                       window, sinks, scale, out, n_splits, ws, stream)
+
+
+def _paged_attn(fn, workspace_bytes, q, cache, desc, cu, max_q, max_tokens, window, sinks, scale, out, n_splits, ws, stream):
     import torch
     if q.dim() != 3:
         raise ValueError(f"q: [n_q][Hq][{cache.desc.d}] expected, not {tuple(q.shape)}")
     n_q, Hq, d = q.shape
     B = cache.desc.B
-    _current(cache)
     max_q = (1 if n_q <= B else n_q) if max_q is None else max_q
     if max_tokens is None:
         max_tokens = min(cache.desc.max_pages, cache.desc.n_pages) * cache.desc.page_tokens
@@ -787,7 +836,7 @@ def mustafar_paged_attn(q, cache: PagedCache, cu, max_q: int | None = None, max_
     qs = _rows("q", q, n_q, Hq, cache)
     _want("cu", cu, (B + 1,), torch.int32, cache.device)
     if ws is None:
-        need = mustafar_paged_attn_workspace_bytes(cache, Hq, n_q, max_q, max_tokens, n_splits)
+        need = workspace_bytes(cache, Hq, n_q, max_q, max_tokens, n_splits)
         if need > 0:
             with _on_stream(stream):
                 ws = torch.empty(need, dtype=torch.uint8, device=cache.device)
@@ -797,11 +846,187 @@ def mustafar_paged_attn(q, cache: PagedCache, cu, max_q: int | None = None, max_
         with _on_stream(stream):
             out = torch.zeros((n_q, Hq, d), dtype=cache.dtype, device=cache.device)
     os_ = _rows("out", out, n_q, Hq, cache)
-    _check("mustafar_paged_attn", lib().mustafar_paged_attn(
-        _dptr(q), qs, n_q, Hq, ctypes.byref(cache.desc), _dptr(cu), window, sinks, float(scale), _dptr(out),
+    _check(fn, getattr(lib(), fn)(
+        _dptr(q), qs, n_q, Hq, ctypes.byref(desc), _dptr(cu), window, sinks, float(scale), _dptr(out),
         os_, max_q, max_tokens, int(n_splits), _dptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
         _stream(stream)))
     return out
+
+
+class PagedCache8:
+    """PagedCache in 8 bits: codes with a power of two for block_tokens tokens of a head.
+
+    k, v [n_pages][H][page_tokens][d] are codes (`code`: torch.float8_e4m3fn or torch.int8), k_scale and v_scale
+    [n_pages][H][page_tokens / block_tokens] (uint8) 127 + the exponents: a value is code * 2**(scale - 127), and
+    one of `dtype` (float16 or bfloat16), the type of the tokens written, of queries and outputs. table, state, free
+    and max_pages are PagedCache's, and mustafar_paged_plan and mustafar_rope take either.
+    """
+
+    def __init__(self, B: int, H: int, d: int, n_pages: int, page_tokens: int = 64, max_pages: int | None = None,
+                 dtype=None, device="cuda", code=None, block_tokens: int = 16, k=None, v=None, k_scale=None, v_scale=None,
+                 table=None, state=None, free=None):
+        import torch
+        dtype = dtype or torch.float16
+        code = code or (k.dtype if k is not None else torch.float8_e4m3fn)
+        types, codes = {torch.float16: FP16, torch.bfloat16: BF16}, {torch.float8_e4m3fn: E4M3, torch.int8: INT8}
+        if dtype not in types:
+            raise ValueError(f"tokens are float16 or bfloat16, not {dtype}")
+        if code not in codes:
+            raise ValueError(f"codes are float8_e4m3fn or int8, not {code}")
+        if block_tokens not in (16, 32, 64) or block_tokens > page_tokens:
+            raise ValueError(f"a block has 16, 32 or 64 tokens and no more than a page, not {block_tokens}")
+        device = k.device if k is not None else device
+        if max_pages is None:
+            max_pages = table.shape[-1] if table is not None and table.dim() else n_pages
+        shape, blocks = (n_pages, H, page_tokens, d), (n_pages, H, page_tokens // block_tokens)
+        if k is None:
+            k = torch.zeros(shape, dtype=torch.uint8, device=device).view(code)
+        if v is None:
+            v = torch.zeros_like(k.view(torch.uint8)).view(code)
+        if k_scale is None:
+            k_scale = torch.zeros(blocks, dtype=torch.uint8, device=device)
+        if v_scale is None:
+            v_scale = torch.zeros(blocks, dtype=torch.uint8, device=device)
+        table, state, free = _page_state(B, n_pages, max_pages, k.device, table, state, free)
+        for name, x in (("k", k), ("v", v)):
+            if tuple(x.shape) != shape or x.dtype != code or x.stride(3) != 1:
+                raise ValueError(f"{name}: [{n_pages}][{H}][{page_tokens}][{d}] of {code} with contiguous channels expected")
+        if k.stride() != v.stride():
+            raise ValueError("k and v have the same strides")
+        _want("v", v, shape, code, k.device, dense=False)
+        for name, x in (("k_scale", k_scale), ("v_scale", v_scale)):
+            _want(name, x, blocks, torch.uint8, k.device)
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.table, self.state, self.free = table, state, free
+        self.dtype, self.device, self.code = dtype, k.device, code
+        self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
+        self.desc8 = pages8_t()
+        _check("mustafar_paged8_init", lib().mustafar_paged8_init(
+            ctypes.byref(self.desc8), _dptr(k), _dptr(v), _dptr(k_scale), _dptr(v_scale), _dptr(table), _dptr(state),
+            _dptr(free), B, H, d, int(page_tokens), int(n_pages), int(max_pages), types[dtype], codes[code],
+            int(block_tokens), k.stride(0), k.stride(1), k.stride(2)))
+        self.desc = self.desc8.pages    # (a view: what the plan takes)
+
+    B, page_tokens, lens = PagedCache.B, PagedCache.page_tokens, PagedCache.lens
+
+    @property
+    def block_tokens(self) -> int:
+        return self.desc8.block_tokens
+
+
+def _codes(cache):
+    if not isinstance(cache, PagedCache8):
+        raise ValueError(f"a PagedCache8 expected, not {type(cache).__name__}")
+    _current(cache)
+
+
+def mustafar_paged8_write(cache: PagedCache8, k_new, v_new, cu, stream=None) -> None:
+    """k_new, v_new [n][H][d] (the cache's dtype; rows of a packed projection too), the last cu[b+1] - cu[b] tokens of
+    every request b of a planned step, quantised into its pages. A block that holds earlier tokens keeps its exponent, or
+    gets the larger one that the new tokens need and its codes are rounded to it. Rows from cu[B] on are left out."""
+    import torch
+    n, H = k_new.shape[0], cache.desc.H
+    _codes(cache)
+    ks, vs = _rows("k_new", k_new, n, H, cache), _rows("v_new", v_new, n, H, cache)
+    _want("cu", cu, (cache.desc.B + 1,), torch.int32, cache.device)
+    _check("mustafar_paged8_write", lib().mustafar_paged8_write(
+        ctypes.byref(cache.desc8), _dptr(k_new), ks, _dptr(v_new), vs, _dptr(cu), n, _stream(stream)))
+
+
+def mustafar_paged8_gather(cache: PagedCache8, n_max: int, first=None, x_k=None, x_v=None, stream=None):
+    """As mustafar_paged_gather: the values of the requests' tokens first[b] .. as dense fp16 [B][H][n_max][d]."""
+    _codes(cache)
+    return _gather("mustafar_paged8_gather", cache, cache.desc8, n_max, first, x_k, x_v, stream)
+
+
+def mustafar_paged8_attn_workspace_bytes(cache: PagedCache8, Hq: int, n_q: int, max_q: int, max_tokens: int,
+                                         n_splits: int = 0) -> int:
+    return lib().mustafar_paged8_attn_workspace_bytes(ctypes.byref(cache.desc8), int(Hq), int(n_q), _int32(max_q),
+                                                      _int32(max_tokens), int(n_splits))
+
+
+def mustafar_paged8_attn(q, cache: PagedCache8, cu, max_q: int | None = None, max_tokens: int | None = None,
+                         window: int = 0, sinks: int = 0, scale: float = 0.0, out=None, n_splits: int = 0, ws=None,
+                         stream=None):
+    """As mustafar_paged_attn, over the values that the codes stand for."""
+    _codes(cache)
+    return _paged_attn("mustafar_paged8_attn", mustafar_paged8_attn_workspace_bytes, q, cache, cache.desc8, cu, max_q, max_tokens,
+                       window, sinks, scale, out, n_splits, ws, stream)
+
+
+def mustafar_rope_rates(rot: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0,
+                        original_len: float = 0.0, low_turns: float = 1.0, high_turns: float = 32.0) -> list:
+    """Radians per position of the rot / 2 pairs. scaling: "plain" (base**(-2 i / rot)), "linear" (divided by factor),
+    "base" (a larger base, so that the slowest is divided by factor) or "turns" (pairs of up to low_turns turns in original_len
+    tokens are divided by factor, those of high_turns and more stay, the others lie between)."""
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling is one of {', '.join(ROPE_SCALINGS)}, not {scaling!r}")
+    rates = (ctypes.c_double * max(1, int(rot) // 2))()
+    _check("mustafar_rope_rates", lib().mustafar_rope_rates(rates, int(rot), float(base), ROPE_SCALINGS[scaling], float(factor),
+                                                            float(original_len), float(low_turns), float(high_turns)))
+    return list(rates)
+
+
+class Rope:
+    """Rotary positions of a model: the first rot channels of a head, in pairs `half` a rotation apart or `interleaved`,
+    with the rates of mustafar_rope_rates (or `rates` [rot / 2], float64) and a magnitude that the rotated channels are
+    multiplied by."""
+
+    def __init__(self, rot: int, base: float = 10000.0, layout: str = "half", scaling: str = "plain", factor: float = 1.0,
+                 original_len: float = 0.0, low_turns: float = 1.0, high_turns: float = 32.0, magnitude: float = 1.0,
+                 rates=None, device="cuda"):
+        import torch
+        if layout not in ROPE_LAYOUTS:
+            raise ValueError(f"layout is one of {', '.join(ROPE_LAYOUTS)}, not {layout!r}")
+        if rates is None:
+            rates = torch.tensor(mustafar_rope_rates(rot, base, scaling, factor, original_len, low_turns, high_turns),
+                                 dtype=torch.float64, device=device)
+        _want("rates", rates, (int(rot) // 2,), torch.float64, rates.device)
+        self.rates, self.device = rates, rates.device
+        self.desc = rotation_t(_dptr(rates), int(rot), ROPE_LAYOUTS[layout], float(magnitude))
+
+
+def mustafar_rope(rope: Rope, q, k=None, positions=None, cache=None, cu=None, inverse: bool = False, out_q=None, out_k=None,
+                  stream=None):
+    """q [n][Hq][d] and k [n][H][d] (float16 or bfloat16; rows of a packed projection too; k may be None) turned by
+    their positions [n] (int32), or by those of a planned step's new tokens: cache (a PagedCache or PagedCache8) and cu. Rows
+    from cu[B] on are left as they were, 0 in tensors that the call makes. inverse: turned back, which is the gradient.
+    Returns (out_q, out_k), new tensors unless given; out_q=q, out_k=k turns in place."""
+    import torch
+    types = {torch.float16: FP16, torch.bfloat16: BF16}
+    if q.dim() != 3 or q.dtype not in types:
+        raise ValueError(f"q: [n][Hq][d] of float16 or bfloat16 expected, not {tuple(q.shape)} of {q.dtype}")
+    n, Hq, d = q.shape
+    if k is not None and (k.dim() != 3 or k.shape[0] != n or k.shape[2] != d):
+        raise ValueError(f"k: [{n}][H][{d}] expected, not {tuple(k.shape)}")
+    if k is None and out_k is not None:
+        raise ValueError("out_k without k")
+    if (positions is None) == (cache is None) or (cache is None) != (cu is None):
+        raise ValueError("positions, or a cache and cu")
+    H = 0 if k is None else k.shape[1]
+    _current(rope, "rates are")
+    if positions is not None:
+        _want("positions", positions, (n,), torch.int32, rope.device)
+    else:
+        _current(cache)
+        _want("cu", cu, (cache.desc.B + 1,), torch.int32, rope.device)
+    side = []
+    for name, x, heads, out in (("q", q, Hq, out_q), ("k", k, H, out_k)):
+        if x is None:
+            side.append((None, 0, 0, None, 0))
+            continue
+        stride = _row_stride(name, x, n, heads, d, q.dtype, rope.device)
+        if out is None:
+            with _on_stream(stream):
+                make = torch.empty if cache is None else torch.zeros
+                out = make((n, heads, d), dtype=q.dtype, device=rope.device)
+        side.append((x, stride, heads, out, _row_stride(f"out_{name}", out, n, heads, d, q.dtype, rope.device)))
+    (_, qs, _, out_q, oqs), (_, ks, _, out_k, oks) = side
+    _check("mustafar_rope", lib().mustafar_rope(
+        ctypes.byref(rope.desc), _dptr(q), qs, Hq, _dptr(k), ks, H, d, n, types[q.dtype], _dptr(positions),
+        None if cache is None else ctypes.byref(cache.desc), _dptr(cu), int(bool(inverse)), _dptr(out_q), oqs, _dptr(out_k),
+        oks, _stream(stream)))
+    return out_q, out_k
 
 
 ROUTE_DEFAULT, ROUTE_WALKS, ROUTE_MATRIX_CORES = 0, 1, 2

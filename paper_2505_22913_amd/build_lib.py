@@ -22,11 +22,11 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libmustafar.so")
 SOURCES = ["api.hip", "compress.hip", "attention.hip", "attention_mfma.hip", "measure.hip", "paged_api.hip", "paged.hip",
-           "paged_attn.hip"]
+           "paged_attn.hip", "paged8_api.hip", "paged8.hip", "paged8_attn.hip", "rope.hip"]
 ARCH = "gfx950"
 # Per source: k_paged_chunk runs two waves a SIMD, one at d = 256; left to itself the compiler gives every
 # matrix product an AGPR result and copies the scores, which the vector units read, out of them.
-EXTRA_FLAGS = {"paged_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+EXTRA_FLAGS = {s: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for s in ("paged_attn.hip", "paged8_attn.hip")}
 
 
 def hipcc() -> str:

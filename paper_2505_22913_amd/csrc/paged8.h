@@ -1,0 +1,83 @@
+// Internal interface of the paged cache in 8 bits (paged8_api.hip and its kernels in paged8.hip
+// and paged8_attn.hip) and of rotary positions (rope.hip).
+#pragma once
+
+#include "paged.h"
+
+namespace mf {
+
+struct Paged8View {
+  PagedView p;  // k and v: codes, a byte each; bf16: the type of tokens, queries and outputs
+  uint8_t* k_scale;
+  uint8_t* v_scale;
+  int int8;  // codes are int8, else e4m3
+  int log2_block;
+};
+
+hipError_t launch_paged8_write(const Paged8View& c, const uint16_t* k_new, int64_t k_stride, const uint16_t* v_new,
+                               int64_t v_stride, const int32_t* cu, int n_new, hipStream_t s);
+hipError_t launch_paged8_gather(const Paged8View& c, const int32_t* first, uint16_t* x_k, uint16_t* x_v, int n_max,
+                                hipStream_t s);
+
+// p.k and p.v are the codes, p.bf16 the type of q and out.
+struct Paged8AttnArgs : PagedAttnArgs {
+  const uint8_t* k_scale;
+  const uint8_t* v_scale;
+  int int8, log2_block;
+};
+
+// As paged_kernels.
+inline PagedPlan paged8_kernels(const PagedView& p, int G, int n_q, int max_q, int64_t max_tokens, int n_splits) {
+  PagedPlan k = {0, 0, 0, 0, (int64_t)n_q * G * p.H, 0};
+  const int64_t requests = p.B < n_q ? p.B : n_q, full = ((int64_t)n_q * G + kFewRows - 1) / kFewRows;
+  const int64_t groups = (requests > full ? requests : full) * p.H, n = 1024 / groups, most = max_tokens / 64;
+  k.few = n_splits > 0 ? n_splits : (int)(n < 1 || most < 1 ? 1 : n < most ? n : most);
+  return k;
+}
+hipError_t launch_paged8_attn(const Paged8AttnArgs& a, hipStream_t s);
+
+// Blocks of tokens that hold the n_new rows of B requests, however they are divided, and k_paged8_write's workgroups for one: a wave
+// has 16 tokens of a head's keys or values, the waves of a block lie in one workgroup.
+constexpr int kWrite8Threads = 256, kWrite8Rows = 16;
+inline int64_t paged8_blocks(const PagedView& p, int log2_block, int n_new) {
+  return ((int64_t)n_new >> log2_block) + 2 * (int64_t)(p.B < n_new ? p.B : n_new);
+}
+inline int paged8_block_groups(const PagedView& p, int log2_block) {
+  const int heads = kWrite8Threads / kWaveSize * kWrite8Rows >> log2_block;  // of keys and values, a workgroup
+  return (2 * p.H + heads - 1) / heads;
+}
+
+struct RopeArgs {
+  const double* rates;
+  int rot, layout;
+  float magnitude;
+  int bf16, inverse;
+  const uint16_t* q;
+  const uint16_t* k;
+  uint16_t* out_q;
+  uint16_t* out_k;
+  int64_t q_stride, k_stride, out_q_stride, out_k_stride;
+  int Hq, H, d, n;
+  const int32_t* positions;  // or cu and state
+  const int32_t* cu;
+  const int32_t* state;
+  int B;
+  int64_t most;  // tokens that an entry can hold
+};
+// A workgroup of k_rope: kRopeTokens tokens of so many heads.
+constexpr int kRopeThreads = 256, kRopeTokens = 4, kMaxRopeHeads = 1 << 16;
+struct RopePlan {
+  int heads, head_groups;
+  int64_t groups;
+};
+inline RopePlan rope_plan(const RopeArgs& a) {
+  const int all = a.Hq + a.H;
+  RopePlan r;
+  r.heads = all < 8 ? all : 8;
+  r.head_groups = (all + r.heads - 1) / r.heads;
+  r.groups = ((int64_t)a.n + kRopeTokens - 1) / kRopeTokens * r.head_groups;
+  return r;
+}
+hipError_t launch_rope(const RopeArgs& a, const RopePlan& plan, hipStream_t s);
+
+}  // namespace mf

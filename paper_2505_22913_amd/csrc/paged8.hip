@@ -1,0 +1,198 @@
+// The paged cache in 8 bits (gfx950): a step's keys and values quantised into pages, requests' pages as
+// dense tensors.
+#include "codes.h"
+#include "paged8.h"
+
+namespace mf {
+
+// ------------------------------------------------------------------------------------------
+// k_paged8_write: a wave has 16 tokens of one head's keys or values, the waves of a block of tokens share a workgroup and
+// their largest magnitude. The new tokens are read once and stay in registers; the block's earlier codes are read only where the
+// new tokens raise its exponent. A workgroup's block is found in the requests' lengths, so that no two have the same one whatever
+// the step.
+// ------------------------------------------------------------------------------------------
+struct BlockTile {
+  int b, row0, first, last;  // request, the row of its first new token, the positions of its first and last
+  int block;                 // first position of the block (over `last`: nothing to do)
+};
+
+// New tokens of an entry: positions first .. last (last < first: none), of which `first` is row row0.
+__device__ __forceinline__ BlockTile new_tokens(const PagedView& p, int b, int cu, int next, int len, int n_new) {
+  BlockTile t;
+  const int n = min(next, n_new) - cu;
+  const int64_t most = (int64_t)p.max_pages << p.log2_page;
+  t.b = b;
+  t.last = (int)min((int64_t)max(len, 0), most) - 1;
+  t.first = max(t.last + 1 - max(n, 0), 0);
+  if (cu < 0) t.last = t.first - 1;
+  t.row0 = cu + n - (t.last + 1 - t.first);
+  t.block = 0;
+  return t;
+}
+
+__device__ __forceinline__ BlockTile block_tile(const PagedView& p, const int32_t* cu, int n_new, int log2_block, int tile) {
+  const int B = p.B, lane = (int)lane_id(), stride = (B + kWave - 1) / kWave;
+  auto entry = [&](int b) { return new_tokens(p, b, cu[b], cu[b + 1], p.state[b], n_new); };
+  auto blocks = [&](int b) {
+    const BlockTile t = entry(b);
+    return t.last < t.first ? 0u : (uint32_t)((t.last >> log2_block) - (t.first >> log2_block) + 1);
+  };
+  uint32_t n = 0;
+  for (int b = lane * stride; b < min((lane + 1) * stride, B); ++b) n += blocks(b);
+  uint32_t incl = wave_incl_scan(n), want = (uint32_t)tile;
+  if (want >= (uint32_t)__builtin_amdgcn_readlane((int)incl, kWave - 1)) return {0, 0, 0, -1, 0};
+  int at = __builtin_popcountll(ballot(incl <= want));
+  want -= (uint32_t)__builtin_amdgcn_readlane((int)(incl - n), at);
+  if (stride > 1) {
+    at *= stride;
+    n = lane < stride && at + lane < B ? blocks(at + lane) : 0u;
+    incl = wave_incl_scan(n);
+    const int x = __builtin_popcountll(ballot(incl <= want));
+    want -= (uint32_t)__builtin_amdgcn_readlane((int)(incl - n), x);
+    at += x;
+  }
+  BlockTile t = entry(__builtin_amdgcn_readfirstlane(at));
+  t.block = ((t.first >> log2_block) + (int)want) << log2_block;
+  return t;
+}
+
+template <int T, bool BF16, bool INT8>
+__global__ __launch_bounds__(kWrite8Threads) void k_paged8_write(Paged8View c, const uint16_t* k_new, int64_t k_stride,
+                                                                 const uint16_t* v_new, int64_t v_stride, const int32_t* cu,
+                                                                 int n_new, int groups) {
+  constexpr int kWaves = kWrite8Threads / kWave, kPieces = 8 * T, kRowsPerLoad = kWave / kPieces, kLoads = kWrite8Rows / kRowsPerLoad;
+  __shared__ float tops[kWaves];
+  const PagedView& p = c.p;
+  const int tile = (int)(blockIdx.x / groups), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), lane = (int)lane_id();
+  const int log2_waves = c.log2_block - 4;  // of a head's block
+  const int head = (int)(blockIdx.x % groups) * (kWaves >> log2_waves) + (wave >> log2_waves), sub = wave & ((1 << log2_waves) - 1);
+  const BlockTile t = block_tile(p, cu, n_new, c.log2_block, tile);
+  if (t.block > t.last) return;  // (all of the workgroup)
+  const int page = p.table[(int64_t)t.b * p.max_pages + (t.block >> p.log2_page)];
+  if ((uint32_t)page >= (uint32_t)p.n_pages) return;
+  const bool work = head < 2 * p.H, values = head >= p.H;
+  const int h = work ? values ? head - p.H : head : 0, place = t.block & ((1 << p.log2_page) - 1);
+  const uint16_t* const x_new = (values ? v_new : k_new) + h * p.d;
+  const int64_t x_stride = values ? v_stride : k_stride;
+  uint8_t* const codes = reinterpret_cast<uint8_t*>(values ? p.v : p.k) + (int64_t)page * p.page_stride + (int64_t)h * p.head_stride;
+  uint8_t* const scale = (values ? c.v_scale : c.k_scale) + (((int64_t)page * p.H + h) << (p.log2_page - c.log2_block)) + (place >> c.log2_block);
+  const bool older = t.block < t.first;
+  const uint32_t before = older && work ? *scale : 0u;
+  // Rows of this wave: positions t.block + 16 sub + kRowsPerLoad i + lane / kPieces.
+  const int row = kWrite8Rows * sub + lane / kPieces, c8 = 8 * (lane % kPieces);
+  u32x4 x[kLoads];
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int pos = t.block + row + kRowsPerLoad * i, r = t.row0 + pos - t.first;
+    x[i] = (u32x4){};
+    if (work && pos >= t.first && pos <= t.last && r < n_new) x[i] = *reinterpret_cast<const u32x4*>(x_new + r * x_stride + c8);
+  }
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      top = fmaxf(top, fmaxf(fabsf(to_float<BF16>(x[i][e] & 0xffffu)), fabsf(to_float<BF16>(x[i][e] >> 16))));  // (not NaN's)
+  top = wave_max(top);
+  if (log2_waves > 0) {
+    if (lane == 0) tops[wave] = top;
+    __syncthreads();
+    for (int i = 0; i < 1 << log2_waves; ++i) top = fmaxf(top, tops[(wave & ~((1 << log2_waves) - 1)) + i]);
+  }
+  if (!work) return;
+  const uint32_t byte = max(byte_for<BF16, INT8>(top), before);
+  if (older && byte != before) {
+    // 2^(before - byte), or, where that is no normal number, so little that every code becomes 0.
+    const float less = power_of((uint32_t)max((int)before - (int)byte + 127, 1));
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = row + kRowsPerLoad * i;
+      if (t.block + r >= t.first) continue;
+      u32x2* const at = reinterpret_cast<u32x2*>(codes + (int64_t)(place + r) * p.token_stride + c8);
+      u32x2 y = *at;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const f32x4 f = decode4<INT8>(y[e], less);
+        y[e] = encode4<INT8>(f[0], f[1], f[2], f[3]);
+      }
+      *at = y;
+    }
+  }
+  const float inverse = power_of(254u - byte);
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int r = row + kRowsPerLoad * i, pos = t.block + r;
+    if (pos < t.first || pos > t.last) continue;
+    *reinterpret_cast<u32x2*>(codes + (int64_t)(place + r) * p.token_stride + c8) =
+        (u32x2){encode_pairs<BF16, INT8>(x[i][0], x[i][1], inverse), encode_pairs<BF16, INT8>(x[i][2], x[i][3], inverse)};
+  }
+  if (lane == 0 && sub == 0) *scale = (uint8_t)byte;
+}
+
+template <int T>
+static hipError_t write8_launch(const Paged8View& c, const uint16_t* k_new, int64_t k_stride, const uint16_t* v_new,
+                                int64_t v_stride, const int32_t* cu, int n_new, hipStream_t s) {
+  const int groups = paged8_block_groups(c.p, c.log2_block);
+  auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)(paged8_blocks(c.p, c.log2_block, n_new) * groups)), dim3(kWrite8Threads), 0, s, c, k_new,
+                       k_stride, v_new, v_stride, cu, n_new, groups);
+  };
+  if (c.int8) c.p.bf16 ? launch(k_paged8_write<T, true, true>) : launch(k_paged8_write<T, false, true>);
+  else c.p.bf16 ? launch(k_paged8_write<T, true, false>) : launch(k_paged8_write<T, false, false>);
+  return hipGetLastError();
+}
+
+hipError_t launch_paged8_write(const Paged8View& c, const uint16_t* k_new, int64_t k_stride, const uint16_t* v_new,
+                               int64_t v_stride, const int32_t* cu, int n_new, hipStream_t s) {
+  switch (c.p.d) {
+    case 64: return write8_launch<1>(c, k_new, k_stride, v_new, v_stride, cu, n_new, s);
+    case 128: return write8_launch<2>(c, k_new, k_stride, v_new, v_stride, cu, n_new, s);
+    default: return write8_launch<4>(c, k_new, k_stride, v_new, v_stride, cu, n_new, s);
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// k_paged8_gather: 8 codes of a key row and of its value row a thread, a head's rows a run of workgroups.
+// ------------------------------------------------------------------------------------------
+template <bool INT8>
+__device__ __forceinline__ u32x2 codes_to_fp16(uint32_t codes, float scale) {
+  f32x4 x = decode4<INT8>(codes, scale);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = x[i] > 65504.f ? 65504.f : x[i] < -65504.f ? -65504.f : x[i];  // (NaN stays)
+  return (u32x2){pack2<false>(x[0], x[1]), pack2<false>(x[2], x[3])};
+}
+
+template <bool INT8>
+__global__ __launch_bounds__(256) void k_paged8_gather(Paged8View c, const int32_t* first, uint16_t* x_k, uint16_t* x_v,
+                                                      int n_max, uint32_t groups) {
+  const PagedView& p = c.p;
+  const uint32_t bh = blockIdx.x / groups, b = bh / p.H, h = bh - b * p.H, log2_dv = 31 - __builtin_clz(p.d / 8);
+  const int64_t i = (int64_t)(blockIdx.x - bh * groups) * 256 + threadIdx.x, j = i >> log2_dv;  // of the rows of b and h
+  const int64_t tok = j + (first ? max(first[b], 0) : 0);
+  if (j >= n_max || tok >= p.state[b] || tok >> p.log2_page >= p.max_pages) return;
+  int page = p.table[(int64_t)b * p.max_pages + (tok >> p.log2_page)];
+  if ((uint32_t)page >= (uint32_t)p.n_pages) page = 0;
+  const int place = (int)(tok & ((1 << p.log2_page) - 1));
+  const int64_t src = (int64_t)page * p.page_stride + (int64_t)h * p.head_stride + (int64_t)place * p.token_stride + 8 * (i & ((1 << log2_dv) - 1));
+  const int64_t block = (((int64_t)page * p.H + h) << (p.log2_page - c.log2_block)) + (place >> c.log2_block);
+  const int64_t dst = (int64_t)bh * n_max * p.d + 8 * i;
+  const u32x2 k = *reinterpret_cast<const u32x2*>(reinterpret_cast<const uint8_t*>(p.k) + src);
+  const u32x2 v = *reinterpret_cast<const u32x2*>(reinterpret_cast<const uint8_t*>(p.v) + src);
+  const float ks = power_of(c.k_scale[block]), vs = power_of(c.v_scale[block]);
+  const u32x2 k0 = codes_to_fp16<INT8>(k.x, ks), k1 = codes_to_fp16<INT8>(k.y, ks);
+  const u32x2 v0 = codes_to_fp16<INT8>(v.x, vs), v1 = codes_to_fp16<INT8>(v.y, vs);
+  *reinterpret_cast<u32x4*>(x_k + dst) = (u32x4){k0.x, k0.y, k1.x, k1.y};
+  *reinterpret_cast<u32x4*>(x_v + dst) = (u32x4){v0.x, v0.y, v1.x, v1.y};
+}
+
+hipError_t launch_paged8_gather(const Paged8View& c, const int32_t* first, uint16_t* x_k, uint16_t* x_v, int n_max,
+                                hipStream_t s) {
+  const int64_t groups = ((int64_t)n_max * (c.p.d / 8) + 255) / 256, bh = (int64_t)c.p.B * c.p.H;
+  auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)(bh * groups)), dim3(256), 0, s, c, first, x_k, x_v, n_max, (uint32_t)groups);
+  };
+  c.int8 ? launch(k_paged8_gather<true>) : launch(k_paged8_gather<false>);
+  return hipGetLastError();
+}
+
+}  // namespace mf

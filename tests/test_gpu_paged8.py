@@ -1,0 +1,619 @@
+"""The paged cache in 8 bits on the GPU: writes and gathers exactly, attention against float64, and a
+serving loop with rotary positions from prompts to compressed caches."""
+import random
+
+import pytest
+import torch
+
+import oracle
+import paper_2505_22913_amd as mf
+from oracle import paged8 as oracle8
+from tests.gpu_common import ATTN_TOL, announce, attn_error
+from tests.paged8_common import CODE, KIND, check, fill8, ints, tokens_of
+from tests.paged_common import starts
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = [torch.float16, torch.bfloat16]
+CODES = ["e4m3", "int8"]
+
+
+# ---- writes and gathers ------------------------------------------------------------------------
+def same(got, want):
+    return torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got.nan_to_num(0.0), want.nan_to_num(0.0))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("H,d,P,block,layout,packed", [(1, 64, 16, 16, "heads", False), (3, 128, 64, 16, "tokens", True),
+                                                       (2, 128, 64, 32, "heads", False), (5, 256, 128, 64, "heads", True),
+                                                       (2, 64, 64, 64, "tokens", False), (4, 256, 32, 16, "heads", True)])
+def test_steps_are_quantised(dtype, code, H, d, P, block, layout, packed):
+    """Steps that add tokens, take some back and replace requests: every held value is the oracle's, and so are the
+    dense tensors that are read back."""
+    rng, g = random.Random(d + block), torch.Generator().manual_seed(P + d)
+    B, n_pages = 5, 40 if P > 32 else 120
+    shape = (n_pages, H, P, d) if layout == "heads" else (n_pages, P, H, d)
+    pool = [torch.randint(0, 256, shape, generator=g, dtype=torch.uint8).cuda().view(CODE[code]) for _ in range(2)]
+    if layout == "tokens":
+        pool = [x.transpose(1, 2) for x in pool]
+    cache = mf.PagedCache8(B, H, d, n_pages, P, dtype=dtype, block_tokens=block, k=pool[0], v=pool[1], max_pages=n_pages)
+    want = [[oracle8.Stored(H, d, code, KIND[dtype], block) for _ in range(B)] for _ in range(2)]
+    for i in range(8):
+        announce(f"write8 {dtype} {code} H={H} d={d} P={P} block={block} step {i}")
+        lens = [x.values.shape[1] for x in want[0]]
+        new = [rng.choice([0, 1, 1, 2, rng.randint(1, 90)]) for _ in range(B)]
+        keep = [rng.choice([n, n, n, 0, rng.randint(0, n)]) if n < 150 else 0 for n in lens]
+        n = sum(new) + 3
+        x = torch.randn(n, 2 * H + (3 if packed else 0), d, generator=g) * 2.0 ** torch.randint(-6, 7, (n, 1, 1), generator=g)
+        x = x.to(dtype)
+        x[sum(new):] = float("nan")                      # a padded step
+        on = x.cuda()
+        cu, _ = mf.mustafar_paged_plan(cache, ints(new), n, keep=ints(keep))
+        assert cache.status.tolist() == [0]
+        mf.mustafar_paged8_write(cache, on[:, :H], on[:, H:2 * H], cu)
+        at = 0
+        for b, m in enumerate(new):
+            for w, stored in enumerate((want[0][b], want[1][b])):
+                stored.step(x[at:at + m, w * H:(w + 1) * H].transpose(0, 1), keep[b])
+            at += m
+        first = [rng.choice([0, rng.randint(0, 40)]) for _ in range(B)]
+        n_max = max(1, max(s.values.shape[1] for s in want[0]))
+        dense = [torch.full((B, H, n_max, d), 7.0, dtype=torch.float16, device="cuda") for _ in range(2)]
+        mf.mustafar_paged8_gather(cache, n_max, first=ints(first), x_k=dense[0], x_v=dense[1])
+        for w, which in enumerate(("k", "v")):
+            for b in range(B):
+                stored = want[w][b].values
+                assert same(tokens_of(cache, which, b).cpu(), stored), f"step {i}: {which} of request {b}"
+                m = max(0, stored.shape[1] - first[b])
+                assert same(dense[w][b, :, :m].cpu(), oracle8.to_fp16(stored[:, first[b]:]))
+                assert bool((dense[w][b, :, m:] == 7).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("code", CODES)
+def test_a_token_at_a_time(dtype, code):
+    """Blocks that fill up token by token while their exponents grow, and magnitudes that fall."""
+    H, d, B = 2, 64, 2
+    g = torch.Generator().manual_seed(1)
+    cache = mf.PagedCache8(B, H, d, 12, 16, dtype=dtype, code=CODE[code])
+    want = [[oracle8.Stored(H, d, code, KIND[dtype], 16) for _ in range(B)] for _ in range(2)]
+    for i in range(40):
+        x = torch.randn(B, 2 * H, d, generator=g)
+        x[0] *= 2.0 ** (i % 16 - 6)
+        x[1] *= 2.0 ** (9 - i % 16)
+        x = x.to(dtype)
+        cu, _ = mf.mustafar_paged_plan(cache, ints([1, 1]), 2)
+        on = x.cuda()
+        for _ in range(1 + i % 2):                       # (written again: the same codes)
+            mf.mustafar_paged8_write(cache, on[:, :H], on[:, H:], cu)
+        for b in range(B):
+            for w, which in enumerate(("k", "v")):
+                want[w][b].step(x[b, w * H:(w + 1) * H][:, None])
+                assert same(tokens_of(cache, which, b).cpu(), want[w][b].values), (i, b, which)
+
+
+SPECIAL = [0.0, -0.0, float("inf"), -float("inf"), float("nan"), 65504.0, -65504.0, 61440.0, 63488.0, 57344.0, 57376.0, 65024.0,
+           448.0, 464.0, 127.0, 127.5, 2.0 ** -14, 2.0 ** -24, -3 * 2.0 ** -24, 2.0 ** -10, 1.0, 1.0625, 1.1875, 0.5, 1.5, 2.5]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("which", range(7))
+def test_values_at_the_ends_of_the_types(dtype, code, which):
+    """Infinities, NaN, zeros, the largest and the smallest values, ties, in a block of their own and with others;
+    the value that is held is finite in the type."""
+    d = 64
+    rows = {0: SPECIAL, 1: [0.0], 2: [float("nan")], 3: [float("inf"), 1.0], 4: [2.0 ** -24, 2.0 ** -23, 3 * 2.0 ** -24],
+            5: [1.0 + i / 16 for i in range(16)] + [448.0], 6: [i + 0.5 for i in range(-20, 20)] + [127.0]}[which]
+    if dtype == torch.bfloat16 and which in (0, 4):
+        rows = rows + [3.3e38, -3.3e38, 2.0 ** 127, 1e-38, 2.0 ** -126, 2.0 ** -133][:6 if which == 0 else 0] + ([2.0 ** -126, 2.0 ** -120, 2.0 ** -117] if which == 4 else [])
+    for alone in (True, False):
+        x = torch.zeros(3, 2, d)
+        for i, value in enumerate(rows):
+            x[(i // d) % 3, :, i % d] = value
+        if not alone:
+            x[2] = torch.randn(1, d, generator=torch.Generator().manual_seed(2))
+        x = x.to(dtype)
+        cache = mf.PagedCache8(1, 1, d, 2, 16, dtype=dtype, code=CODE[code])
+        cu, _ = mf.mustafar_paged_plan(cache, ints([3]), 3)
+        mf.mustafar_paged8_write(cache, x[:, :1].cuda(), x[:, 1:].cuda(), cu)
+        stored = oracle8.Stored(1, d, code, KIND[dtype], 16)
+        stored.step(x[:, :1].transpose(0, 1))
+        x_k, x_v = mf.mustafar_paged8_gather(cache, 3)
+        for w, dense in (("k", x_k), ("v", x_v)):
+            got = tokens_of(cache, w, 0).cpu()
+            assert same(got, stored.values)
+            assert same(got, got.to(dtype).double()) and not bool(torch.isinf(got.to(dtype)).any())
+            assert same(dense[0].cpu(), oracle8.to_fp16(stored.values))
+
+
+@pytest.mark.parametrize("code", CODES)
+def test_what_a_step_does_not_write_stays(code):
+    """Rows behind cu[B], a refused plan, rows before a request's first token, pages outside the pool."""
+    H, d, P, B = 2, 128, 16, 4
+    cache, _, _ = fill8(B, H, d, P, [40, 3, 0, 33], torch.float16, code, 16, seed=3)
+    before = [x.clone() for x in (cache.k.view(torch.uint8), cache.v.view(torch.uint8), cache.k_scale, cache.v_scale)]
+
+    def changed():
+        now = (cache.k.view(torch.uint8), cache.v.view(torch.uint8), cache.k_scale, cache.v_scale)
+        return [not torch.equal(x, y) for x, y in zip(now, before)]
+    x = torch.randn(50, H, d, device="cuda").half()
+    mf.mustafar_paged8_write(cache, x, x, ints([0, 0, 0, 0, 0]))
+    assert changed() == [False] * 4
+    cu, _ = mf.mustafar_paged_plan(cache, ints([5000, 0, 0, 0]), 50)
+    assert cache.status.tolist() != [0]
+    mf.mustafar_paged8_write(cache, x, x, cu)
+    assert changed() == [False] * 4
+    table = cache.table.clone()
+    cache.table[0] = cache.desc.n_pages                  # request 0's pages are bad ones: left out
+    cache.table[3, 2] = -7
+    mf.mustafar_paged8_write(cache, x[:40], x[:40], ints([0, 39, 39, 39, 40]))
+    assert changed() == [False] * 4
+    cache.table.copy_(table)
+    # request 1 has 3 tokens and 10 rows: the last 3 are its tokens; request 2 has none and 5 rows
+    mf.mustafar_paged8_write(cache, x, x, ints([0, 0, 10, 15, 15]))
+    want = oracle8.Stored(H, d, code, "fp16", 16)
+    want.step(x[7:10].transpose(0, 1).cpu())
+    assert same(tokens_of(cache, "k", 1).cpu(), want.values) and same(tokens_of(cache, "v", 1).cpu(), want.values)
+    page = int(cache.table[1, 0])
+    for now, was in zip((cache.k.view(torch.uint8), cache.v.view(torch.uint8), cache.k_scale, cache.v_scale), before):
+        now, was = now.clone(), was.clone()
+        if now.dim() == 4:
+            assert torch.equal(now[page, :, 3:], was[page, :, 3:])
+        now[page] = was[page]
+        assert torch.equal(now, was)
+
+
+def test_as_many_requests_as_there_can_be():
+    """4096 requests, some with rows: a wave has 64 of them a lane."""
+    B, d = 4096, 64
+    rng = random.Random(4)
+    new = [rng.choice([0, 0, 1, 2, 17]) for _ in range(B)]
+    new[-1] = 40
+    cache = mf.PagedCache8(B, 1, d, sum((n + 15) // 16 for n in new) + 5, 16, max_pages=4)
+    cu, _ = mf.mustafar_paged_plan(cache, ints(new), sum(new))
+    x = torch.randn(sum(new), 2, d, device="cuda").half()
+    mf.mustafar_paged8_write(cache, x[:, :1], x[:, 1:], cu)
+    x_k, x_v = mf.mustafar_paged8_gather(cache, 40)
+    at, cpu = 0, x.cpu()
+    for b, n in enumerate(new):
+        if n and (b % 37 == 0 or b == B - 1):
+            for w, dense in enumerate((x_k, x_v)):
+                want = oracle8.Stored(1, d, "e4m3", "fp16", 16)
+                want.step(cpu[at:at + n, w:w + 1].transpose(0, 1))
+                assert same(dense[b, :, :n].cpu(), oracle8.to_fp16(want.values)), b
+        at += n
+    # every request's largest value is held to half a step of e4m3
+    rows = torch.repeat_interleave(torch.arange(B, device="cuda"), ints(new))
+    place = torch.arange(sum(new), device="cuda") - cu[rows].long()
+    err = (x_k[rows, 0, place].float() - x[:, 0].float()).abs()
+    assert bool((err <= x[:, 0].float().abs() * 2.0 ** -4 + 2.0 ** -10).all())
+
+
+# ---- attention ---------------------------------------------------------------------------------
+def attend(dtype, code, H, G, d, P, block, cached, new, window=0, sinks=0, scale=0.0, n_splits=0, seed=0, layout="heads",
+           packed=False, junk=None, k_scale=0, **hints):
+    lens = [a + b for a, b in zip(cached, new)]
+    announce(f"attend8 {dtype} {code} H={H} G={G} d={d} P={P} block={block} cached={cached} new={new} window={window} "
+             f"sinks={sinks} splits={n_splits} layout={layout} packed={packed}")
+    cache, ks, vs = fill8(len(new), H, d, P, lens, dtype, code, block, seed=seed, layout=layout, junk=junk, k_scale=k_scale)
+    g = torch.Generator().manual_seed(seed + 1)
+    n_q = sum(new)
+    x = torch.randn(n_q, H * G + (2 * H if packed else 0), d, generator=g).to(dtype).cuda()
+    q = x[:, :H * G]
+    out = torch.full((n_q, H * G + (1 if packed else 0), d), 9.0, dtype=dtype, device="cuda")[:, :H * G]
+    got = mf.mustafar_paged8_attn(q, cache, starts(new), window=window, sinks=sinks, scale=scale, n_splits=n_splits, out=out,
+                                  **hints)
+    torch.cuda.synchronize()
+    worst = check(got, q, ks, vs, new, lens, dtype, window, sinks, scale if scale > 0 else None, label="attend8")
+    announce(f"  2-norm of the error: {worst:.2f} half steps of the type")
+    return got, q, cache, ks, vs
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("H,G", [(2, 1), (1, 2), (2, 4), (1, 8), (1, 5), (1, 64)])
+def test_single_tokens(dtype, code, d, H, G):
+    attend(dtype, code, H, G, d, 16, 16, [0, 1, 15, 63, 64, 200, 777], [1] * 7, seed=d + G)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("H,G", [(2, 1), (1, 3), (1, 8)])
+@pytest.mark.parametrize("P,block", [(16, 16), (64, 64), (256, 32)])
+def test_chunks_of_prompts(dtype, code, d, H, G, P, block):
+    attend(dtype, code, H, G, d, P, block, [0, 100, 0, 7, 63], [130, 65, 1, 33, 200], seed=d + G + P)
+
+
+@pytest.mark.parametrize("dtype,code", [(torch.float16, "int8"), (torch.bfloat16, "e4m3")])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (7, 3), (64, 4), (100, 0), (33, 70), (1000, 100), (2 ** 31 - 1, 3)])
+@pytest.mark.parametrize("new", [[1, 1, 1, 1], [70, 1, 0, 300]])
+def test_windows_and_sinks(dtype, code, window, sinks, new):
+    attend(dtype, code, 2, 2, 128, 32, 32, [5, 400, 90, 130], new, window=window, sinks=sinks, seed=window % 1000)
+
+
+@pytest.mark.parametrize("dtype,code,d,n_splits", [(torch.float16, "e4m3", 64, 0), (torch.bfloat16, "int8", 64, 20),
+                                                   (torch.float16, "int8", 128, 3), (torch.bfloat16, "e4m3", 128, 20),
+                                                   (torch.float16, "e4m3", 256, 5), (torch.bfloat16, "e4m3", 256, 70)])
+@pytest.mark.parametrize("B", [20, 65, 130])
+def test_many_requests_of_single_tokens_and_a_few_chunks(dtype, code, d, n_splits, B):
+    rng = random.Random(B + n_splits)
+    cached = [rng.choice([0, 1, 30, 64, 200]) for _ in range(B)]
+    new = [1] * B
+    for b, n in ((0, 0), (3, 40), (B - 2, 70), (B - 1, 5)):
+        new[b] = n
+    attend(dtype, code, 2, 4, d, 16, 16, cached, new, n_splits=n_splits, seed=B)
+    attend(dtype, code, 2, 4, d, 16, 16, cached, [min(n, 1) for n in new], n_splits=n_splits, seed=B)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("n_splits", [1, 2, 7, 64, 129, 700])
+@pytest.mark.parametrize("new,window,sinks", [([1, 1, 1], 0, 0), ([40, 1, 200], 0, 0), ([40, 1, 200], 130, 65)])
+def test_splits(d, n_splits, new, window, sinks):
+    attend(torch.bfloat16, "int8", 2, 4, d, 64, 16, [2900, 3, 300], new, window=window, sinks=sinks, n_splits=n_splits, seed=n_splits)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("new", [[1, 1], [50, 150]])
+def test_layouts_and_packed_rows(dtype, code, new):
+    attend(dtype, code, 2, 4, 128, 32, 32, [100, 300], new, layout="tokens", packed=True, seed=3, scale=0.05)
+
+
+@pytest.mark.parametrize("dtype,new", [(torch.bfloat16, [1, 1, 1]), (torch.float16, [1, 300, 64])])
+@pytest.mark.parametrize("code", CODES)
+def test_long_requests(dtype, code, new):
+    attend(dtype, code, 2, 4, 128, 64, 64, [20000, 9000, 131], new, seed=10)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("new", [[1, 1], [70, 33]])
+@pytest.mark.parametrize("k_scale", [5, 10])
+def test_large_scores(dtype, code, new, k_scale):
+    """Scores of hundreds and of tens of thousands: one token takes nearly all the weight."""
+    attend(dtype, code, 1, 4, 128, 16, 16, [300, 50], new, k_scale=k_scale, seed=6)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("v_scale", [-90, -14, 10, 100])
+@pytest.mark.parametrize("new", [[1, 1], [70, 33]])
+def test_blocks_of_very_different_exponents(dtype, code, v_scale, new):
+    """Values of some blocks far under or over the others', to the ends of the type."""
+    least, most = {("fp16", "e4m3"): (112, 134), ("fp16", "int8"): (103, 135), ("bf16", "e4m3"): (17, 246), ("bf16", "int8"): (17, 247)}[KIND[dtype], code]
+    cache, ks, _ = fill8(2, 1, 64, 16, [300, 90], dtype, code, 16, seed=7)
+    byte = cache.v_scale
+    byte[::3] = torch.clamp(byte[::3].int() + v_scale, least, most).to(torch.uint8)
+    vs = [tokens_of(cache, "v", b).to(dtype) for b in range(2)]
+    q = torch.randn(sum(new), 2, 64, device="cuda").to(dtype)
+    got = mf.mustafar_paged8_attn(q, cache, starts(new))
+    check(got, q, ks, vs, new, [300, 90], dtype, label="exponents")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("code,junk", [("e4m3", 0x7f), ("e4m3", 0xff), ("e4m3", 0x7e), ("int8", 0x80)])
+@pytest.mark.parametrize("new", [[1, 1, 1], [90, 1, 17]])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (20, 3)])
+def test_what_no_row_sees_takes_no_part(dtype, code, junk, new, window, sinks):
+    """Pages' unwritten rows hold NaN, blocks without tokens exponents beyond fp32; table entries of pages out of every
+    row's sight are bad, and so are their blocks' exponents."""
+    cached = [200, 17, 64]
+    lens = [a + b for a, b in zip(cached, new)]
+    cache, ks, vs = fill8(3, 2, 128, 16, lens, dtype, code, 16, seed=2, junk=junk)
+    if window:
+        for b, (n, L) in enumerate(zip(new, lens)):
+            for i in range((L + 15) // 16):
+                if i * 16 >= sinks and i * 16 + 15 <= L - n - window:
+                    page = int(cache.table[b, i])
+                    cache.k_scale[page], cache.v_scale[page] = 255, 255
+                    cache.v.view(torch.uint8)[page] = junk
+                    cache.table[b, i] = random.Random(i).choice([page, -1, 1 << 30])
+    q = torch.randn(sum(new), 8, 128, device="cuda").to(dtype)
+    got = mf.mustafar_paged8_attn(q, cache, starts(new), window=window, sinks=sinks)
+    check(got, q, ks, vs, new, lens, dtype, window, sinks, label="junk")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (30, 2)])
+@pytest.mark.parametrize("G", [1, 4])
+@pytest.mark.parametrize("bad", ["nan code", "inf q", "nan q"])
+def test_what_is_not_finite_reaches_the_rows_that_see_it(dtype, window, sinks, G, bad):
+    """A NaN code of a value (in another request of a key), or a query that is not finite, and no other row."""
+    cached, new = [70, 150, 10], [60, 100, 1]
+    lens = [a + b for a, b in zip(cached, new)]
+    cache, ks, vs = fill8(3, 1, 128, 16, lens, dtype, "e4m3", 16, seed=4)
+    q = torch.randn(sum(new), G, 128, device="cuda").to(dtype)
+    if bad == "nan code":
+        for b, j, which in ((0, 100, "v"), (1, 200, "k"), (2, 3, "v")):
+            page, at = int(cache.table[b, j // 16]), j % 16
+            (cache.v if which == "v" else cache.k).view(torch.uint8)[page, 0, at, 5] = 0x7f
+            (vs if which == "v" else ks)[b][0, j, 5] = float("nan")
+    else:
+        rows = [3, 61, 100, sum(new) - 1]
+        q[rows, 0, 7] = float(bad.split()[0])
+    got = mf.mustafar_paged8_attn(q, cache, starts(new), window=window, sinks=sinks)
+    if bad == "nan code":
+        check(got, q, ks, vs, new, lens, dtype, window, sinks, label="not finite")
+        return
+    assert bool(torch.isnan(got[rows, 0]).all())
+    clean, at = q.clone(), 0
+    clean[rows, 0, 7] = 0
+    want = mf.mustafar_paged8_attn(clean, cache, starts(new), window=window, sinks=sinks)
+    got, want = got.clone(), want.clone()
+    got[rows, 0] = want[rows, 0] = 0
+    check(got.index_put((torch.tensor(rows, device="cuda"), torch.tensor(0, device="cuda")), mf.mustafar_paged8_attn(
+        clean, cache, starts(new), window=window, sinks=sinks)[rows, 0]), clean, ks, vs, new, lens, dtype, window, sinks, label="others")
+
+
+@pytest.mark.parametrize("code", CODES)
+def test_rows_without_tokens_and_rows_behind_the_last(code):
+    """A request without new tokens, one that holds fewer tokens than it has rows, one that holds none; a padded batch; a
+    length beyond the table."""
+    for dtype in DTYPES:
+        cache, ks, vs = fill8(5, 2, 128, 16, [40, 0, 3, 70, 20], dtype, code, 16, seed=1)
+        new = [2, 3, 5, 0, 20]
+        q = torch.randn(40, 8, 128, device="cuda").to(dtype)
+        out = torch.full_like(q, 3.0)
+        mf.mustafar_paged8_attn(q, cache, starts(new), out=out)
+        check(out, q, ks, vs, new, [40, 0, 3, 70, 20], dtype, label="empty")
+        assert bool((out[30:] == 3).all())
+    cache, ks, vs = fill8(1, 1, 64, 16, [64], torch.float16, code, 16, seed=12, max_pages=4)
+    cache.state[0] = 70        # 64 tokens fit
+    q = torch.randn(1, 1, 64, device="cuda").half()
+    check(mf.mustafar_paged8_attn(q, cache, starts([1])), q, ks, vs, [1], [64], torch.float16, label="beyond")
+
+
+@pytest.mark.parametrize("new", [[1, 1], [64, 5]])
+def test_hints_only_choose(new):
+    for max_q, max_tokens in ((1, 1), (1, 5000), (64, 700), (1000, 100000), (0, 0)):
+        attend(torch.float16, "e4m3", 2, 4, 128, 16, 16, [500, 600], new, max_q=max_q, max_tokens=max_tokens, seed=11)
+
+
+@pytest.mark.parametrize("n_splits", [0, 5, 70])
+@pytest.mark.parametrize("new", [[1, 1, 1], [90, 1, 3], [40, 70, 33]])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_what_a_workspace_held_takes_no_part(d, new, n_splits):
+    """A workspace of NaN: ranges without tokens, requests shorter than there are ranges, rows that see nothing."""
+    cached = [3000, 2, 500]
+    lens = [a + b for a, b in zip(cached, new)]
+    cache, ks, vs = fill8(3, 2, d, 16, lens, torch.float16, "int8", 16, seed=60)
+    cache.state[1] = 1              # fewer tokens than rows, where there is more than one
+    lens[1], ks[1], vs[1] = 1, ks[1][:, :1], vs[1][:, :1]
+    q = torch.randn(sum(new), 8, d, device="cuda").half()
+    need = mf.mustafar_paged8_attn_workspace_bytes(cache, 8, sum(new), max(new), 4000, n_splits)
+    ws = torch.full((max(need, 16),), 255, dtype=torch.uint8, device="cuda")
+    got = mf.mustafar_paged8_attn(q, cache, starts(new), max_q=max(new), max_tokens=4000, n_splits=n_splits, ws=ws)
+    check(got, q, ks, vs, new, lens, torch.float16, label="workspace of NaN")
+
+
+@pytest.mark.parametrize("code", CODES)
+def test_pools_of_more_than_two_to_the_32_bytes(code):
+    """Pages whose offsets pass 32 bits: written, read back and attended to."""
+    H, d, P = 8, 256, 1024
+    n_pages = (1 << 32) // (H * d * P) + 40
+    pool = [torch.empty((n_pages, H, P, d), dtype=torch.uint8, device="cuda").view(CODE[code]) for _ in range(2)]
+    cache = mf.PagedCache8(2, H, d, n_pages, P, max_pages=4, k=pool[0], v=pool[1], dtype=torch.bfloat16, block_tokens=64)
+    new = [1500, 1030]
+    cu, _ = mf.mustafar_paged_plan(cache, ints(new), sum(new))
+    cache.table.copy_(n_pages - 1 - cache.table)    # the last pages of the pool
+    assert int(cache.table[0, 0]) == n_pages - 1 and (n_pages - 4) * H * P * d > 1 << 32
+    x = torch.randn(sum(new), 3 * H, d, device="cuda").bfloat16()
+    q, k, v = x[:, :H], x[:, H:2 * H], x[:, 2 * H:]
+    mf.mustafar_paged8_write(cache, k, v, cu)
+    ks, vs = ([tokens_of(cache, w, b).bfloat16() for b in range(2)] for w in ("k", "v"))
+    assert bool(((ks[0].transpose(0, 1).float() - k[:1500].float()).abs() <= 0.07 * k[:1500].float().abs() + 0.05).all())
+    got = mf.mustafar_paged8_attn(q[-1100:], cache, starts([70, 1030]))
+    check(got, q[-1100:], ks, vs, [70, 1030], new, torch.bfloat16, label="far pages")
+    x_k, _ = mf.mustafar_paged8_gather(cache, 1500)
+    assert torch.equal(x_k[0], ks[0].float().half())
+
+
+# ---- together ----------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,code,block", [(torch.float16, "e4m3", 16), (torch.bfloat16, "int8", 32), (torch.bfloat16, "e4m3", 64)])
+def test_a_serving_loop_from_prompts_to_compressed_caches(dtype, code, block):
+    """Prompts in chunks and single tokens through plan, rotary positions, write and attention, every step against float64;
+    then the pages become compressed caches and a window, whose decode attention is the oracle's."""
+    B, H, G, d, P, W = 3, 2, 4, 128, 64, 32
+    lens = [150, 77, 201]
+    g = torch.Generator().manual_seed(13)
+    cache = mf.PagedCache8(B, H, d, 20, P, max_pages=8, dtype=dtype, code=CODE[code], block_tokens=block)
+    rope = mf.Rope(96, 10000.0, "half", "turns", factor=4.0, original_len=128, magnitude=1.1)
+    rates = oracle8.rates(96, 10000.0, "turns", 4.0, 128)
+    stored = [[oracle8.Stored(H, d, code, KIND[dtype], block) for _ in range(B)] for _ in range(2)]
+    done = [0] * B
+    for chunk in (64, 50, 1, 1, 100):
+        new = [min(chunk, n - m) for n, m in zip(lens, done)]
+        n = sum(new) + 5                                    # a padded step
+        x = torch.randn(n, (G + 2) * H, d, generator=g).to(dtype)
+        on = x.cuda()
+        q, k, v = on[:, :G * H], on[:, G * H:G * H + H], on[:, G * H + H:]
+        cu, _ = mf.mustafar_paged_plan(cache, ints(new), n)
+        mf.mustafar_rope(rope, q, k, cache=cache, cu=cu, out_q=q, out_k=k)      # in place, in the packed projection
+        pos = torch.cat([torch.arange(m, m + a) for m, a in zip(done, new)])
+        turned, mag = oracle8.rotate(x[:sum(new), :G * H + H], pos, rates, 96, "half", 1.1)
+        u = torch.finfo(dtype).eps / 2
+        err = (on[:sum(new), :G * H + H].cpu().double() - turned).abs()
+        assert bool((err <= u * turned.abs() + 8 * 2.0 ** -24 * mag + 2.0 ** -25).all())
+        assert torch.equal(on[sum(new):].cpu(), x[sum(new):]) and torch.equal(v.cpu(), x[:, G * H + H:])
+        mf.mustafar_paged8_write(cache, k, v, cu)
+        out = mf.mustafar_paged8_attn(q, cache, cu, out=torch.full((n, G * H, d), 5.0, dtype=dtype, device="cuda"))
+        at = 0
+        for b, m in enumerate(new):
+            for w, rows in enumerate((k, v)):
+                stored[w][b].step(rows[at:at + m].transpose(0, 1).cpu())
+                assert same(tokens_of(cache, "kv"[w], b).cpu(), stored[w][b].values)
+            at += m
+        done = [m + a for m, a in zip(done, new)]
+        check(out, q, [s.values.to(dtype) for s in stored[0]], [s.values.to(dtype) for s in stored[1]], new, done, dtype,
+              label=f"chunk {chunk}")
+        assert bool((out[-5:] == 5).all())
+    assert done == lens
+    x_k, x_v = mf.mustafar_paged8_gather(cache, max(lens))
+    Kc, Vc, win = mf.CompressedCache(B, H, d, 0.5, 256), mf.CompressedCache(B, H, d, 0.7, 256), mf.DenseWindow(B, H, d, W)
+    mf.mustafar_window_prefill(win, Kc, Vc, x_k, x_v, lens)
+    q = torch.randn(B, H * G, d, device="cuda").half()
+    out = mf.mustafar_window_decode_attn(q, Kc, Vc, win).cpu().numpy()
+    for b, n in enumerate(lens):
+        kb, vb = (oracle8.to_fp16(s[b].values).numpy()[None] for s in stored)
+        want = oracle.sparse_decode_attention(q[b:b + 1].cpu().numpy(), oracle.compress(kb[:, :, :n - W].copy(), 0.5),
+                                              oracle.compress(vb[:, :, :n - W].copy(), 0.7), kb[:, :, n - W:].copy(), vb[:, :, n - W:].copy())
+        assert attn_error(out[b:b + 1], want) <= ATTN_TOL
+
+
+@pytest.mark.parametrize("dtype,code", [(torch.float16, "int8"), (torch.bfloat16, "e4m3")])
+def test_a_captured_step_replays(dtype, code):
+    """Plan, rotary positions, write and attention of a step in one graph, replayed with eager work between the replays:
+    every replay advances the state and gives what eager calls on a second cache give."""
+    B, H, G, d, P = 3, 2, 4, 128, 16
+    lens, add = [100, 31, 500], [1, 40, 9]
+    caches = [fill8(B, H, d, P, lens, dtype, code, 16, seed=14, spare=60, max_pages=64)[0] for _ in range(2)]
+    new, n = ints(add), 60
+    rope = mf.Rope(d, layout="interleaved")
+    rows = [torch.randn(n, (G + 2) * H, d, device="cuda").to(dtype) for _ in range(4)]
+    x = rows[0].clone()
+    cu, slots, status = torch.zeros(B + 1, dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda"), ints([0])
+    out, turned = torch.zeros(n, H * G, d, dtype=dtype, device="cuda"), torch.zeros(n, (G + 1) * H, d, dtype=dtype, device="cuda")
+    need = mf.mustafar_paged8_attn_workspace_bytes(caches[0], H * G, n, 40, 1000)
+    ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+
+    def step(cache, x, cu, slots, status, out, turned):
+        mf.mustafar_paged_plan(cache, new, n, cu=cu, slots=slots, status=status)
+        q, k = turned[:, :H * G], turned[:, H * G:]
+        mf.mustafar_rope(rope, x[:, :H * G], x[:, H * G:H * (G + 1)], cache=cache, cu=cu, out_q=q, out_k=k)
+        mf.mustafar_paged8_write(cache, k, x[:, H * (G + 1):], cu)
+        return mf.mustafar_paged8_attn(q, cache, cu, max_q=40, max_tokens=1000, out=out, ws=ws)
+
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        step(caches[0], x, cu, slots, status, out, turned)
+    for r in range(4):
+        x.copy_(rows[r])
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        want = step(caches[1], rows[r], cu.clone(), slots.clone(), status.clone(), torch.zeros_like(out), torch.zeros_like(turned))
+        torch.cuda.synchronize()
+        assert status.tolist() == [0] and caches[0].lens.tolist() == [a + (r + 1) * b for a, b in zip(lens, add)]
+        assert torch.equal(got, want), r
+        for b in range(B):
+            for w in ("k", "v"):
+                assert torch.equal(tokens_of(caches[0], w, b), tokens_of(caches[1], w, b))
+
+
+def test_a_workspace_that_two_captured_calls_share():
+    """Two graphs of calls of different sizes with one workspace, replayed in turns with eager calls between them."""
+    dtype, made = torch.bfloat16, []
+    for i, (cached, new) in enumerate((([3000, 40], [1, 1]), ([900, 100], [60, 1]))):
+        lens = [a + b for a, b in zip(cached, new)]
+        cache, ks, vs = fill8(2, 2, 128, 16, lens, dtype, "e4m3", 16, seed=40 + i)
+        made.append((cache, ks, vs, lens, new, torch.randn(sum(new), 8, 128, device="cuda").to(dtype), starts(new)))
+    need = max(mf.mustafar_paged8_attn_workspace_bytes(m[0], 8, sum(m[4]), max(m[4]), max(m[3])) for m in made)
+    assert need > 0
+    ws, graphs, outs = torch.empty(need, dtype=torch.uint8, device="cuda"), [], []
+
+    def call(m, out):
+        mf.mustafar_paged8_attn(m[5], m[0], m[6], max_q=max(m[4]), max_tokens=max(m[3]), out=out, ws=ws)
+    for m in made:
+        out = torch.zeros_like(m[5])
+        call(m, out)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call(m, out)
+        graphs.append(graph)
+        outs.append(out)
+    for i in (0, 1, 1, 0, 0, 1):
+        outs[i].fill_(9.0)
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        m = made[i]
+        check(outs[i], m[5], m[1], m[2], m[4], m[3], dtype, label=f"graph {i}")
+        again = torch.empty_like(m[5])
+        call(m, again)
+        assert torch.equal(again, outs[i])       # every call's sums are in one order
+
+
+def test_other_streams():
+    """Calls on streams that are not the current one, two at once."""
+    dtype = torch.float16
+    made = [fill8(2, 2, 128, 16, [700, 300], dtype, "e4m3", 16, seed=s) for s in (20, 21)]
+    qs = [torch.randn(130, 8, 128, device="cuda").to(dtype) for _ in range(2)]
+    cu, streams = starts([100, 30]), [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        outs = [mf.mustafar_paged8_attn(q, m[0], cu, stream=s) for q, m, s in zip(qs, made, streams)]
+        dense = [mf.mustafar_paged8_gather(m[0], 700, stream=s) for m, s in zip(made, streams)]
+        torch.cuda.synchronize()
+        for out, q, m, x in zip(outs, qs, made, dense):
+            check(out, q, m[1], m[2], [100, 30], [700, 300], dtype, label="streams")
+            assert torch.equal(x[0][0], m[1][0].half()) and torch.equal(x[1][1, :, :300], m[2][1].half())
+
+
+def test_layers_share_a_steps_table_state_and_stack():
+    """Two layers of 8 bits and a dense one behind one plan."""
+    B, H, d = 2, 2, 64
+    first = mf.PagedCache8(B, H, d, 20, 16, max_pages=8)
+    second = mf.PagedCache8(B, H, d, 20, 16, code=torch.int8, table=first.table, state=first.state, free=first.free)
+    third = mf.PagedCache(B, H, d, 20, 16, table=first.table, state=first.state, free=first.free)
+    for new in ([40, 3], [1, 1], [0, 30]):
+        cu, slots = mf.mustafar_paged_plan(first, ints(new), sum(new))
+        x = torch.randn(sum(new), 2 * H, d, device="cuda").half()
+        for layer in (first, second):
+            mf.mustafar_paged8_write(layer, x[:, :H], x[:, H:], cu)
+        mf.mustafar_paged_write(third, x[:, :H], x[:, H:], slots)
+    dense = mf.mustafar_paged_gather(third, 41)
+    for layer, step in ((first, 2.0 ** -4), (second, None)):
+        for got, want in zip(mf.mustafar_paged8_gather(layer, 41), dense):
+            err = (got.float() - want.float()).abs()
+            # e4m3: half a step relative to the value (and one of the grid's end); int8: half a step of at most 2 * 4.5 / 127, at
+            # most one whole for the tokens that later ones raised the exponent of
+            most = want.float().abs() * step + 2.0 ** -9 if step else torch.full_like(err, 0.08)
+            assert bool((err <= most).all())
+
+
+def test_the_binding_refuses_what_does_not_fit():
+    """Shapes, types, strides and devices are checked before anything is launched."""
+    cache, _, _ = fill8(2, 2, 64, 16, [20, 30], torch.float16, "e4m3", 16, seed=50)
+    dense = mf.PagedCache(2, 2, 64, 8, 16)
+    held = [x.clone() for x in (cache.k.view(torch.uint8), cache.v_scale)]
+    x = torch.zeros(2, 2, 64, dtype=torch.float16, device="cuda")
+    q, cu = torch.zeros(2, 4, 64, dtype=torch.float16, device="cuda"), starts([1, 1])
+    write = lambda **kw: mf.mustafar_paged8_write(**{**dict(cache=cache, k_new=x, v_new=x, cu=cu), **kw})  # noqa: E731
+    attn = lambda **kw: mf.mustafar_paged8_attn(**{**dict(q=q, cache=cache, cu=cu), **kw})  # noqa: E731
+    gather = lambda **kw: mf.mustafar_paged8_gather(**{**dict(cache=cache, n_max=4), **kw})  # noqa: E731
+    make = lambda **kw: mf.PagedCache8(**{**dict(B=2, H=2, d=64, n_pages=8, page_tokens=32), **kw})  # noqa: E731
+    byte = torch.zeros(8, 2, 2, dtype=torch.uint8, device="cuda")
+    bad = [(write, dict(k_new=x.bfloat16())), (write, dict(v_new=x[:1])), (write, dict(k_new=x.cpu())), (write, dict(k_new=x[:, :1])),
+           (write, dict(k_new=x.transpose(0, 1).contiguous().transpose(0, 1))), (write, dict(cu=cu[:2])), (write, dict(cu=cu.long())),
+           (write, dict(cu=cu.cpu())), (write, dict(cache=dense)), (attn, dict(cache=dense)), (gather, dict(cache=dense)),
+           (attn, dict(q=q.bfloat16())), (attn, dict(q=q[0])), (attn, dict(q=q[..., :32])), (attn, dict(q=q.cpu())),
+           (attn, dict(cu=cu[:2])), (attn, dict(out=q[:1])), (attn, dict(out=q.float())), (attn, dict(ws=torch.zeros(1 << 20))),
+           (gather, dict(first=ints([0]))), (gather, dict(x_k=x)), (gather, dict(x_k=torch.zeros(2, 2, 4, 64, device="cuda"))),
+           (make, dict(dtype=torch.float32)), (make, dict(code=torch.float8_e5m2)), (make, dict(block_tokens=8)),
+           (make, dict(block_tokens=64)), (make, dict(k_scale=byte[:7])), (make, dict(k_scale=byte.int())), (make, dict(v_scale=byte.cpu())),
+           (make, dict(k=torch.zeros(8, 2, 32, 64, dtype=torch.float16, device="cuda"))),
+           (make, dict(k=torch.zeros(8, 2, 64, 32, dtype=torch.int8, device="cuda").transpose(2, 3))),
+           (make, dict(k=torch.zeros(8, 2, 32, 64, dtype=torch.int8, device="cuda"), code=torch.float8_e4m3fn)),
+           (make, dict(state=ints([0, 0]))), (make, dict(table=ints([0])))]
+    for call, kw in bad:
+        with pytest.raises(ValueError):
+            call(**kw)
+    codes = torch.zeros(8, 2, 32, 64 + 8, dtype=torch.int8, device="cuda")
+    for call, kw in ((attn, dict(q=torch.zeros(2, 3, 64, dtype=torch.float16, device="cuda"))), (attn, dict(window=-1)),
+                     (attn, dict(n_splits=4, ws=torch.zeros(16, dtype=torch.uint8, device="cuda"))),
+                     (attn, dict(q=torch.zeros(2, 130, 64, dtype=torch.float16, device="cuda"))), (make, dict(d=96)),
+                     (make, dict(k=codes[..., :64], v=codes[..., :64])), (make, dict(page_tokens=48)),
+                     (mf.mustafar_paged_write, dict(cache=cache, k_new=x, v_new=x, slots=ints([0, 1]))),
+                     (mf.mustafar_paged_attn, dict(q=q, cache=cache, cu=cu)), (mf.mustafar_paged_gather, dict(cache=cache, n_max=4))):
+        with pytest.raises(mf.MustafarError):
+            call(**kw)
+    for call, kw in ((attn, dict(q=q[:0], cu=starts([0, 0]))), (write, dict(k_new=x[:0], v_new=x[:0])), (gather, dict(n_max=0))):
+        call(**kw)                                                                     # nothing to do
+    torch.cuda.synchronize()
+    assert torch.equal(cache.k.view(torch.uint8), held[0]) and torch.equal(cache.v_scale, held[1])
