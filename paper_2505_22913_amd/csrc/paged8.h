@@ -26,14 +26,6 @@ struct Paged8AttnArgs : PagedAttnArgs {
   int int8, log2_block;
 };
 
-// As paged_kernels.
-inline PagedPlan paged8_kernels(const PagedView& p, int G, int n_q, int max_q, int64_t max_tokens, int n_splits) {
-  PagedPlan k = {0, 0, 0, 0, (int64_t)n_q * G * p.H, 0};
-  const int64_t requests = p.B < n_q ? p.B : n_q, full = ((int64_t)n_q * G + kFewRows - 1) / kFewRows;
-  const int64_t groups = (requests > full ? requests : full) * p.H, n = 1024 / groups, most = max_tokens / 64;
-  k.few = n_splits > 0 ? n_splits : (int)(n < 1 || most < 1 ? 1 : n < most ? n : most);
-  return k;
-}
 hipError_t launch_paged8_attn(const Paged8AttnArgs& a, hipStream_t s);
 
 // Blocks of tokens that hold the n_new rows of B requests, however they are divided, and k_paged8_write's workgroups for one: a wave

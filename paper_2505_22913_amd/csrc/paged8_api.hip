@@ -83,7 +83,7 @@ int mustafar_paged8_gather(const mustafar_pages8_t* p, const void* first, void* 
 size_t mustafar_paged8_attn_workspace_bytes(const mustafar_pages8_t* p, int Hq, int n_q, int max_q, int max_tokens,
                                             int n_splits) {
   if (check_pages8(p) != MUSTAFAR_OK) return 0;
-  return attn_ws_bytes(view8_of(p).p, Hq, n_q, max_q, max_tokens, n_splits, paged8_kernels);
+  return attn_ws_bytes(view8_of(p).p, Hq, n_q, max_q, max_tokens, n_splits, paged_kernels);
 }
 
 int mustafar_paged8_attn(const void* q, int64_t q_stride, int n_q, int Hq, const mustafar_pages8_t* p, const void* cu,
@@ -94,7 +94,7 @@ int mustafar_paged8_attn(const void* q, int64_t q_stride, int n_q, int Hq, const
   const Paged8View c = view8_of(p);
   Paged8AttnArgs a;
   const int what = attn_args(&a, q, q_stride, n_q, Hq, c.p, cu, window, sinks, scale, out, out_stride, max_q, max_tokens, n_splits,
-                             ws, ws_bytes, paged8_kernels);
+                             ws, ws_bytes, paged_kernels);
   if (what != MUSTAFAR_OK || n_q == 0) return what;
   a.k_scale = c.k_scale;
   a.v_scale = c.v_scale;
