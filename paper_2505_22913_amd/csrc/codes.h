@@ -60,6 +60,23 @@ __device__ __forceinline__ f32x4 decode4(uint32_t codes, float scale) {
   }
 }
 
+// Four int8 codes as whole numbers of the type, in two pairs.
+template <bool BF16>
+__device__ __forceinline__ u32x2 whole_pairs(uint32_t codes) {
+  if constexpr (BF16) {
+    // (a number of 7 bits has no more in fp32 than in its upper half)
+    const f32x4 x = decode4<true>(codes, 1.f);
+    auto pair = [](float a, float b) { return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, a), 0x07060302u); };
+    return (u32x2){pair(x[0], x[1]), pair(x[2], x[3])};
+  } else {
+    // 0x64 above the code + 128 is 1024 + that; its difference from 1152 is the code.
+    const uint32_t u = codes ^ 0x80808080u;
+    const half2_t zero = {(_Float16)1152.f, (_Float16)1152.f};
+    return (u32x2){__builtin_bit_cast(uint32_t, __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) - zero),
+                   __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) - zero)};
+  }
+}
+
 // Four codes as values of the type, exactly, in two pairs.
 template <bool BF16, bool INT8>
 __device__ __forceinline__ u32x2 decode_pairs(uint32_t codes, float scale) {
@@ -74,12 +91,10 @@ __device__ __forceinline__ u32x2 decode_pairs(uint32_t codes, float scale) {
     const f32x4 x = decode4<true>(codes, scale);
     return (u32x2){pack2<true>(x[0], x[1]), pack2<true>(x[2], x[3])};
   } else {
-    // 0x64 above the code + 128 is 1024 + that; its difference from 1152 is the code.
-    const uint32_t u = codes ^ 0x80808080u;
-    const half2_t s = {(_Float16)scale, (_Float16)scale}, zero = {(_Float16)1152.f, (_Float16)1152.f};
-    const half2_t lo = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u));
-    const half2_t hi = __builtin_bit_cast(half2_t, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u));
-    return (u32x2){__builtin_bit_cast(uint32_t, (lo - zero) * s), __builtin_bit_cast(uint32_t, (hi - zero) * s)};
+    const u32x2 x = whole_pairs<false>(codes);
+    const half2_t s = {(_Float16)scale, (_Float16)scale};
+    auto scaled = [&](uint32_t pair) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2_t, pair) * s); };
+    return (u32x2){scaled(x.x), scaled(x.y)};
   }
 }
 

@@ -24,8 +24,55 @@ struct Paged8AttnArgs : PagedAttnArgs {
   const uint8_t* k_scale;
   const uint8_t* v_scale;
   int int8, log2_block;
+  // Ranges of a kv-head in a launch of k_paged8_rows that shares `budget` of them out among the requests by their lengths (flat, the
+  // launch's, is more where there are more tiles of rows; 0: `few` ranges of every request). info: for each row where its results
+  // begin and how many ranges they are of.
+  int64_t flat;
+  int budget;
+  int2* info;
 };
 
+// As PagedPlan; `few` is 2 where there are `flat` ranges.
+struct Paged8Plan : PagedPlan {
+  int64_t flat;
+  int budget;
+};
+// Waves of k_paged8_rows, where requests are divided, and the tokens of a range from which they are shared out by the requests' lengths.
+constexpr int kFew8Waves = 1024, kFlat8Tokens = 768;
+
+// Rows of the ranges' results of k_paged8_rows, 16 of each of `flat`.
+template <class Plan>
+inline int64_t paged8_few_rows(const PagedView& p, const Plan& k, int64_t few_rows) {
+  return k.flat ? k.flat * p.H * kFewRows : paged_parts(few_rows, k.few);
+}
+inline int64_t paged8_parts(const Paged8AttnArgs& a, int64_t few_rows) { return paged8_few_rows(a.p, a, few_rows); }
+
+struct Kernels8 {
+  using Plan = Paged8Plan;
+  static Plan choose(const PagedView& p, int G, int n_q, int max_q, int64_t max_tokens, int n_splits) {
+    Plan k;
+    static_cast<PagedPlan&>(k) = paged_kernels(p, G, n_q, max_q, max_tokens, n_splits);
+    k.flat = 0;
+    k.budget = 0;
+    if (k.few == 0 || n_splits > 0) return k;
+    // Tiles of rows of a kv-head (as paged_kernels counts them, and how many there can be).
+    const int64_t requests = p.B < n_q ? p.B : n_q, full = k.mixed ? 0 : ((int64_t)n_q * G + kFewRows - 1) / kFewRows;
+    const int64_t units = requests > full ? requests : full, most_units = requests + (k.mixed ? 0 : (int64_t)n_q * G / kFewRows);
+    const int64_t n = kFew8Waves / (units * p.H), most = max_tokens / 64;
+    k.few = (int)(n < 1 || most < 1 ? 1 : n < most ? n : most);
+    if (k.few == 1 || requests == 1 || max_tokens < kFlat8Tokens * k.few) return k;
+    k.few = 2;
+    k.budget = kFew8Waves / p.H;
+    k.flat = k.budget > most_units ? k.budget : most_units;
+    return k;
+  }
+  static int64_t ws_bytes(const PagedView& p, int64_t rows, const Plan& k) {
+    return (paged8_few_rows(p, k, k.few_rows) + paged_parts(rows, k.most_many)) * (p.d + 2) * 4 + (k.flat ? 8 * k.few_rows : 0);
+  }
+  static double few_groups(const PagedView& p, const Plan& k, int64_t tiles) {
+    return k.flat ? (double)k.flat * p.H : (double)tiles * p.H * k.few;
+  }
+};
 hipError_t launch_paged8_attn(const Paged8AttnArgs& a, hipStream_t s);
 
 // Blocks of tokens that hold the n_new rows of B requests, however they are divided, and k_paged8_write's workgroups for one: a wave

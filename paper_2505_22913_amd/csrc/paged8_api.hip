@@ -83,7 +83,7 @@ int mustafar_paged8_gather(const mustafar_pages8_t* p, const void* first, void* 
 size_t mustafar_paged8_attn_workspace_bytes(const mustafar_pages8_t* p, int Hq, int n_q, int max_q, int max_tokens,
                                             int n_splits) {
   if (check_pages8(p) != MUSTAFAR_OK) return 0;
-  return attn_ws_bytes(view8_of(p).p, Hq, n_q, max_q, max_tokens, n_splits, paged_kernels);
+  return attn_ws_bytes<Kernels8>(view8_of(p).p, Hq, n_q, max_q, max_tokens, n_splits);
 }
 
 int mustafar_paged8_attn(const void* q, int64_t q_stride, int n_q, int Hq, const mustafar_pages8_t* p, const void* cu,
@@ -93,13 +93,16 @@ int mustafar_paged8_attn(const void* q, int64_t q_stride, int n_q, int Hq, const
   if (st != MUSTAFAR_OK) return st;
   const Paged8View c = view8_of(p);
   Paged8AttnArgs a;
-  const int what = attn_args(&a, q, q_stride, n_q, Hq, c.p, cu, window, sinks, scale, out, out_stride, max_q, max_tokens, n_splits,
-                             ws, ws_bytes, paged_kernels);
+  Paged8Plan plan;
+  const int what = attn_args<Kernels8>(&a, q, q_stride, n_q, Hq, c.p, cu, window, sinks, scale, out, out_stride, max_q, max_tokens,
+                                       n_splits, ws, ws_bytes, &plan);
   if (what != MUSTAFAR_OK || n_q == 0) return what;
   a.k_scale = c.k_scale;
   a.v_scale = c.v_scale;
   a.int8 = c.int8;
   a.log2_block = c.log2_block;
+  a.flat = plan.flat;
+  a.budget = plan.budget;
   return status_of(launch_paged8_attn(a, (hipStream_t)stream));
 }
 

@@ -29,6 +29,11 @@ struct Pages8 {
   __device__ __forceinline__ float value(const Held& t, int c) const { return code(a.p.v, t.at + c) * t.vs; }
 };
 
+// Tile s n / of of n tiles in `of` ranges (at most 2^16), in 32 bits.
+__device__ __forceinline__ int range_start(int n, int s, int of) {
+  return n / of * s + (int)((uint32_t)(n % of) * (uint32_t)s / (uint32_t)of);
+}
+
 // ------------------------------------------------------------------------------------------
 // k_paged8_chunk: 32 rows a wave, 8 waves a workgroup (4 at d = 256), tiles of 64 tokens (32): chunks of prompts.
 //
@@ -59,8 +64,7 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
   const uint32_t lane = lane_id(), r32 = lane % 32, half = lane / 32;
   const int wrow = rt.row0 + 32 * wave;  // the wave's first row
   const TileList tl(rt.base + rt.row0 / a.G, rt.base + (min(rt.row0 + BM, rt.rows) - 1) / a.G, a.window, a.sinks, BN);
-  const int t0 = (int)((int64_t)tl.n * split / part.n_splits);
-  const int n = (int)((int64_t)tl.n * (split + 1) / part.n_splits) - t0;  // tiles of the workgroup
+  const int t0 = range_start(tl.n, split, part.n_splits), n = range_start(tl.n, split + 1, part.n_splits) - t0;  // tiles of the workgroup
   // The wave's rows' positions, and its tiles: those behind its last position are the others'.
   const int pos0 = rt.base + min(wrow, rt.rows - 1) / a.G, pos1 = rt.base + min(wrow + 31, rt.rows - 1) / a.G;
   const int mine = wrow >= rt.rows || pos1 < 0 ? 0 : min(n, max(tl.count_to(pos1, BN) - t0, 0));
@@ -390,7 +394,8 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
 #pragma unroll
     for (int r = 0; r < 16; ++r) z = fmaf(o[c][r], 0.f, z);
   if (ballot(row < rt.rows && (z != z || fabsf(shift) >= kFar<BF16>))) {
-    redo_rows<T, BF16>(a, Pages8<INT8>{a}, part, rt, h, wrow, 32, tl, t0, t0 + n, split, BN);
+    redo_rows<T, BF16>(a, Pages8<INT8>{a}, part, rt, h, wrow, 32, tl, t0, t0 + n,
+                       [&](int r) { return split * part.rows + part_row(a, part, rt, h, r); }, BN);
     return;
   }
   const int tok = row / a.G, hq = h * a.G + (row - tok * a.G);
@@ -426,42 +431,153 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
 }
 
 // ------------------------------------------------------------------------------------------
-// k_paged8_rows: at most 16 rows, one wave, tiles of 32 tokens.
+// k_paged8_rows: at most 16 rows, one wave: single tokens (and few) over a long cache.
 //
-// As k_paged_rows: the products' operands come straight from memory. A lane loads 16 codes of a key row at once, channels
-// 64 c + 16 (l / 16), which are two operands of 8 channels each (the order of a product's channels is free as long as q
-// has the same); of the values it loads channels 4 T (l % 16) .. of eight tokens and transposes them, a byte permute for two codes,
-// before they become values of the type. The scale goes into that conversion.
+// The codes arrive in LDS, two or three tiles of it at once and for this wave alone, so that there is no barrier: 16 bytes a lane where
+// the lane reads them again as the two operands of 8 channels that they are (keys: row l % 16, channels 64 c + 16 (l / 16); the order
+// of a product's channels is free as long as q has the same), and rows of values whose pieces are exchanged so that the
+// transposing reads, 16 channels of eight tokens, find them in different banks. A lane gets eight tokens' codes of one channel; they
+// become values of the type, with their block's power of two, in registers. (Loads to registers, a tile or two ahead: the
+// compiler copies registers in flight from one turn to the next, so that each turn waits for all loads: 1.36 us a tile of 64
+// tokens at d = 64 for 8 KB.)
 // ------------------------------------------------------------------------------------------
-constexpr int kRows8Tile = 32;
+template <int T>
+constexpr int rows8_groups() { return T == 1 ? 4 : 2; }  // of 16 tokens, a tile
+template <int T>
+constexpr int rows8_ring() { return T == 2 ? 3 : 2; }    // tiles in LDS
+
+// Range f of a launch whose ranges are shared out among the requests by what they see: `chunk` tiles each (at least 64 tokens), evenly
+// within a request, as few of them as make no more than a.budget ranges (one a tile of rows, if those are more).
+struct Unit {
+  RowTile rt;
+  int split, splits;
+  uint32_t first;  // range of the launch that its first one is
+};
+__device__ __forceinline__ bool unit_of(const Paged8AttnArgs& a, uint32_t f, int BN, Unit& u) {
+  struct Entry {
+    int cu, rows, base, tiles, n;  // its row in q, rows, position of the first; tiles of rows, and of tokens that they see
+  };
+  const int B = a.p.B, lane = (int)lane_id(), stride = (B + kWave - 1) / kWave;
+  auto entry = [&](int b) {
+    const RowTile rt = rows_at(a, b, a.cu[b], a.cu[b + 1], a.p.state[b]);
+    Entry e = {rt.tok0, rt.rows, rt.base, 0, 0};
+    if (rt.rows > 0) {
+      e.tiles = a.mixed ? rt.rows <= kFewRows : (rt.rows + kFewRows - 1) / kFewRows;
+      e.n = TileList(rt.base, rt.base + min(a.cu[b + 1], a.n_q) - rt.tok0 - 1, a.window, a.sinks, BN).n;
+    }
+    return e;
+  };
+  Entry e = {0, 0, 0, 0, 0};
+  uint64_t work = 0;
+  uint32_t units = 0;
+  for (int b = lane * stride; b < min((lane + 1) * stride, B); ++b) {
+    e = entry(b);
+    work += (uint64_t)(uint32_t)e.tiles * (uint32_t)e.n;
+    units += (uint32_t)e.tiles;
+  }
+  auto sum = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)wave_incl_scan(x), kWave - 1); };
+  const uint64_t total = sum((uint32_t)(work & 0xffffu)) + ((uint64_t)sum((uint32_t)(work >> 16)) << 16);
+  uint32_t chunk = 1, count = 0;
+  auto ranges = [&](const Entry& x) { return max(((uint32_t)x.n + chunk - 1) / chunk, 1u); };
+  auto divide = [&](uint32_t by) {
+    chunk = total < 0x80000000u ? ((uint32_t)total + by - 1) / by : (uint32_t)min(total / by + 1, (uint64_t)0x7fffffff);
+    chunk = max(chunk, (uint32_t)(kWave / BN));
+    count = 0;
+    for (int b = lane * stride; b < min((lane + 1) * stride, B); ++b) {
+      if (stride > 1) e = entry(b);
+      count += (uint32_t)e.tiles * ranges(e);
+    }
+  };
+  // Each request's last range may be a part of one. Where that makes too many, one for each is kept back.
+  const uint32_t budget = (uint32_t)a.budget;
+  divide(budget);
+  if (sum(count) > budget) divide(budget - min(sum(units), budget - 1));
+  uint32_t incl = wave_incl_scan(count), want = f;
+  if (want >= (uint32_t)__builtin_amdgcn_readlane((int)incl, kWave - 1)) return false;
+  int at = __builtin_popcountll(ballot(incl <= want)), b = at;
+  want -= (uint32_t)__builtin_amdgcn_readlane((int)(incl - count), at);
+  if (stride > 1) {
+    b *= stride;
+    e = {0, 0, 0, 0, 0};
+    if (lane < stride && b + lane < B) e = entry(b + lane);
+    count = (uint32_t)e.tiles * ranges(e);
+    incl = wave_incl_scan(count);
+    at = __builtin_popcountll(ballot(incl <= want));
+    want -= (uint32_t)__builtin_amdgcn_readlane((int)(incl - count), at);
+    b += at;
+  }
+  u.splits = __builtin_amdgcn_readlane((int)ranges(e), at);
+  u.rt.b = b;
+  u.rt.tok0 = __builtin_amdgcn_readlane(e.cu, at);
+  u.rt.rows = __builtin_amdgcn_readlane(e.rows, at);
+  u.rt.base = __builtin_amdgcn_readlane(e.base, at);
+  const int row_tile = (int)(want / (uint32_t)u.splits);
+  u.rt.row0 = row_tile * kFewRows;
+  u.split = (int)want - row_tile * u.splits;
+  u.first = f - (uint32_t)u.split;
+  return true;
+}
+
+// Four direct loads of 16 bytes a lane to dst, dst + 1024, .. (m0, their LDS address, is put back; five cycles lie between a base
+// that the vector units wrote and its use, one between m0 and its). What the wave has read of the place before is there.
+__device__ __forceinline__ void load_4_to_lds(uint32_t dst, const unsigned char* b0, uint32_t o0, const unsigned char* b1, uint32_t o1,
+                                              const unsigned char* b2, uint32_t o2, const unsigned char* b3, uint32_t o3) {
+  uint32_t m0;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_waitcnt lgkmcnt(0)\n\ts_nop 2\n\tglobal_load_lds_dwordx4 %2, %6 nt\n\t"
+               "s_add_u32 m0, m0, 1024\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %7 nt\n\t"
+               "s_add_u32 m0, m0, 1024\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %8 nt\n\t"
+               "s_add_u32 m0, m0, 1024\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %5, %9 nt\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0) : "s"(dst), "v"(o0), "v"(o1), "v"(o2), "v"(o3), "s"(b0), "s"(b1), "s"(b2), "s"(b3) : "memory", "scc");
+}
 
 template <int T, bool BF16, bool INT8>
 __global__ __launch_bounds__(kWave) void k_paged8_rows(Paged8AttnArgs a, PartOut part) {
-  constexpr int d = kTile * T, NC = 2 * T, NO = 4 * T, BN = kRows8Tile;
+  constexpr int d = kTile * T, NC = 2 * T, NO = 4 * T, NG = rows8_groups<T>(), BN = 16 * NG, R = rows8_ring<T>();
+  constexpr int kLanes = 4 * T, kRowsPerLoad = 16 / T;             // of a row of values, of a load of them
+  constexpr int kLoads = NG * T;                                   // of a tile's keys, and of its values
+  // int8 codes become whole numbers of the type without their scale, which multiplies the scores and, in bf16, whose exponents have
+  // room for it, the probabilities: fewer instructions than to multiply them.
+  constexpr bool kScaled = INT8 && BF16;
+  constexpr uint32_t kHalf = 1024 * kLoads, kSlot = 2 * kHalf;     // bytes of each, of a tile
+  __shared__ __align__(1024) unsigned char smem[R * kSlot];
   const PagedView& p = a.p;
-  const int h = blockIdx.x % p.H, split = (blockIdx.x / p.H) % part.n_splits, tile = blockIdx.x / (p.H * part.n_splits);
-  const RowTile rt = a.mixed ? rows_of(a, tile) : row_tile<kFewRows>(a, tile, false);
-  if (rt.row0 >= rt.rows || (a.mixed && rt.rows > kFewRows)) return;
+  const int h = blockIdx.x % p.H;
+  Unit u;
+  if (a.flat) {
+    if (!unit_of(a, blockIdx.x / p.H, BN, u)) return;
+  } else {
+    const int tile = blockIdx.x / (p.H * part.n_splits);
+    u.split = (blockIdx.x / p.H) % part.n_splits;
+    u.splits = part.n_splits;
+    u.rt = a.mixed ? rows_of(a, tile) : row_tile<kFewRows>(a, tile, false);
+    if (u.rt.row0 >= u.rt.rows || (a.mixed && u.rt.rows > kFewRows)) return;
+  }
+  const RowTile rt = u.rt;
+  // Where the results of row r of the request go if they are a range's.
+  auto result_at = [&](int r) __attribute__((always_inline)) {
+    if (a.flat) return ((int64_t)(u.first + (uint32_t)u.split) * p.H + h) * kFewRows + (r - rt.row0);
+    return u.split * part.rows + part_row(a, part, rt, h, r);
+  };
   const uint32_t lane = lane_id(), r16 = lane % 16, q4 = lane / 16;
   const int row = min(rt.row0 + (int)r16, rt.rows - 1), tok = row / a.G, pos = rt.base + tok;
   const int pos0 = rt.base + rt.row0 / a.G, pos1 = rt.base + (min(rt.row0 + kFewRows, rt.rows) - 1) / a.G;
   const TileList tl(pos0, pos1, a.window, a.sinks, BN);
-  const int t0 = (int)((int64_t)tl.n * split / part.n_splits);
-  const int n = (int)((int64_t)tl.n * (split + 1) / part.n_splits) - t0;
+  const int t0 = range_start(tl.n, u.split, u.splits), n = range_start(tl.n, u.split + 1, u.splits) - t0;
+  // Where its ranges' results begin and how many there are, for each row.
+  if (a.flat && u.split == 0 && q4 == 0 && rt.row0 + (int)r16 < rt.rows)
+    a.info[part_row(a, part, rt, h, row)] = make_int2((int)result_at(row), u.splits);
   // Tiles [clean0, clean1) are seen whole by every row, [whole0, whole1) by some.
   const int clean0 = a.window > 0 ? tl.count_to(before(pos1, a.window), BN) - t0 : 0, clean1 = tl.count_to(pos0 - BN + 1, BN) - t0;
   const int whole0 = tl.count_to(tl.lo - 1, BN) - t0, whole1 = tl.count_to(tl.hi - BN + 1, BN) - t0;
 
-  // Lane i holds the offset in k and v, and the scales, of group i of 16 tokens of the 32 tiles at hand (one that no row sees is
-  // replaced by the nearest that some row does; pages hold 16 tokens or more, and so do blocks).
-  uint32_t at_lo = 0, at_hi = 0, scales = 0;
-  const uint32_t row_bytes = (uint32_t)p.token_stride;
-  auto group_of = [&](int t, int g) __attribute__((always_inline)) {
-    const int g0 = tl.start(t0 + t, BN) + 16 * g;
-    return g0 < tl.sinks ? g0 : min(max(g0, tl.lo & ~15), tl.hi & ~15);
-  };
+  // Lane i holds the offset in k and v, and the scales, of group i of 16 tokens of the 64 / NG tiles whose loads are next (one that
+  // no row sees is replaced by the nearest that some row does; pages hold 16 tokens or more, and so do blocks).
+  constexpr int kBatch = kWave / NG;
+  static_assert(R <= kBatch, "tiles under way are of two batches at most");
+  uint32_t at_lo = 0, at_hi = 0, scales = 0, scales_before = 0;
   auto look_up = [&](int first) __attribute__((always_inline)) {
-    const int g0 = group_of(min(first + (int)lane / 2, n - 1), lane & 1);
+    const int j = tl.start(t0 + min(first + (int)lane / NG, n - 1), BN) + 16 * ((int)lane % NG);
+    const int g0 = j < tl.sinks ? j : min(max(j, tl.lo & ~15), tl.hi & ~15);
     int page = p.table[(int64_t)rt.b * p.max_pages + (g0 >> p.log2_page)];
     if ((uint32_t)page >= (uint32_t)p.n_pages) page = 0;
     const int place = g0 & ((1 << p.log2_page) - 1);
@@ -469,96 +585,112 @@ __global__ __launch_bounds__(kWave) void k_paged8_rows(Paged8AttnArgs a, PartOut
     const int64_t block = (((int64_t)page * p.H + h) << (p.log2_page - a.log2_block)) + (place >> a.log2_block);
     at_lo = (uint32_t)at;
     at_hi = (uint32_t)(at >> 32);
+    scales_before = scales;
     scales = (uint32_t)a.k_scale[block] | (uint32_t)a.v_scale[block] << 8;
   };
-  auto base_of = [&](const uint16_t* x, int t, int g) __attribute__((always_inline)) {
-    const int i = (2 * t + g) % kWave;
-    return reinterpret_cast<const unsigned char*>(x) + ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)at_hi, i) << 32 |
-                                                        (uint32_t)__builtin_amdgcn_readlane((int)at_lo, i));
+  // Loads: the lane's place in a group's keys, and its row of values and piece of it (rows of the two groups of a product's tokens
+  // lie in different banks, and so do four rows from a fourth one on).
+  const uint32_t lds0 = (uint32_t)(uintptr_t)smem, row_bytes = (uint32_t)p.token_stride;
+  const uint32_t k_off = r16 * row_bytes + 16u * q4, v_row = lane / kLanes;
+  auto exchanged = [&](uint32_t row_of_group, uint32_t group) __attribute__((always_inline)) {
+    return (T == 4 ? row_of_group & 3 : T == 2 ? row_of_group >> 1 & 1 : 0u) | (group & 1) * T;
   };
-  // Row r of a group of a tile at the ends of what is seen: the nearest that some row sees (the others may be what memory held,
-  // and 0 times that is not 0).
-  auto nearest = [&](int r, int t, int g) __attribute__((always_inline)) {
-    const int g0 = group_of(t, g);
-    const bool first = g0 < tl.sinks;
-    const int from = first ? 0 : tl.lo, to = first && tl.lo > g0 + 15 ? tl.sinks - 1 : tl.hi;
-    return min(max(r, from - g0), min(to - g0, 15));
-  };
-  u32x4 kr[2][T];
-  uint32_t vr[8][T];
-  float ks[2], vs[2];  // of the tile whose codes are loaded
-  auto load_keys = [&](int t) __attribute__((always_inline)) {
-    if (t % (kWave / 2) == 0) look_up(t);
-    const bool edge = t < whole0 || t >= whole1;
+  uint32_t v_off[2];
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      uint32_t r = r16;
-      if (edge) r = (uint32_t)nearest((int)r, t, g);
-      const unsigned char* x = base_of(p.k, t, g) + (r * row_bytes + 16u * q4);
+  for (int i = 0; i < 2; ++i) v_off[i] = v_row * row_bytes + 16u * ((lane % kLanes) ^ exchanged(v_row, i));
+  const unsigned char *const k0 = reinterpret_cast<const unsigned char*>(p.k), *const v0 = reinterpret_cast<const unsigned char*>(p.v);
+  auto stage = [&](int t, int slot) __attribute__((always_inline)) {
+    if (t % kBatch == 0) look_up(t);
+    uint64_t at[NG];
 #pragma unroll
-      for (int c = 0; c < T; ++c) kr[g][c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(x + 64 * c));
-      ks[g] = power_of((uint32_t)__builtin_amdgcn_readlane((int)scales, (2 * t + g) % kWave) & 0xffu);
+    for (int g = 0; g < NG; ++g) {
+      const int i = (NG * t + g) % kWave;
+      at[g] = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)at_hi, i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)at_lo, i);
     }
-  };
-  auto load_values = [&](int t) __attribute__((always_inline)) {
-    const bool edge = t < whole0 || t >= whole1;
+    const uint32_t dst = (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds0 + (uint32_t)slot * kSlot));
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      uint32_t r = 4 * q4 + i % 4;
-      if (edge) r = (uint32_t)nearest((int)r, t, i / 4);
-      const unsigned char* x = base_of(p.v, t, i / 4) + (r * row_bytes + (uint32_t)NO * r16);
-      if constexpr (T == 1) {
-        vr[i][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(x));
-      } else if constexpr (T == 2) {
-        const u32x2 v = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(x));
-        vr[i][0] = v.x;
-        vr[i][1] = v.y;
-      } else {
-        const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(x));
-#pragma unroll
-        for (int m = 0; m < 4; ++m) vr[i][m] = v[m];
-      }
+    for (int l = 0; l < kLoads; l += 4) {
+      // keys: load l is channels 64 (l % T) .. of group l / T
+      auto key = [&](int i) __attribute__((always_inline)) { return k0 + at[i / T] + 64 * (i % T); };
+      load_4_to_lds(dst + 1024 * l, key(l), k_off, key(l + 1), k_off, key(l + 2), k_off, key(l + 3), k_off);
     }
 #pragma unroll
-    for (int g = 0; g < 2; ++g) vs[g] = power_of((uint32_t)__builtin_amdgcn_readlane((int)scales, (2 * t + g) % kWave) >> 8 & 0xffu);
+    for (int l = 0; l < kLoads; l += 4) {
+      // values: rows kRowsPerLoad (l % T) .. of it
+      auto value = [&](int i) __attribute__((always_inline)) { return v0 + at[i / T] + (uint64_t)(kRowsPerLoad * (i % T)) * row_bytes; };
+      load_4_to_lds(dst + kHalf + 1024 * l, value(l), v_off[l / T % 2], value(l + 1), v_off[(l + 1) / T % 2], value(l + 2), v_off[(l + 2) / T % 2],
+                    value(l + 3), v_off[(l + 3) / T % 2]);
+    }
+  };
+  // What no row sees of a tile's values is cleared: it may be what memory held, and 0 times NaN is not 0 (int8 has none, and a
+  // block with a token that is seen has its scale; the scores of such keys are replaced).
+  auto clear_values = [&](int t, uint32_t slot_at) __attribute__((always_inline)) {
+    if (INT8 || (t >= whole0 && t < whole1)) return;
+    const int j0 = tl.start(t0 + t, BN) + (int)v_row;
+#pragma unroll 1
+    for (int l = 0; l < kLoads; ++l) {
+      const int j = j0 + kRowsPerLoad * l;
+      if (j > tl.hi || (j < tl.lo && j >= tl.sinks))
+        *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(slot_at + kHalf + 1024 * l + 16 * lane) = (u32x4){0u, 0u, 0u, 0u};
+    }
+    asm volatile("" ::: "memory");
+  };
+  // Lanes 2 i and 2 i + 1 of 16 address the row of token i of their product's eight: 4 (l / 16) .. of its first group, then its second.
+  const uint32_t read_row = 4 * q4 + r16 / 2 % 4, read_group = r16 / 8;
+  const uint32_t read_at = (16 * read_group + read_row) * d + 8 * (r16 & 1), read_x = exchanged(read_row, read_group);
+  auto values_at = [&](uint32_t slot_at, int c, int g) __attribute__((always_inline)) {  // channels 16 c .., of groups g and g + 1
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    const uint32_t x = slot_at + kHalf + 16 * g * d + read_at + 16u * ((uint32_t)c ^ read_x);
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(reinterpret_cast<__attribute__((address_space(3))) i32x2*>(x)));
   };
 
   const float inv_scale = 1.f / a.scale_log2;
   float l = 0.f, shift = 0.f, limit = -INFINITY;
-  f32x4 o[NO];
+  f32x4 o[NO];  // rows 4 (l / 16) + e, channel 16 c + l % 16
 #pragma unroll
   for (int c = 0; c < NO; ++c) o[c] = (f32x4){};
   if (n > 0) {
-    load_keys(0);
     u32x4 qb[NC];  // Q as the B operand: column = row, k = 64 (c / 2) + 16 (l / 16) + 8 (c % 2) + i
     {
       const uint16_t* q = a.q + (int64_t)(rt.tok0 + tok) * a.q_stride + (h * a.G + row - tok * a.G) * d + 16 * q4;
 #pragma unroll
       for (int c = 0; c < NC; ++c) qb[c] = *reinterpret_cast<const u32x4*>(q + 64 * (c / 2) + 8 * (c % 2));
     }
-    load_values(0);
-    for (int t = 0; t < n; ++t) {
-      f32x4 s[2] = {};
+    // The scale bytes of group g of tile t, whose batch of tiles is that of the newest one that is placed, `newest`, or the one before.
+    auto scale_bytes = [&](int t, int newest, int g) __attribute__((always_inline)) {
+      const uint32_t word = t / kBatch == newest / kBatch ? scales : scales_before;
+      return (uint32_t)__builtin_amdgcn_readlane((int)word, (NG * t + g) % kWave);
+    };
+    auto scores = [&](int t, int newest, uint32_t slot_at, f32x4 (&s)[NG]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int g = 0; g < 2; ++g)
+      for (int g = 0; g < NG; ++g) {
+        const float scale = power_of(scale_bytes(t, newest, g) & 0xffu);
+        s[g] = (f32x4){};
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          const u32x2 lo = decode_pairs<BF16, INT8>(kr[g][c / 2][2 * (c % 2)], ks[g]), hi = decode_pairs<BF16, INT8>(kr[g][c / 2][2 * (c % 2) + 1], ks[g]);
-          s[g] = mfma16<BF16>((u32x4){lo.x, lo.y, hi.x, hi.y}, qb[c], s[g]);
+        for (int c = 0; c < T; ++c) {
+          const u32x4 k = lds_load<u32x4>(slot_at + 1024 * (g * T + c) + 16 * lane);
+          u32x2 x[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i] = INT8 ? whole_pairs<BF16>(k[i]) : decode_pairs<BF16, false>(k[i], scale);
+          s[g] = mfma16<BF16>((u32x4){x[0].x, x[0].y, x[1].x, x[1].y}, qb[2 * c], s[g]);
+          s[g] = mfma16<BF16>((u32x4){x[2].x, x[2].y, x[3].x, x[3].y}, qb[2 * c + 1], s[g]);
         }
-      // (the values of the tile whose offsets this may replace are loaded already)
-      if (t + 1 < n) load_keys(t + 1);
+        if constexpr (INT8) s[g] *= scale;
+      }
+    };
+    // The scores of tile t are masked and the shift follows them.
+    auto settle = [&](int t, f32x4 (&s)[NG]) __attribute__((always_inline)) {
       if (t < clean0 || t >= clean1) {
         const int j0 = tl.start(t0 + t, BN) + 4 * (int)q4;
 #pragma unroll
-        for (int g = 0; g < 2; ++g)
+        for (int g = 0; g < NG; ++g)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             if (!sees(pos, j0 + 16 * g + e, a.window, a.sinks)) s[g][e] = -INFINITY;
       }
       float top = s[0][0];
 #pragma unroll
-      for (int e = 1; e < 8; ++e) top = fmaxf(top, s[e / 4][e % 4]);
+      for (int e = 1; e < 4 * NG; ++e) top = fmaxf(top, s[e / 4][e % 4]);
       if (ballot(top > limit)) {
         top = fmaxf(top, __shfl_xor(top, 16, kWave));
         top = fmaxf(top, __shfl_xor(top, 32, kWave));
@@ -575,38 +707,50 @@ __global__ __launch_bounds__(kWave) void k_paged8_rows(Paged8AttnArgs a, PartOut
           for (int c = 0; c < NO; ++c) o[c][e] *= ae;
         }
       }
-      u32x4 pa, pl;  // the probabilities in two parts of the type, the second what the first leaves
+    };
+    // Tile t's probabilities, in two parts of the type, the second what the first leaves, and their products with its values.
+    auto outputs = [&](int t, int newest, uint32_t slot_at, const f32x4 (&s)[NG]) __attribute__((always_inline)) {
+      u32x4 pa[NG / 2], pl[NG / 2];
+      float vs[NG];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float x = __builtin_amdgcn_exp2f(fmaf(s[e / 2][2 * (e % 2)], a.scale_log2, shift));
-        const float y = __builtin_amdgcn_exp2f(fmaf(s[e / 2][2 * (e % 2) + 1], a.scale_log2, shift));
-        pa[e] = pack2<BF16>(x, y);
-        pl[e] = pack2<BF16>(x - to_float<BF16>(pa[e] & 0xffffu), y - to_float<BF16>(pa[e] >> 16));
+      for (int g = 0; g < NG; ++g) vs[g] = power_of(scale_bytes(t, newest, g) >> 8 & 0xffu);
+#pragma unroll
+      for (int e = 0; e < 2 * NG; ++e) {
+        float x = __builtin_amdgcn_exp2f(fmaf(s[e / 2][2 * (e % 2)], a.scale_log2, shift));
+        float y = __builtin_amdgcn_exp2f(fmaf(s[e / 2][2 * (e % 2) + 1], a.scale_log2, shift));
         l += x + y;
+        if (kScaled) x *= vs[e / 2], y *= vs[e / 2];
+        pa[e / 4][e % 4] = pack2<BF16>(x, y);
+        pl[e / 4][e % 4] = pack2<BF16>(x - to_float<BF16>(pa[e / 4][e % 4] & 0xffffu), y - to_float<BF16>(pa[e / 4][e % 4] >> 16));
       }
 #pragma unroll
-      for (int m = 0; m < T; ++m) {
-        // Channels 4 m .. of the lane's: a word of four tokens for each.
-        uint32_t w[2][4];
+      for (int g = 0; g < NG; g += 2)
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          const uint32_t ab = __builtin_amdgcn_perm(vr[4 * g + 1][m], vr[4 * g][m], 0x05010400u);      // a0 b0 a1 b1
-          const uint32_t ab2 = __builtin_amdgcn_perm(vr[4 * g + 1][m], vr[4 * g][m], 0x07030602u);     // a2 b2 a3 b3
-          const uint32_t cd = __builtin_amdgcn_perm(vr[4 * g + 3][m], vr[4 * g + 2][m], 0x05010400u);
-          const uint32_t cd2 = __builtin_amdgcn_perm(vr[4 * g + 3][m], vr[4 * g + 2][m], 0x07030602u);
-          w[g][0] = __builtin_amdgcn_perm(cd, ab, 0x05040100u);
-          w[g][1] = __builtin_amdgcn_perm(cd, ab, 0x07060302u);
-          w[g][2] = __builtin_amdgcn_perm(cd2, ab2, 0x05040100u);
-          w[g][3] = __builtin_amdgcn_perm(cd2, ab2, 0x07060302u);
+        for (int c = 0; c < NO; ++c) {
+          const u32x2 w = values_at(slot_at, c, g);
+          const u32x2 x = kScaled ? whole_pairs<BF16>(w.x) : decode_pairs<BF16, INT8>(w.x, vs[g]);
+          const u32x2 y = kScaled ? whole_pairs<BF16>(w.y) : decode_pairs<BF16, INT8>(w.y, vs[g + 1]);
+          const u32x4 v = {x.x, x.y, y.x, y.y};
+          o[c] = mfma16<BF16>(pl[g / 2], v, mfma16<BF16>(pa[g / 2], v, o[c]));
         }
+    };
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const u32x2 lo = decode_pairs<BF16, INT8>(w[0][c], vs[0]), hi = decode_pairs<BF16, INT8>(w[1][c], vs[1]);
-          const u32x4 v = {lo.x, lo.y, hi.x, hi.y};
-          o[4 * m + c] = mfma16<BF16>(pl, v, mfma16<BF16>(pa, v, o[4 * m + c]));
-        }
-      }
-      if (t + 1 < n) load_values(t + 1);
+    for (int i = 0; i < R; ++i)
+      if (i < n) stage(i, i);
+    int slot = 0;
+    for (int t = 0; t < n; ++t) {
+      // The tile's loads have arrived; those of the tiles behind it are under way.
+      if (t + R <= n) wait_loads<2 * kLoads * (R - 1)>();
+      else wait_loads<0>();
+      const uint32_t slot_at = lds0 + (uint32_t)slot * kSlot;
+      const int newest = min(t + R, n) - 1;
+      f32x4 s[NG];
+      scores(t, newest, slot_at, s);
+      settle(t, s);
+      clear_values(t, slot_at);
+      outputs(t, newest, slot_at, s);
+      if (t + R < n) stage(t + R, slot);
+      slot = slot + 1 == R ? 0 : slot + 1;
     }
   }
 
@@ -619,12 +763,12 @@ __global__ __launch_bounds__(kWave) void k_paged8_rows(Paged8AttnArgs a, PartOut
     for (int e = 0; e < 4; ++e)
       if (rt.row0 + (int)(4 * q4) + e < rt.rows) z = fmaf(o[c][e], 0.f, z);
   if (ballot(z != z || (rt.row0 + (int)r16 < rt.rows && fabsf(shift) >= kFar<BF16>))) {
-    redo_rows<T, BF16>(a, Pages8<INT8>{a}, part, rt, h, rt.row0, kFewRows, tl, t0, t0 + n, split, BN);
+    redo_rows<T, BF16>(a, Pages8<INT8>{a}, part, rt, h, rt.row0, kFewRows, tl, t0, t0 + n, result_at, BN);
     return;
   }
-  if (part.n_splits > 1 && q4 == 0 && rt.row0 + (int)r16 < rt.rows)
-    part.ml[split * part.rows + part_row(a, part, rt, h, row)] =
-        make_float2(limit > -INFINITY ? -shift : -INFINITY, pos < 0 ? -1.f : l);
+  if (part.n_splits > 1 && q4 == 0 && rt.row0 + (int)r16 < rt.rows) {
+    part.ml[result_at(row)] = make_float2(limit > -INFINITY ? -shift : -INFINITY, pos < 0 ? -1.f : l);
+  }
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const int orow = rt.row0 + (int)(4 * q4) + e, otok = orow / a.G, hq = h * a.G + orow - otok * a.G;
@@ -632,30 +776,72 @@ __global__ __launch_bounds__(kWave) void k_paged8_rows(Paged8AttnArgs a, PartOut
     if (orow >= rt.rows) continue;
     const int64_t t = rt.tok0 + otok;
     if (part.n_splits > 1) {
-      f32x4* dst = reinterpret_cast<f32x4*>(part.o + (split * part.rows + part_row(a, part, rt, h, orow)) * d + NO * r16);
+      float* dst = part.o + result_at(orow) * d + r16;
 #pragma unroll
-      for (int c = 0; c < T; ++c) dst[c] = (f32x4){o[4 * c][e], o[4 * c + 1][e], o[4 * c + 2][e], o[4 * c + 3][e]};
+      for (int c = 0; c < NO; ++c) dst[16 * c] = o[c][e];
     } else {
       const float inv = rt.base + otok < 0 ? 0.f : 1.f / le;
-      u32x2* dst = reinterpret_cast<u32x2*>(a.out + t * a.out_stride + hq * d + NO * r16);
+      uint16_t* dst = a.out + t * a.out_stride + hq * d + r16;
 #pragma unroll
-      for (int c = 0; c < T; ++c)
-        dst[c] = (u32x2){pack2<BF16>(o[4 * c][e] * inv, o[4 * c + 1][e] * inv), pack2<BF16>(o[4 * c + 2][e] * inv, o[4 * c + 3][e] * inv)};
+      for (int c = 0; c < NO; ++c) dst[16 * c] = (uint16_t)pack2<BF16>(o[c][e] * inv, 0.f);
     }
   }
 }
 
+// ------------------------------------------------------------------------------------------
+// k_paged8_merge: joins the ranges of a row where requests have different numbers of them. As k_paged_merge.
+// ------------------------------------------------------------------------------------------
+template <int T, bool BF16, int OF, bool WIDE>
+__global__ __launch_bounds__(kMergeThreads) void k_paged8_merge(Paged8AttnArgs a, PartOut part) {
+  constexpr int L = 16 * T, S = kMergeThreads / L;
+  const int64_t i0 = WIDE ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * S + (int)threadIdx.x / L;
+  int t, hq;
+  int2 info = make_int2(0, 0);
+  bool mine;
+  if (a.mixed) {  // row r of an entry and kv-head
+    const int r = (int)(i0 % kFewRows), h = (int)(i0 / kFewRows % a.p.H), b = (int)(i0 / kFewRows / a.p.H);
+    if (b >= a.p.B) return;
+    const RowTile rt = rows_of(a, b);  // (a wave's rows are one request's: S divides kFewRows)
+    mine = r < rt.rows && rt.rows <= kFewRows;
+    t = rt.tok0 + r / a.G;
+    hq = h * a.G + r % a.G;
+    if (mine) info = a.info[part.by_entry ? i0 : (int64_t)t * a.Hq + hq];
+  } else {
+    t = (int)(i0 / a.Hq);
+    hq = (int)(i0 - (int64_t)t * a.Hq);
+    if (i0 >= (int64_t)a.n_q * a.Hq) return;
+    info = a.info[i0];  // (of a row of a request if it is one)
+    mine = t < a.cu[a.p.B];
+  }
+  if (!mine) return;  // (all of a stream; WIDE: all of the workgroup)
+  // (starts that are none, not ascending, have rows that no range is of: what memory held is not read for an address)
+  const int64_t step = (int64_t)a.p.H * kFewRows;
+  if (info.x < 0 || info.y < 1 || info.x + (info.y - 1) * step >= a.flat * step) return;
+  merge_row<T, BF16, OF, WIDE>(a, part.ml, part.o, step, info.y, info.x, t, hq);
+}
+
+template <int T, bool BF16>
+static hipError_t merge8_launch(const Paged8AttnArgs& a, const PartOut& part, hipStream_t s) {
+  const int64_t rows = a.mixed ? (int64_t)a.p.B * a.p.H * kFewRows : (int64_t)a.n_q * a.Hq;
+  if (rows >= kMergeWideRows)
+    hipLaunchKernelGGL((k_paged8_merge<T, BF16, 16 * T, false>), dim3((uint32_t)merge_groups(rows, T)), dim3(kMergeThreads), 0, s, a, part);
+  else
+    hipLaunchKernelGGL((k_paged8_merge<T, BF16, kWave, true>), dim3((uint32_t)rows), dim3(kMergeThreads), 0, s, a, part);
+  return hipGetLastError();
+}
+
 template <int T, bool BF16, bool INT8>
-static hipError_t attn8_launch(const Paged8AttnArgs& a, hipStream_t s) {
+static hipError_t attn8_launch(Paged8AttnArgs a, hipStream_t s) {
   // (all outputs first, aligned as they are accessed)
-  const int64_t rows = (int64_t)a.n_q * a.Hq, n_few = paged_parts(a.few_rows, a.few), n_many = paged_parts(rows, a.many);
+  const int64_t rows = (int64_t)a.n_q * a.Hq, n_few = paged8_parts(a, a.few_rows), n_many = paged_parts(rows, a.many);
   float* const o = (float*)a.ws;
   float2* const ml = (float2*)(o + (n_few + n_many) * (64 * T));
+  a.info = (int2*)(ml + n_few + n_many);
   const PartOut few = {ml, o, a.few_rows, a.by_entry, a.few}, many = {ml + n_few, o + n_few * (64 * T), rows, 0, a.many};
   hipError_t e;
   if (a.few > 0) {
-    const int64_t tiles = a.mixed ? a.p.B : paged_tiles(a.p, a.G, a.n_q, kFewRows);
-    hipLaunchKernelGGL((k_paged8_rows<T, BF16, INT8>), dim3((uint32_t)(tiles * a.p.H * a.few)), dim3(kWave), 0, s, a, few);
+    const int64_t ranges = a.flat ? a.flat : (a.mixed ? a.p.B : paged_tiles(a.p, a.G, a.n_q, kFewRows)) * a.few;
+    hipLaunchKernelGGL((k_paged8_rows<T, BF16, INT8>), dim3((uint32_t)(ranges * a.p.H)), dim3(kWave), 0, s, a, few);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (a.many > 0) {
@@ -664,7 +850,7 @@ static hipError_t attn8_launch(const Paged8AttnArgs& a, hipStream_t s) {
                        a, many);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  if ((e = launch_paged_merge(a, few, true, s)) != hipSuccess) return e;
+  if ((e = a.flat ? merge8_launch<T, BF16>(a, few, s) : launch_paged_merge(a, few, true, s)) != hipSuccess) return e;
   return launch_paged_merge(a, many, false, s);
 }
 

@@ -74,7 +74,7 @@ int mustafar_paged_gather(const mustafar_pages_t* p, const void* first, void* x_
 
 size_t mustafar_paged_attn_workspace_bytes(const mustafar_pages_t* p, int Hq, int n_q, int max_q, int max_tokens,
                                            int n_splits) {
-  return check_pages(p) != MUSTAFAR_OK ? 0 : attn_ws_bytes(view_of(p), Hq, n_q, max_q, max_tokens, n_splits, paged_kernels);
+  return check_pages(p) != MUSTAFAR_OK ? 0 : attn_ws_bytes<Kernels16>(view_of(p), Hq, n_q, max_q, max_tokens, n_splits);
 }
 
 int mustafar_paged_attn(const void* q, int64_t q_stride, int n_q, int Hq, const mustafar_pages_t* p, const void* cu,
@@ -83,8 +83,9 @@ int mustafar_paged_attn(const void* q, int64_t q_stride, int n_q, int Hq, const 
   int st = check_pages(p);
   if (st != MUSTAFAR_OK) return st;
   PagedAttnArgs a;
-  st = attn_args(&a, q, q_stride, n_q, Hq, view_of(p), cu, window, sinks, scale, out, out_stride, max_q, max_tokens, n_splits, ws,
-                 ws_bytes, paged_kernels);
+  PagedPlan plan;
+  st = attn_args<Kernels16>(&a, q, q_stride, n_q, Hq, view_of(p), cu, window, sinks, scale, out, out_stride, max_q, max_tokens,
+                            n_splits, ws, ws_bytes, &plan);
   if (st != MUSTAFAR_OK || n_q == 0) return st;
   return status_of(launch_paged_attn(a, (hipStream_t)stream));
 }

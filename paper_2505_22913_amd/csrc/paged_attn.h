@@ -272,16 +272,17 @@ __device__ __forceinline__ int64_t part_row(const PagedAttnArgs& a, const PartOu
   return (int64_t)(rt.tok0 + tok) * a.Hq + h * a.G + r - tok * a.G;
 }
 
-template <int T, bool BF16, class Pages>
+// result_at(r): where the range's results of row r of the request go, if there are several.
+template <int T, bool BF16, class Pages, class At>
 __device__ __forceinline__ void redo_rows(const PagedAttnArgs& a, const Pages& pages, const PartOut& part, const RowTile& rt, int h, int first_row,
-                                       int n_rows, TileList tl, int t0, int t1, int split, int BN) {
+                                       int n_rows, TileList tl, int t0, int t1, At result_at, int BN) {
   constexpr int d = kTile * T;
   const int lane = (int)lane_id();
   for (int r = first_row; r < min(first_row + n_rows, rt.rows); ++r) {
     const int tok = r / a.G, hq = h * a.G + (r - tok * a.G), t = rt.tok0 + tok, pos = rt.base + tok;
     const RowState<T> s = one_row<T, BF16>(a, pages, rt.b, h, a.q + t * a.q_stride + hq * d, pos, tl, t0, t1, BN);
     if (part.n_splits > 1) {
-      const int64_t row = split * part.rows + part_row(a, part, rt, h, r);
+      const int64_t row = result_at(r);
       // (what the maximum's rounding leaves goes into the sums: other ranges' are multiples of 2^m with theirs. Beyond 2^27 scores
       // of fp32 differ by more than 2^8 or not at all.)
       const float m = s.m * a.scale_log2, f = __builtin_amdgcn_exp2f(fminf(fmaxf(fmaf(s.m, a.scale_log2, -m), -8.f), 8.f));
@@ -292,6 +293,73 @@ __device__ __forceinline__ void redo_rows(const PagedAttnArgs& a, const Pages& p
         a.out[t * a.out_stride + hq * d + kTile * c + lane] = (uint16_t)pack2<BF16>(pos < 0 ? 0.f : s.o[c] / s.l, 0.f);
     }
   }
+}
+
+// ------------------------------------------------------------------------------------------
+// The n_splits ranges of a row together, into row t and head hq of a.out: range s of it lies at row + s * rows of ml and o.
+// ------------------------------------------------------------------------------------------
+constexpr int kMergeAhead = 8, kMergeWideRows = 512;
+
+template <int T, bool BF16, int OF, bool WIDE>
+__device__ __forceinline__ void merge_row(const PagedAttnArgs& a, const float2* ml, const float* o_of, int64_t rows, int n_splits,
+                                          int64_t row, int t, int hq) {
+  constexpr int d = kTile * T, L = 16 * T, S = kMergeThreads / L;
+  constexpr int kStep = WIDE ? S : 1, kAhead = kMergeAhead < OF / kStep ? kMergeAhead : OF / kStep;
+  static_assert(OF % (kStep * kAhead) == 0, "the ranges under way are of one round of weights");
+  const int lane = (int)lane_id(), stream = (int)threadIdx.x / L, sub = (int)threadIdx.x % L;
+  const int first = WIDE ? stream : 0, at = lane % OF;
+  f32x4 x[kAhead], o = {};
+  auto load = [&](int s0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (s0 + kStep * k < n_splits) x[k] = *reinterpret_cast<const f32x4*>(o_of + ((s0 + kStep * k) * rows + row) * d + 4 * sub);
+  };
+  load(first);
+  float M = -INFINITY, l = 0.f;
+  for (int s = at; s < n_splits; s += OF) M = fmaxf(M, ml[s * rows + row].x);
+#pragma unroll
+  for (int k = 1; k < OF; k *= 2) M = fmaxf(M, __shfl_xor(M, k, kWave));
+  uint64_t nothing = 0;
+  for (int s0 = 0; s0 < n_splits; s0 += OF) {
+    // lane i of those: the weight of range s0 + i, 0 for one without any (its output is not looked at)
+    float2 of = make_float2(-INFINITY, 0.f);
+    if (s0 + at < n_splits) of = ml[(s0 + at) * rows + row];
+    const float w = of.x != -INFINITY || of.y != 0.f ? at_least(__builtin_amdgcn_exp2f(of.x - M)) : 0.f;
+    if (w != 0.f) l = fmaf(of.y, w, l);
+    nothing |= ballot(of.y < 0.f);
+    const int end = min(s0 + OF, n_splits);
+    for (int s = s0; s < end; s += kStep * kAhead) {
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int sk = s + first + kStep * k;
+        if (OF == kMergeAhead && sk >= end) break;
+        const float wk = __shfl(w, (lane & -OF) | ((sk - s0) % OF), kWave);
+        if (sk < end && wk != 0.f)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] = fmaf(x[k][e], wk, o[e]);
+      }
+      load(s + first + kStep * kAhead);
+    }
+  }
+#pragma unroll
+  for (int k = 1; k < OF; k *= 2) l += __shfl_xor(l, k, kWave);
+  const bool zero = (nothing >> (lane & -OF) & (~0ull >> (kWave - OF))) != 0;
+  if constexpr (WIDE) {
+    __shared__ f32x4 sums[kMergeThreads / kWave][L];
+#pragma unroll
+    for (int k = L; k < kWave; k *= 2)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], k, kWave);
+    if (lane < L) sums[threadIdx.x / kWave][lane] = o;
+    __syncthreads();
+    if (threadIdx.x >= L) return;
+    o = sums[0][sub];
+#pragma unroll
+    for (int w = 1; w < kMergeThreads / kWave; ++w) o += sums[w][sub];
+  }
+  u32x2 y = {};
+  if (!zero) y = (u32x2){pack2<BF16>(o[0] / l, o[1] / l), pack2<BF16>(o[2] / l, o[3] / l)};
+  *reinterpret_cast<u32x2*>(a.out + t * a.out_stride + hq * d + 4 * sub) = y;
 }
 
 // ------------------------------------------------------------------------------------------

@@ -335,7 +335,8 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
 #pragma unroll
     for (int r = 0; r < 16; ++r) z = fmaf(o[c][r], 0.f, z);
   if (ballot(row < rt.rows && (z != z || fabsf(shift) >= kFar<BF16>))) {
-    redo_rows<T, BF16>(a, Pages16<BF16>{p}, part, rt, h, wrow, 32, tl, t0, t0 + n, split, BN);
+    redo_rows<T, BF16>(a, Pages16<BF16>{p}, part, rt, h, wrow, 32, tl, t0, t0 + n,
+                       [&](int r) { return split * part.rows + part_row(a, part, rt, h, r); }, BN);
     return;
   }
   const int tok = row / a.G, hq = h * a.G + (row - tok * a.G);
@@ -554,7 +555,8 @@ __global__ __launch_bounds__(kWave) void k_paged_rows(PagedAttnArgs a, PartOut p
     for (int e = 0; e < 4; ++e)
       if (rt.row0 + (int)(4 * q4) + e < rt.rows) z = fmaf(o[c][e], 0.f, z);
   if (ballot(z != z || (rt.row0 + (int)r16 < rt.rows && fabsf(shift) >= kFar<BF16>))) {
-    redo_rows<T, BF16>(a, Pages16<BF16>{p}, part, rt, h, rt.row0, kFewRows, tl, t0, t0 + n, split, BN);
+    redo_rows<T, BF16>(a, Pages16<BF16>{p}, part, rt, h, rt.row0, kFewRows, tl, t0, t0 + n,
+                       [&](int r) { return split * part.rows + part_row(a, part, rt, h, r); }, BN);
     return;
   }
   if (part.n_splits > 1 && q4 == 0 && rt.row0 + (int)r16 < rt.rows)
@@ -589,14 +591,10 @@ __global__ __launch_bounds__(kWave) void k_paged_rows(PagedAttnArgs a, PartOut p
 // d = 128, 16384 rows of 4 ranges take 9.4 us (3.8 TB/s; 12.5 with a wave a row). One stream a row against a workgroup a row:
 // 32 rows of 256 ranges 23.4 and 7.2 us, 512 of 16 4.8 both, 992 of 8 to 16 6.5 and 7.8, 2404 of 21 7.6 and 13.0.
 // ------------------------------------------------------------------------------------------
-constexpr int kMergeAhead = 8, kMergeWideRows = 512;
-
 template <int T, bool BF16, int OF, bool WIDE>
 __global__ __launch_bounds__(kMergeThreads) void k_paged_merge(PagedAttnArgs a, PartOut part, int of_few) {
-  constexpr int d = kTile * T, L = 16 * T, S = kMergeThreads / L;
-  constexpr int kStep = WIDE ? S : 1, kAhead = kMergeAhead < OF / kStep ? kMergeAhead : OF / kStep;
-  static_assert(OF % (kStep * kAhead) == 0, "the ranges under way are of one round of weights");
-  const int lane = (int)lane_id(), stream = (int)threadIdx.x / L, sub = (int)threadIdx.x % L;
+  constexpr int L = 16 * T, S = kMergeThreads / L;
+  const int stream = (int)threadIdx.x / L;
   const int64_t rows = part.rows, i0 = WIDE ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * S + stream;
   // The row: of q and all its heads, or, where the requests of few rows have ranges of their own, the r-th of a request's and kv-head's.
   int t, hq;
@@ -623,59 +621,7 @@ __global__ __launch_bounds__(kMergeThreads) void k_paged_merge(PagedAttnArgs a, 
   }
   if (!mine) return;  // (all of a stream; WIDE: all of the workgroup)
   const int64_t row = part.by_entry ? i0 : (int64_t)t * a.Hq + hq;
-  const int first = WIDE ? stream : 0, at = lane % OF;
-  f32x4 x[kAhead], o = {};
-  auto load = [&](int s0) __attribute__((always_inline)) {
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k)
-      if (s0 + kStep * k < part.n_splits) x[k] = *reinterpret_cast<const f32x4*>(part.o + ((s0 + kStep * k) * rows + row) * d + 4 * sub);
-  };
-  load(first);
-  float M = -INFINITY, l = 0.f;
-  for (int s = at; s < part.n_splits; s += OF) M = fmaxf(M, part.ml[s * rows + row].x);
-#pragma unroll
-  for (int k = 1; k < OF; k *= 2) M = fmaxf(M, __shfl_xor(M, k, kWave));
-  uint64_t nothing = 0;
-  for (int s0 = 0; s0 < part.n_splits; s0 += OF) {
-    // lane i of those: the weight of range s0 + i, 0 for one without any (its output is not looked at)
-    float2 ml = make_float2(-INFINITY, 0.f);
-    if (s0 + at < part.n_splits) ml = part.ml[(s0 + at) * rows + row];
-    const float w = ml.x != -INFINITY || ml.y != 0.f ? at_least(__builtin_amdgcn_exp2f(ml.x - M)) : 0.f;
-    if (w != 0.f) l = fmaf(ml.y, w, l);
-    nothing |= ballot(ml.y < 0.f);
-    const int end = min(s0 + OF, part.n_splits);
-    for (int s = s0; s < end; s += kStep * kAhead) {
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const int sk = s + first + kStep * k;
-        if (OF == kMergeAhead && sk >= end) break;
-        const float wk = __shfl(w, (lane & -OF) | ((sk - s0) % OF), kWave);
-        if (sk < end && wk != 0.f)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[e] = fmaf(x[k][e], wk, o[e]);
-      }
-      load(s + first + kStep * kAhead);
-    }
-  }
-#pragma unroll
-  for (int k = 1; k < OF; k *= 2) l += __shfl_xor(l, k, kWave);
-  const bool zero = (nothing >> (lane & -OF) & (~0ull >> (kWave - OF))) != 0;
-  if constexpr (WIDE) {
-    __shared__ f32x4 sums[kMergeThreads / kWave][L];
-#pragma unroll
-    for (int k = L; k < kWave; k *= 2)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], k, kWave);
-    if (lane < L) sums[threadIdx.x / kWave][lane] = o;
-    __syncthreads();
-    if (threadIdx.x >= L) return;
-    o = sums[0][sub];
-#pragma unroll
-    for (int w = 1; w < kMergeThreads / kWave; ++w) o += sums[w][sub];
-  }
-  u32x2 y = {};
-  if (!zero) y = (u32x2){pack2<BF16>(o[0] / l, o[1] / l), pack2<BF16>(o[2] / l, o[3] / l)};
-  *reinterpret_cast<u32x2*>(a.out + t * a.out_stride + hq * d + 4 * sub) = y;
+  merge_row<T, BF16, OF, WIDE>(a, part.ml, part.o, rows, part.n_splits, row, t, hq);
 }
 
 template <int T, bool BF16>

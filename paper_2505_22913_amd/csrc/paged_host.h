@@ -88,18 +88,28 @@ inline bool overlap(const void* a, const void* b, size_t bytes) {
 // ------------------------------------------------------------------------------------------
 // Attention: the arguments of both kinds of pages; `kernels` chooses theirs.
 // ------------------------------------------------------------------------------------------
-using PagedKernels = PagedPlan (*)(const PagedView&, int G, int n_q, int max_q, int64_t max_tokens, int n_splits);
+struct Kernels16 {
+  using Plan = PagedPlan;
+  static Plan choose(const PagedView& p, int G, int n_q, int max_q, int64_t max_tokens, int n_splits) {
+    return paged_kernels(p, G, n_q, max_q, max_tokens, n_splits);
+  }
+  static int64_t ws_bytes(const PagedView& p, int64_t rows, const Plan& k) { return paged_ws_bytes(p, rows, k); }
+  // Workgroups of few rows for so many tiles of them.
+  static double few_groups(const PagedView& p, const Plan& k, int64_t tiles) { return (double)tiles * p.H * k.few; }
+};
 
-inline size_t attn_ws_bytes(const PagedView& p, int Hq, int n_q, int max_q, int max_tokens, int n_splits, PagedKernels kernels) {
+template <class Kernels>
+inline size_t attn_ws_bytes(const PagedView& p, int Hq, int n_q, int max_q, int max_tokens, int n_splits) {
   if (Hq < 1 || Hq % p.H != 0 || Hq / p.H > MUSTAFAR_PAGED_MAX_GROUP) return 0;
   if (n_q < 1 || max_q < 0 || max_tokens < 0 || n_splits > kMaxSplits || (int64_t)n_q * Hq >= kMaxRows) return 0;
-  return (size_t)paged_ws_bytes(p, (int64_t)n_q * Hq, kernels(p, Hq / p.H, n_q, max_q, max_tokens, n_splits));
+  return (size_t)Kernels::ws_bytes(p, (int64_t)n_q * Hq, Kernels::choose(p, Hq / p.H, n_q, max_q, max_tokens, n_splits));
 }
 
-// Checks them and fills *a (not where n_q is 0: there is nothing to do).
+// Checks them and fills *a and *plan (not where n_q is 0: there is nothing to do).
+template <class Kernels>
 inline int attn_args(PagedAttnArgs* a, const void* q, int64_t q_stride, int n_q, int Hq, const PagedView& p, const void* cu,
                      int window, int sinks, float scale, void* out, int64_t out_stride, int max_q, int max_tokens, int n_splits,
-                     void* ws, size_t ws_bytes, PagedKernels kernels) {
+                     void* ws, size_t ws_bytes, typename Kernels::Plan* plan) {
   if (Hq < 1 || Hq % p.H != 0 || n_q < 0 || max_q < 0 || max_tokens < 0 || window < 0 || sinks < 0) return MUSTAFAR_EINVAL;
   if (Hq / p.H > MUSTAFAR_PAGED_MAX_GROUP) return MUSTAFAR_EUNSUPPORTED;
   if (n_q == 0) return MUSTAFAR_OK;
@@ -110,20 +120,21 @@ inline int attn_args(PagedAttnArgs* a, const void* q, int64_t q_stride, int n_q,
     return MUSTAFAR_EINVAL;
   if ((int64_t)n_q * Hq >= kMaxRows) return MUSTAFAR_EINVAL;
   if (n_splits > kMaxSplits) return MUSTAFAR_EINVAL;
-  const size_t need = attn_ws_bytes(p, Hq, n_q, max_q, max_tokens, n_splits, kernels);
+  const size_t need = attn_ws_bytes<Kernels>(p, Hq, n_q, max_q, max_tokens, n_splits);
   if (need > 0 && (!aligned(ws, 16) || ws_bytes < need)) return MUSTAFAR_EWORKSPACE;
   // (what the rows see: never more than the workspace was sized for)
   const int64_t seen = window > 0 ? (int64_t)window + max_q + sinks : max_tokens;
-  const PagedPlan k = kernels(p, Hq / p.H, n_q, max_q, seen < max_tokens ? seen : max_tokens, n_splits);
+  const typename Kernels::Plan k = Kernels::choose(p, Hq / p.H, n_q, max_q, seen < max_tokens ? seen : max_tokens, n_splits);
   const int T = p.d / kTileChannels;
   const int64_t q_rows = (int64_t)n_q * Hq, few_rows = k.mixed ? (int64_t)p.B * p.H * kFewRows : q_rows;
   const int64_t few = k.mixed ? p.B : paged_tiles(p, Hq / p.H, n_q, kFewRows);
   const int64_t many = paged_tiles(p, Hq / p.H, n_q, chunk_rows(T));
-  if (!launches((double)few * p.H * k.few, kWaveSize) || !launches((double)many * p.H * k.many, kWaveSize * chunk_waves(T)))
+  if (!launches(Kernels::few_groups(p, k, few), kWaveSize) || !launches((double)many * p.H * k.many, kWaveSize * chunk_waves(T)))
     return MUSTAFAR_EINVAL;
   if ((k.few > 1 && !launches((double)merge_groups(few_rows, T), kMergeThreads)) ||
       (k.many > 1 && !launches((double)merge_groups(q_rows, T), kMergeThreads)))
     return MUSTAFAR_EINVAL;
+  *plan = k;
   a->p = p;
   a->few = k.few;
   a->many = k.many;

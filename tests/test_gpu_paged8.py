@@ -256,6 +256,53 @@ def test_splits(d, n_splits, new, window, sinks):
     attend(torch.bfloat16, "int8", 2, 4, d, 64, 16, [2900, 3, 300], new, window=window, sinks=sinks, n_splits=n_splits, seed=n_splits)
 
 
+FLAT = 10 ** 7      # a bound of requests' lengths for which ranges are shared out among them
+
+
+@pytest.mark.parametrize("dtype,code,d", [(torch.float16, "e4m3", 64), (torch.bfloat16, "int8", 128), (torch.float16, "int8", 256)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (500, 3)])
+@pytest.mark.parametrize("H,G,new,cached", [
+    (1, 4, [1, 1, 1, 1], [9000, 3, 700, 0]), (2, 1, [1, 0, 2, 1], [2500, 40, 5000, 63]), (2, 4, [1, 60, 1, 0, 3], [3000, 500, 1, 9, 2000]),
+    (1, 16, [1, 1, 1], [64, 2000, 1]), (3, 2, [1] * 70, list(range(0, 2100, 30))), (1, 1, [1] * 200, [17 * b % 900 for b in range(200)])])
+def test_ranges_are_shared_out_by_the_requests_lengths(dtype, code, d, window, sinks, H, G, new, cached):
+    """Requests of very different lengths, some without rows or of many rows, of up to 64 and of more."""
+    attend(dtype, code, H, G, d, 16, 16, cached, new, window=window, sinks=sinks, seed=len(new) + d, max_tokens=FLAT,
+           max_q=max(new) if max(new) * G > 16 else 1)
+
+
+@pytest.mark.parametrize("B", [256, 500])
+def test_as_many_requests_as_have_ranges(B):
+    """One range a request and hardly more; the launch has no more than there are."""
+    rng = random.Random(B)
+    attend(torch.float16, "e4m3", 1, 2, 64, 16, 16, [rng.choice([0, 5, 100, 800]) for _ in range(B)], [1] * B, seed=B, max_tokens=FLAT)
+    attend(torch.bfloat16, "e4m3", 2, 2, 64, 16, 16, [rng.choice([0, 5, 100, 800]) for _ in range(B)], [rng.choice([0, 1, 2]) for _ in range(B)],
+           seed=B, max_tokens=FLAT, max_q=2)
+
+
+@pytest.mark.parametrize("new,max_q", [([40, 1, 3], 1), ([1, 17, 5], 4), ([100, 70, 1], 2)])
+def test_wrong_bounds_where_ranges_are_shared_out(new, max_q):
+    """Requests of many rows though the call says that all have few."""
+    attend(torch.float16, "int8", 2, 4, 128, 16, 16, [700, 3000, 20], new, seed=5, max_q=max_q, max_tokens=FLAT)
+
+
+@pytest.mark.parametrize("junk", [0, 255])
+@pytest.mark.parametrize("new", [[1, 1, 0, 1], [1, 50, 0, 2], [2, 3, 1, 4]])
+def test_what_a_workspace_held_takes_no_part_where_ranges_are_shared_out(new, junk):
+    """Also of rows that see nothing and of rows that are no request's."""
+    lens = [3000, 1, 500, 90]
+    cache, ks, vs = fill8(4, 2, 128, 16, lens, torch.bfloat16, "e4m3", 16, seed=61)
+    n = sum(new)
+    q = torch.randn(n + 3, 8, 128, device="cuda").bfloat16()
+    need = mf.mustafar_paged8_attn_workspace_bytes(cache, 8, n + 3, max(new), FLAT)
+    ws = torch.full((need,), junk, dtype=torch.uint8, device="cuda")
+    out = torch.full_like(q, 6.0)
+    mf.mustafar_paged8_attn(q, cache, starts(new), max_q=max(new), max_tokens=FLAT, ws=ws, out=out)
+    check(out[:n], q[:n], ks, vs, new, lens, torch.bfloat16, label="workspace")
+    assert bool((out[n:] == 6).all())
+    mf.mustafar_paged8_attn(q, cache, starts([0, 0, 0, 0]), max_q=1, max_tokens=FLAT, ws=ws.fill_(junk), out=out.fill_(6.0))
+    assert bool((out == 6).all())       # a refused plan's step
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("code", CODES)
 @pytest.mark.parametrize("new", [[1, 1], [50, 150]])
@@ -507,18 +554,18 @@ def test_a_captured_step_replays(dtype, code):
 
 
 def test_a_workspace_that_two_captured_calls_share():
-    """Two graphs of calls of different sizes with one workspace, replayed in turns with eager calls between them."""
+    """Graphs of calls of different sizes with one workspace, replayed in turns with eager calls between them."""
     dtype, made = torch.bfloat16, []
-    for i, (cached, new) in enumerate((([3000, 40], [1, 1]), ([900, 100], [60, 1]))):
+    for i, (cached, new, most) in enumerate((([3000, 40], [1, 1], 3100), ([900, 100], [60, 1], 960), ([5000, 700], [1, 2], FLAT))):
         lens = [a + b for a, b in zip(cached, new)]
         cache, ks, vs = fill8(2, 2, 128, 16, lens, dtype, "e4m3", 16, seed=40 + i)
-        made.append((cache, ks, vs, lens, new, torch.randn(sum(new), 8, 128, device="cuda").to(dtype), starts(new)))
-    need = max(mf.mustafar_paged8_attn_workspace_bytes(m[0], 8, sum(m[4]), max(m[4]), max(m[3])) for m in made)
+        made.append((cache, ks, vs, lens, new, torch.randn(sum(new), 8, 128, device="cuda").to(dtype), starts(new), most))
+    need = max(mf.mustafar_paged8_attn_workspace_bytes(m[0], 8, sum(m[4]), max(m[4]), m[7]) for m in made)
     assert need > 0
     ws, graphs, outs = torch.empty(need, dtype=torch.uint8, device="cuda"), [], []
 
     def call(m, out):
-        mf.mustafar_paged8_attn(m[5], m[0], m[6], max_q=max(m[4]), max_tokens=max(m[3]), out=out, ws=ws)
+        mf.mustafar_paged8_attn(m[5], m[0], m[6], max_q=max(m[4]), max_tokens=m[7], out=out, ws=ws)
     for m in made:
         out = torch.zeros_like(m[5])
         call(m, out)
@@ -528,7 +575,7 @@ def test_a_workspace_that_two_captured_calls_share():
             call(m, out)
         graphs.append(graph)
         outs.append(out)
-    for i in (0, 1, 1, 0, 0, 1):
+    for i in (0, 1, 2, 1, 0, 2, 0, 1, 2):
         outs[i].fill_(9.0)
         graphs[i].replay()
         torch.cuda.synchronize()
