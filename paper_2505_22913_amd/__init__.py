@@ -707,11 +707,24 @@ def _page_state(B, n_pages, max_pages, device, table, state, free):
     return table, state, free
 
 
-def _current(cache, what="the cache is"):
+def _current(cache):
     """The cache's device has to be the current one: the launches go there."""
     import torch
     if cache.device.index != torch.cuda.current_device():
-        raise ValueError(f"{what} on {cache.device}, the current device is cuda:{torch.cuda.current_device()}")
+        raise ValueError(f"the cache is on {cache.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _launch(owner, stream, what="the cache is") -> int | None:
+    """Raw handle of `stream`, or of torch's current stream, for a call on tensors of the owner's device, which has to be the
+    current one (one look-up of it for both)."""
+    import torch
+    index = torch.cuda.current_device()
+    if owner.device.index != index:
+        raise ValueError(f"{what} on {owner.device}, the current device is cuda:{index}")
+    if stream is not None:
+        return stream.cuda_stream
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return _stream(None) if raw is None else raw(index)
 
 
 def _rows(name, x, n, heads, cache):
@@ -784,22 +797,24 @@ def mustafar_paged_gather(cache: PagedCache, n_max: int, first=None, x_k=None, x
     """The requests' tokens first[b] (int32 [B], None: 0) .. as dense fp16 x_k, x_v [B][H][n_max][d], the
     input of mustafar_window_prefill; rows behind a request's last are left as they were (0 in
     tensors that the call makes)."""
-    _current(cache)
     return _gather("mustafar_paged_gather", cache, cache.desc, n_max, first, x_k, x_v, stream)
 
 
 def _gather(fn, cache, desc, n_max, first, x_k, x_v, stream):
     import torch
-    shape = (cache.desc.B, cache.desc.H, int(n_max), cache.desc.d)
-    with _on_stream(stream):
-        x_k = torch.zeros(shape, dtype=torch.float16, device=cache.device) if x_k is None else x_k
-        x_v = torch.zeros(shape, dtype=torch.float16, device=cache.device) if x_v is None else x_v
+    pages = cache.desc
+    shape = (pages.B, pages.H, int(n_max), pages.d)
+    handle = _launch(cache, stream)
+    if x_k is None or x_v is None:
+        with _on_stream(stream):
+            x_k = torch.zeros(shape, dtype=torch.float16, device=cache.device) if x_k is None else x_k
+            x_v = torch.zeros(shape, dtype=torch.float16, device=cache.device) if x_v is None else x_v
     _want("x_k", x_k, shape, torch.float16, cache.device)
     _want("x_v", x_v, shape, torch.float16, cache.device)
     if first is not None:
         _want("first", first, (shape[0],), torch.int32, cache.device)
     _check(fn, getattr(lib(), fn)(
-        ctypes.byref(desc), _dptr(first), _dptr(x_k), _dptr(x_v), shape[2], _stream(stream)))
+        ctypes.byref(desc), None if first is None else first.data_ptr(), x_k.data_ptr(), x_v.data_ptr(), shape[2], handle))
     return x_k, x_v
 
 
@@ -818,7 +833,6 @@ def mustafar_paged_attn(q, cache: PagedCache, cu, max_q: int | None = None, max_
     row each if n_q <= B, else n_q; all that a table can hold); with bounds near the truth calls are faster.
     Returns out [n_q][Hq][d]; rows from cu[B] on (all of a refused plan's) are left as they were, 0 in a tensor that
     the call makes."""
-    _current(cache)
     return _paged_attn("mustafar_paged_attn", mustafar_paged_attn_workspace_bytes, q, cache, cache.desc, cu, max_q, max_tokens,
                        window, sinks, scale, out, n_splits, ws, stream)
 
@@ -833,6 +847,7 @@ def _paged_attn(fn, workspace_bytes, q, cache, desc, cu, max_q, max_tokens, wind
     if max_tokens is None:
         max_tokens = min(cache.desc.max_pages, cache.desc.n_pages) * cache.desc.page_tokens
     max_q, max_tokens, window, sinks = _int32(max_q), _int32(max_tokens), _int32(window), _int32(sinks)
+    handle = _launch(cache, stream)
     qs = _rows("q", q, n_q, Hq, cache)
     _want("cu", cu, (B + 1,), torch.int32, cache.device)
     if ws is None:
@@ -847,9 +862,9 @@ def _paged_attn(fn, workspace_bytes, q, cache, desc, cu, max_q, max_tokens, wind
             out = torch.zeros((n_q, Hq, d), dtype=cache.dtype, device=cache.device)
     os_ = _rows("out", out, n_q, Hq, cache)
     _check(fn, getattr(lib(), fn)(
-        _dptr(q), qs, n_q, Hq, ctypes.byref(desc), _dptr(cu), window, sinks, float(scale), _dptr(out),
-        os_, max_q, max_tokens, int(n_splits), _dptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
-        _stream(stream)))
+        q.data_ptr(), qs, n_q, Hq, ctypes.byref(desc), cu.data_ptr(), window, sinks, float(scale), out.data_ptr(),
+        os_, max_q, max_tokens, int(n_splits), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.nbytes,
+        handle))
     return out
 
 
@@ -917,7 +932,6 @@ class PagedCache8:
 def _codes(cache):
     if not isinstance(cache, PagedCache8):
         raise ValueError(f"a PagedCache8 expected, not {type(cache).__name__}")
-    _current(cache)
 
 
 def mustafar_paged8_write(cache: PagedCache8, k_new, v_new, cu, stream=None) -> None:
@@ -925,12 +939,13 @@ def mustafar_paged8_write(cache: PagedCache8, k_new, v_new, cu, stream=None) -> 
     every request b of a planned step, quantised into its pages. A block that holds earlier tokens keeps its exponent, or
     gets the larger one that the new tokens need and its codes are rounded to it. Rows from cu[B] on are left out."""
     import torch
-    n, H = k_new.shape[0], cache.desc.H
     _codes(cache)
+    n, H = k_new.shape[0], cache.desc.H
+    handle = _launch(cache, stream)
     ks, vs = _rows("k_new", k_new, n, H, cache), _rows("v_new", v_new, n, H, cache)
     _want("cu", cu, (cache.desc.B + 1,), torch.int32, cache.device)
     _check("mustafar_paged8_write", lib().mustafar_paged8_write(
-        ctypes.byref(cache.desc8), _dptr(k_new), ks, _dptr(v_new), vs, _dptr(cu), n, _stream(stream)))
+        ctypes.byref(cache.desc8), k_new.data_ptr(), ks, v_new.data_ptr(), vs, cu.data_ptr(), n, handle))
 
 
 def mustafar_paged8_gather(cache: PagedCache8, n_max: int, first=None, x_k=None, x_v=None, stream=None):
@@ -993,40 +1008,50 @@ def mustafar_rope(rope: Rope, q, k=None, positions=None, cache=None, cu=None, in
     from cu[B] on are left as they were, 0 in tensors that the call makes. inverse: turned back, which is the gradient.
     Returns (out_q, out_k), new tensors unless given; out_q=q, out_k=k turns in place."""
     import torch
-    types = {torch.float16: FP16, torch.bfloat16: BF16}
-    if q.dim() != 3 or q.dtype not in types:
-        raise ValueError(f"q: [n][Hq][d] of float16 or bfloat16 expected, not {tuple(q.shape)} of {q.dtype}")
+    dtype, device = q.dtype, rope.device
+    if q.dim() != 3 or (dtype is not torch.float16 and dtype is not torch.bfloat16):
+        raise ValueError(f"q: [n][Hq][d] of float16 or bfloat16 expected, not {tuple(q.shape)} of {dtype}")
     n, Hq, d = q.shape
-    if k is not None and (k.dim() != 3 or k.shape[0] != n or k.shape[2] != d):
-        raise ValueError(f"k: [{n}][H][{d}] expected, not {tuple(k.shape)}")
-    if k is None and out_k is not None:
-        raise ValueError("out_k without k")
-    if (positions is None) == (cache is None) or (cache is None) != (cu is None):
-        raise ValueError("positions, or a cache and cu")
-    H = 0 if k is None else k.shape[1]
-    _current(rope, "rates are")
+    handle = _launch(rope, stream, "rates are")
     if positions is not None:
-        _want("positions", positions, (n,), torch.int32, rope.device)
+        if cache is not None or cu is not None:
+            raise ValueError("positions, or a cache and cu")
+        _want("positions", positions, (n,), torch.int32, device)
+        where = positions.data_ptr(), None, None
     else:
-        _current(cache)
-        _want("cu", cu, (cache.desc.B + 1,), torch.int32, rope.device)
-    side = []
-    for name, x, heads, out in (("q", q, Hq, out_q), ("k", k, H, out_k)):
-        if x is None:
-            side.append((None, 0, 0, None, 0))
-            continue
-        stride = _row_stride(name, x, n, heads, d, q.dtype, rope.device)
-        if out is None:
-            with _on_stream(stream):
-                make = torch.empty if cache is None else torch.zeros
-                out = make((n, heads, d), dtype=q.dtype, device=rope.device)
-        side.append((x, stride, heads, out, _row_stride(f"out_{name}", out, n, heads, d, q.dtype, rope.device)))
-    (_, qs, _, out_q, oqs), (_, ks, _, out_k, oks) = side
+        if cache is None or cu is None:
+            raise ValueError("positions, or a cache and cu")
+        if cache.device != device:
+            raise ValueError(f"rates are on {device}, the cache on {cache.device}")
+        _want("cu", cu, (cache.desc.B + 1,), torch.int32, device)
+        where = None, ctypes.byref(cache.desc), cu.data_ptr()
+    qs = _row_stride("q", q, n, Hq, d, dtype, device)
+    if out_q is None:
+        out_q = _rope_out(q, cache, stream)
+    oqs = _row_stride("out_q", out_q, n, Hq, d, dtype, device)
+    if k is None:
+        if out_k is not None:
+            raise ValueError("out_k without k")
+        keys = outs = None, 0
+        H = 0
+    else:
+        if k.dim() != 3:
+            raise ValueError(f"k: [{n}][H][{d}] expected, not {tuple(k.shape)}")
+        H = k.shape[1]
+        keys = k.data_ptr(), _row_stride("k", k, n, H, d, dtype, device)
+        if out_k is None:
+            out_k = _rope_out(k, cache, stream)
+        outs = out_k.data_ptr(), _row_stride("out_k", out_k, n, H, d, dtype, device)
     _check("mustafar_rope", lib().mustafar_rope(
-        ctypes.byref(rope.desc), _dptr(q), qs, Hq, _dptr(k), ks, H, d, n, types[q.dtype], _dptr(positions),
-        None if cache is None else ctypes.byref(cache.desc), _dptr(cu), int(bool(inverse)), _dptr(out_q), oqs, _dptr(out_k),
-        oks, _stream(stream)))
+        ctypes.byref(rope.desc), q.data_ptr(), qs, Hq, *keys, H, d, n, FP16 if dtype is torch.float16 else BF16, *where,
+        1 if inverse else 0, out_q.data_ptr(), oqs, *outs, handle))
     return out_q, out_k
+
+
+def _rope_out(x, cache, stream):
+    import torch
+    with _on_stream(stream):
+        return (torch.empty if cache is None else torch.zeros)(x.shape, dtype=x.dtype, device=x.device)
 
 
 ROUTE_DEFAULT, ROUTE_WALKS, ROUTE_MATRIX_CORES = 0, 1, 2

@@ -2,6 +2,7 @@
 // and paged8_attn.hip) and of rotary positions (rope.hip).
 #pragma once
 
+#include "mustafar.h"
 #include "paged.h"
 
 namespace mf {
@@ -105,18 +106,27 @@ struct RopeArgs {
 };
 // A workgroup of k_rope: kRopeTokens tokens of so many heads.
 constexpr int kRopeThreads = 256, kRopeTokens = 4, kMaxRopeHeads = 1 << 16;
+enum RopeForm { kRopeHalf, kRopePairs, kRopeAny };
 struct RopePlan {
+  RopeForm form;
   int heads, head_groups;
   int64_t groups;
 };
 inline RopePlan rope_plan(const RopeArgs& a) {
   const int all = a.Hq + a.H;
   RopePlan r;
-  r.heads = all < 8 ? all : 8;
+  const bool half = a.layout == MUSTAFAR_ROPE_HALF;
+  r.form = a.rot % (half ? 16 : 8) != 0 ? kRopeAny : half ? kRopeHalf : kRopePairs;
+  // (12 and two pieces of rows a thread where they go through LDS: 24.8 us for 26.7 with 8, a part of 20 of 80 channels of 4096
+  // tokens of 64 heads; else 8 and one piece: 41.4 us for 42.1 with 20 heads, 45.7 with two pieces, 9600 tokens of 40 heads of 128)
+  // 32 KB of LDS at most.
+  const int fit = (8192 / ((a.rot + 7) & ~7) - 8) / 2, most = r.form != kRopeAny ? 8 : fit < 12 ? fit : 12;
+  r.heads = all < most ? all : most;
   r.head_groups = (all + r.heads - 1) / r.heads;
   r.groups = ((int64_t)a.n + kRopeTokens - 1) / kRopeTokens * r.head_groups;
   return r;
 }
+
 hipError_t launch_rope(const RopeArgs& a, const RopePlan& plan, hipStream_t s);
 
 }  // namespace mf

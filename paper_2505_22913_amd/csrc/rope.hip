@@ -1,7 +1,6 @@
 // Rotary positions (gfx950): pairs of channels of queries and keys turned by their token's position.
 #include "mf_device.h"
 #include "paged8.h"
-#include "mustafar.h"
 #include "paged_attn.h"
 
 namespace mf {
@@ -13,8 +12,6 @@ namespace mf {
 //
 // The angle is p * r in 64 bits, reduced to a part of a turn there: in 32 bits position 10^6 would be off by up to 0.06 radians.
 // ------------------------------------------------------------------------------------------
-enum RopeForm { kRopeHalf, kRopePairs, kRopeAny };
-
 // What a row's request is, of row t of a step.
 struct RopeRow {
   int64_t pos;
@@ -31,11 +28,46 @@ template <int FORM, bool BF16>
 __global__ __launch_bounds__(kRopeThreads) void k_rope(RopeArgs a, int heads, int head_groups) {
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ int valid[kRopeTokens];
+  const bool half = a.layout == MUSTAFAR_ROPE_HALF;
   const int pairs = a.rot / 2, pad = (pairs + 7) & ~7, all = a.Hq + a.H;
   float* const turns = reinterpret_cast<float*>(smem);  // [kRopeTokens][cosines, sines][pad]
-  uint16_t* const stage = reinterpret_cast<uint16_t*>(turns + kRopeTokens * 2 * pad);
+  // kRopeAny: [kRopeTokens][channels], and the rows' channels that are turned, up to a whole piece
+  const int channels = (a.rot + 7) & ~7;
+  float2* const factors = reinterpret_cast<float2*>(smem);
+  uint16_t* const stage = reinterpret_cast<uint16_t*>(factors + kRopeTokens * channels);
   const int tile = (int)(blockIdx.x / head_groups), h0 = (int)(blockIdx.x % head_groups) * heads, nh = min(heads, all - h0);
   const int t0 = tile * kRopeTokens, wave = (int)(threadIdx.x / kWave), lane = (int)lane_id();
+  // Row r of the workgroup: token r / nh, head h0 + r % nh. A thread has one piece of every step-th row.
+  const bool in_place = (a.Hq == 0 || a.out_q == a.q) && (a.H == 0 || a.out_k == a.k);
+  const int turned = FORM == kRopeHalf ? a.rot / 16 : (a.rot + 7) / 8;  // pieces that are turned; the others are copied
+  const int pieces = in_place ? turned : FORM == kRopeAny ? a.d / 8 : turned + (a.d - a.rot) / 8;
+  const int piece = (int)threadIdx.x % pieces, sub = (int)threadIdx.x / pieces, step = kRopeThreads / pieces;
+  const int rows = sub < step ? kRopeTokens * nh : 0;
+  const bool copied = piece >= turned;
+  const int at = FORM == kRopeAny || !copied ? 8 * piece : a.rot + 8 * (piece - turned);
+  auto from = [&](int tok, int h) {
+    return h < a.Hq ? a.q + (int64_t)(t0 + tok) * a.q_stride + h * a.d : a.k + (int64_t)(t0 + tok) * a.k_stride + (h - a.Hq) * a.d;
+  };
+  auto to = [&](int tok, int h) {
+    return h < a.Hq ? a.out_q + (int64_t)(t0 + tok) * a.out_q_stride + h * a.d
+                    : a.out_k + (int64_t)(t0 + tok) * a.out_k_stride + (h - a.Hq) * a.d;
+  };
+  struct Item {
+    u32x4 x, partner;
+  };
+  constexpr int kItems = FORM == kRopeAny ? 2 : 1;
+  Item items[kItems];
+  auto load = [&](int r0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      const int r = r0 + i * step, tok = r / nh;
+      if (r >= rows || t0 + tok >= a.n) continue;
+      const uint16_t* const x = from(tok, h0 + r - tok * nh) + at;
+      items[i].x = *reinterpret_cast<const u32x4*>(x);
+      if (FORM == kRopeHalf && !copied) items[i].partner = *reinterpret_cast<const u32x4*>(x + pairs);
+    }
+  };
+  load(sub);  // (under way while the angles are computed)
   {
     const RopeRow row = rope_row(a, t0 + wave);
     if (lane == 0) valid[wave] = row.valid;
@@ -44,107 +76,88 @@ __global__ __launch_bounds__(kRopeThreads) void k_rope(RopeArgs a, int heads, in
       x -= rint(x);
       float s, c;
       sincospif((float)(2 * x), &s, &c);
-      turns[(2 * wave) * pad + i] = c * a.magnitude;
-      turns[(2 * wave + 1) * pad + i] = (a.inverse ? -s : s) * a.magnitude;
+      c *= a.magnitude;
+      s *= a.inverse ? -a.magnitude : a.magnitude;
+      if constexpr (FORM == kRopeAny) {  // of each channel: what it and its partner are multiplied by
+        factors[wave * channels + (half ? i : 2 * i)] = make_float2(c, -s);
+        factors[wave * channels + (half ? i + pairs : 2 * i + 1)] = make_float2(c, s);
+      } else {
+        turns[(2 * wave) * pad + i] = c;
+        turns[(2 * wave + 1) * pad + i] = s;
+      }
     }
   }
   __syncthreads();
-  // Row r of the workgroup: token r / nh, head h0 + r % nh.
-  const bool in_place = (a.Hq == 0 || a.out_q == a.q) && (a.H == 0 || a.out_k == a.k);
-  const int turned = FORM == kRopeHalf ? a.rot / 16 : (a.rot + 7) / 8;  // pieces that are turned; the others are copied
-  const int pieces = turned + (in_place ? 0 : (a.d - a.rot) / 8);
-  const int piece = (int)threadIdx.x % pieces, sub = (int)threadIdx.x / pieces, step = kRopeThreads / pieces;
-  const int rows = kRopeTokens * nh;
-  auto from = [&](int tok, int h) {
-    return h < a.Hq ? a.q + (int64_t)(t0 + tok) * a.q_stride + h * a.d : a.k + (int64_t)(t0 + tok) * a.k_stride + (h - a.Hq) * a.d;
-  };
-  auto to = [&](int tok, int h) {
-    return h < a.Hq ? a.out_q + (int64_t)(t0 + tok) * a.out_q_stride + h * a.d
-                    : a.out_k + (int64_t)(t0 + tok) * a.out_k_stride + (h - a.Hq) * a.d;
-  };
-  if constexpr (FORM == kRopeAny) {
-    const int whole = in_place ? turned : a.d / 8;
-    for (int i = (int)threadIdx.x; i < rows * whole; i += kRopeThreads) {
-      const int r = i / whole, c = i - r * whole, tok = r / nh;
-      if (!valid[tok]) continue;
-      *reinterpret_cast<u32x4*>(stage + r * a.d + 8 * c) = *reinterpret_cast<const u32x4*>(from(tok, h0 + r - tok * nh) + 8 * c);
+  for (int r0 = sub; r0 < rows; r0 += kItems * step) {
+    if (r0 != sub) load(r0);
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      const int r = r0 + i * step, tok = r / nh;
+      if (r >= rows || !valid[tok]) continue;
+      uint16_t* const y = to(tok, h0 + r - tok * nh) + at;
+      const u32x4 x = items[i].x;
+      if (copied) {
+        *reinterpret_cast<u32x4*>(y) = x;
+      } else if constexpr (FORM == kRopeAny) {
+        *reinterpret_cast<u32x4*>(stage + r * channels + at) = x;
+      } else if constexpr (FORM == kRopeHalf) {
+        const u32x4 z = items[i].partner;
+        const float *cosine = turns + 2 * tok * pad + at, *sine = cosine + pad;
+        u32x4 ya, yb;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float p[2], q[2];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const float u = to_float<BF16>(k ? x[e] >> 16 : x[e] & 0xffffu), v = to_float<BF16>(k ? z[e] >> 16 : z[e] & 0xffffu);
+            const float c = cosine[2 * e + k], s = sine[2 * e + k];
+            p[k] = fmaf(u, c, -v * s);
+            q[k] = fmaf(v, c, u * s);
+          }
+          ya[e] = pack2<BF16>(p[0], p[1]);
+          yb[e] = pack2<BF16>(q[0], q[1]);
+        }
+        *reinterpret_cast<u32x4*>(y) = ya;
+        *reinterpret_cast<u32x4*>(y + pairs) = yb;
+      } else {
+        const float *cosine = turns + 2 * tok * pad + 4 * piece, *sine = cosine + pad;
+        u32x4 ys;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float u = to_float<BF16>(x[e] & 0xffffu), v = to_float<BF16>(x[e] >> 16), c = cosine[e], s = sine[e];
+          ys[e] = pack2<BF16>(fmaf(u, c, -v * s), fmaf(v, c, u * s));
+        }
+        *reinterpret_cast<u32x4*>(y) = ys;
+      }
     }
+  }
+  if constexpr (FORM == kRopeAny) {
     __syncthreads();
-    for (int i = (int)threadIdx.x; i < rows * whole; i += kRopeThreads) {
-      const int r = i / whole, c8 = 8 * (i - r * whole), tok = r / nh;
+    for (int i = (int)threadIdx.x; i < kRopeTokens * nh * turned; i += kRopeThreads) {
+      const int r = i / turned, c8 = 8 * (i - r * turned), tok = r / nh;
       if (!valid[tok]) continue;
-      const uint16_t* const x = stage + r * a.d;
-      const float *cosine = turns + 2 * tok * pad, *sine = cosine + pad;
+      const uint16_t* const x = stage + r * channels;
+      const float2* const f = factors + tok * channels;
       float y[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int c = c8 + e;
+        const int c = c8 + e, other = half ? (c < pairs ? c + pairs : c - pairs) : c ^ 1;
         y[e] = to_float<BF16>(x[c]);
-        if (c < a.rot) {
-          const bool second = a.layout == MUSTAFAR_ROPE_HALF ? c >= pairs : (c & 1) != 0;
-          const int pair = a.layout == MUSTAFAR_ROPE_HALF ? (second ? c - pairs : c) : c / 2;
-          const int other = a.layout == MUSTAFAR_ROPE_HALF ? (second ? c - pairs : c + pairs) : c ^ 1;
-          const float s = sine[pair], z = to_float<BF16>(x[other]);
-          y[e] = fmaf(y[e], cosine[pair], z * (second ? s : -s));
-        }
+        if (c < a.rot) y[e] = fmaf(y[e], f[c].x, to_float<BF16>(x[other]) * f[c].y);
       }
       *reinterpret_cast<u32x4*>(to(tok, h0 + r - tok * nh) + c8) =
           (u32x4){pack2<BF16>(y[0], y[1]), pack2<BF16>(y[2], y[3]), pack2<BF16>(y[4], y[5]), pack2<BF16>(y[6], y[7])};
-    }
-    return;
-  }
-  if (sub >= step) return;
-  for (int r = sub; r < rows; r += step) {
-    const int tok = r / nh, h = h0 + r - tok * nh;
-    if (!valid[tok]) continue;
-    const uint16_t* const x = from(tok, h);
-    uint16_t* const y = to(tok, h);
-    if (piece >= turned) {
-      const int c = a.rot + 8 * (piece - turned);
-      *reinterpret_cast<u32x4*>(y + c) = *reinterpret_cast<const u32x4*>(x + c);
-      continue;
-    }
-    if constexpr (FORM == kRopeHalf) {
-      const u32x4 xa = *reinterpret_cast<const u32x4*>(x + 8 * piece), xb = *reinterpret_cast<const u32x4*>(x + pairs + 8 * piece);
-      const float *cosine = turns + 2 * tok * pad + 8 * piece, *sine = cosine + pad;
-      u32x4 ya, yb;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float p[2], q[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const float u = to_float<BF16>(i ? xa[e] >> 16 : xa[e] & 0xffffu), v = to_float<BF16>(i ? xb[e] >> 16 : xb[e] & 0xffffu);
-          const float c = cosine[2 * e + i], s = sine[2 * e + i];
-          p[i] = fmaf(u, c, -v * s);
-          q[i] = fmaf(v, c, u * s);
-        }
-        ya[e] = pack2<BF16>(p[0], p[1]);
-        yb[e] = pack2<BF16>(q[0], q[1]);
-      }
-      *reinterpret_cast<u32x4*>(y + 8 * piece) = ya;
-      *reinterpret_cast<u32x4*>(y + pairs + 8 * piece) = yb;
-    } else {
-      const u32x4 xs = *reinterpret_cast<const u32x4*>(x + 8 * piece);
-      const float *cosine = turns + 2 * tok * pad + 4 * piece, *sine = cosine + pad;
-      u32x4 ys;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float u = to_float<BF16>(xs[e] & 0xffffu), v = to_float<BF16>(xs[e] >> 16), c = cosine[e], s = sine[e];
-        ys[e] = pack2<BF16>(fmaf(u, c, -v * s), fmaf(v, c, u * s));
-      }
-      *reinterpret_cast<u32x4*>(y + 8 * piece) = ys;
     }
   }
 }
 
 hipError_t launch_rope(const RopeArgs& a, const RopePlan& plan, hipStream_t s) {
-  const bool half = a.layout == MUSTAFAR_ROPE_HALF;
-  const int form = a.rot % (half ? 16 : 8) != 0 ? kRopeAny : half ? kRopeHalf : kRopePairs;
-  const size_t lds = kRopeTokens * (8 * (size_t)((a.rot / 2 + 7) & ~7) + (form == kRopeAny ? 2 * (size_t)plan.heads * a.d : 0));
+  const size_t channels = (a.rot + 7) & ~7;
+  const size_t lds = kRopeTokens * (plan.form == kRopeAny ? (8 + 2 * (size_t)plan.heads) * channels : 8 * (size_t)((a.rot / 2 + 7) & ~7));
   auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3((uint32_t)plan.groups), dim3(kRopeThreads), lds, s, a, plan.heads, plan.head_groups);
   };
-  switch (2 * form + a.bf16) {
+  switch (2 * plan.form + a.bf16) {
     case 2 * kRopeHalf: launch(k_rope<kRopeHalf, false>); break;
     case 2 * kRopeHalf + 1: launch(k_rope<kRopeHalf, true>); break;
     case 2 * kRopePairs: launch(k_rope<kRopePairs, false>); break;

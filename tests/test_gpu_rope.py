@@ -60,6 +60,17 @@ def test_layouts_parts_and_sizes(dtype, layout, d, rot, Hq, H):
                 assert torch.equal(again[:, :Hq], out_q) and torch.equal(other, out_k) and torch.equal(again[:, Hq:], on[:, Hq:])
 
 
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("d,rot,Hq,H", [(512, 510, 20, 3), (512, 18, 40, 8), (80, 20, 33, 31), (256, 254, 64, 8), (16, 2, 1, 1)])
+def test_many_heads_whose_pairs_lie_in_no_pieces(layout, d, rot, Hq, H):
+    x = torch.randn(6, Hq + H, d, generator=torch.Generator().manual_seed(d + rot)).bfloat16()
+    positions = torch.tensor([0, 5, -3, 70000, 1, 2], dtype=torch.int32)
+    on = x.cuda()
+    q, k = mf.mustafar_rope(mf.Rope(rot, layout=layout), on[:, :Hq], on[:, Hq:], positions=positions.cuda())
+    close(torch.cat([q, k], 1), x, positions, oracle8.rates(rot, 10000.0), rot, layout)
+    assert torch.equal(torch.cat([q, k], 1)[..., rot:], on[..., rot:])
+
+
 @pytest.mark.parametrize("scaling,kw", [("linear", dict(factor=8.0)), ("base", dict(factor=4.0)),
                                         ("turns", dict(factor=8.0, original_len=8192, low_turns=1.0, high_turns=4.0))])
 @pytest.mark.parametrize("dtype", DTYPES)
