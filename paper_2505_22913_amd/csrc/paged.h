@@ -7,6 +7,8 @@
 
 namespace mf {
 
+constexpr int64_t kLastLevel = 256 << 20;  // bytes of the last cache
+
 struct PagedView {
   uint16_t* k;
   uint16_t* v;

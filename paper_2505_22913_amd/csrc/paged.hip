@@ -249,8 +249,6 @@ hipError_t launch_paged_write(const PagedView& p, const uint16_t* k_new, int64_t
 // outputs of 537 MB take 112 us non-temporal (5.9 TB/s, reads and writes) and 132 through the caches (with a kernel that
 // reads them next, 494 and 502); of 134 MB, which the last cache holds for that kernel, 128 and 117 with it.
 // ------------------------------------------------------------------------------------------
-constexpr int64_t kLastLevel = 256 << 20;  // bytes of the last cache
-
 __device__ __forceinline__ uint32_t bf16_pair_to_fp16(uint32_t w) {
   uint32_t r = 0u;
 #pragma unroll

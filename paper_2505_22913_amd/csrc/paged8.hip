@@ -68,17 +68,11 @@ __global__ __launch_bounds__(kWrite8Threads) void k_paged8_write(Paged8View c, c
   const int head = (int)(blockIdx.x % groups) * (kWaves >> log2_waves) + (wave >> log2_waves), sub = wave & ((1 << log2_waves) - 1);
   const BlockTile t = block_tile(p, cu, n_new, c.log2_block, tile);
   if (t.block > t.last) return;  // (all of the workgroup)
-  const int page = p.table[(int64_t)t.b * p.max_pages + (t.block >> p.log2_page)];
-  if ((uint32_t)page >= (uint32_t)p.n_pages) return;
   const bool work = head < 2 * p.H, values = head >= p.H;
   const int h = work ? values ? head - p.H : head : 0, place = t.block & ((1 << p.log2_page) - 1);
   const uint16_t* const x_new = (values ? v_new : k_new) + h * p.d;
   const int64_t x_stride = values ? v_stride : k_stride;
-  uint8_t* const codes = reinterpret_cast<uint8_t*>(values ? p.v : p.k) + (int64_t)page * p.page_stride + (int64_t)h * p.head_stride;
-  uint8_t* const scale = (values ? c.v_scale : c.k_scale) + (((int64_t)page * p.H + h) << (p.log2_page - c.log2_block)) + (place >> c.log2_block);
-  const bool older = t.block < t.first;
-  const uint32_t before = older && work ? *scale : 0u;
-  // Rows of this wave: positions t.block + 16 sub + kRowsPerLoad i + lane / kPieces.
+  // Rows of this wave: positions t.block + row + kRowsPerLoad i. The new ones are under way while the page is looked up.
   const int row = kWrite8Rows * sub + lane / kPieces, c8 = 8 * (lane % kPieces);
   u32x4 x[kLoads];
   float top = 0.f;
@@ -86,8 +80,14 @@ __global__ __launch_bounds__(kWrite8Threads) void k_paged8_write(Paged8View c, c
   for (int i = 0; i < kLoads; ++i) {
     const int pos = t.block + row + kRowsPerLoad * i, r = t.row0 + pos - t.first;
     x[i] = (u32x4){};
-    if (work && pos >= t.first && pos <= t.last && r < n_new) x[i] = *reinterpret_cast<const u32x4*>(x_new + r * x_stride + c8);
+    if (work && pos >= t.first && pos <= t.last && r < n_new) x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(x_new + r * x_stride + c8));
   }
+  const int page = p.table[(int64_t)t.b * p.max_pages + (t.block >> p.log2_page)];
+  if ((uint32_t)page >= (uint32_t)p.n_pages) return;
+  uint8_t* const codes = reinterpret_cast<uint8_t*>(values ? p.v : p.k) + (int64_t)page * p.page_stride + (int64_t)h * p.head_stride;
+  uint8_t* const scale = (values ? c.v_scale : c.k_scale) + (((int64_t)page * p.H + h) << (p.log2_page - c.log2_block)) + (place >> c.log2_block);
+  const bool older = t.block < t.first;
+  const uint32_t before = older && work ? *scale : 0u;
 #pragma unroll
   for (int i = 0; i < kLoads; ++i)
 #pragma unroll
@@ -162,7 +162,7 @@ __device__ __forceinline__ u32x2 codes_to_fp16(uint32_t codes, float scale) {
   return (u32x2){pack2<false>(x[0], x[1]), pack2<false>(x[2], x[3])};
 }
 
-template <bool INT8>
+template <bool INT8, bool STREAM>
 __global__ __launch_bounds__(256) void k_paged8_gather(Paged8View c, const int32_t* first, uint16_t* x_k, uint16_t* x_v,
                                                       int n_max, uint32_t groups) {
   const PagedView& p = c.p;
@@ -176,13 +176,21 @@ __global__ __launch_bounds__(256) void k_paged8_gather(Paged8View c, const int32
   const int64_t src = (int64_t)page * p.page_stride + (int64_t)h * p.head_stride + (int64_t)place * p.token_stride + 8 * (i & ((1 << log2_dv) - 1));
   const int64_t block = (((int64_t)page * p.H + h) << (p.log2_page - c.log2_block)) + (place >> c.log2_block);
   const int64_t dst = (int64_t)bh * n_max * p.d + 8 * i;
-  const u32x2 k = *reinterpret_cast<const u32x2*>(reinterpret_cast<const uint8_t*>(p.k) + src);
-  const u32x2 v = *reinterpret_cast<const u32x2*>(reinterpret_cast<const uint8_t*>(p.v) + src);
+  const auto* const from_k = reinterpret_cast<const u32x2*>(reinterpret_cast<const uint8_t*>(p.k) + src);
+  const auto* const from_v = reinterpret_cast<const u32x2*>(reinterpret_cast<const uint8_t*>(p.v) + src);
+  const u32x2 k = STREAM ? __builtin_nontemporal_load(from_k) : *from_k, v = STREAM ? __builtin_nontemporal_load(from_v) : *from_v;
   const float ks = power_of(c.k_scale[block]), vs = power_of(c.v_scale[block]);
   const u32x2 k0 = codes_to_fp16<INT8>(k.x, ks), k1 = codes_to_fp16<INT8>(k.y, ks);
   const u32x2 v0 = codes_to_fp16<INT8>(v.x, vs), v1 = codes_to_fp16<INT8>(v.y, vs);
-  *reinterpret_cast<u32x4*>(x_k + dst) = (u32x4){k0.x, k0.y, k1.x, k1.y};
-  *reinterpret_cast<u32x4*>(x_v + dst) = (u32x4){v0.x, v0.y, v1.x, v1.y};
+  const u32x4 dense_k = {k0.x, k0.y, k1.x, k1.y}, dense_v = {v0.x, v0.y, v1.x, v1.y};
+  auto *const to_k = reinterpret_cast<u32x4*>(x_k + dst), *const to_v = reinterpret_cast<u32x4*>(x_v + dst);
+  if constexpr (STREAM) {
+    __builtin_nontemporal_store(dense_k, to_k);
+    __builtin_nontemporal_store(dense_v, to_v);
+  } else {
+    *to_k = dense_k;
+    *to_v = dense_v;
+  }
 }
 
 hipError_t launch_paged8_gather(const Paged8View& c, const int32_t* first, uint16_t* x_k, uint16_t* x_v, int n_max,
@@ -191,7 +199,8 @@ hipError_t launch_paged8_gather(const Paged8View& c, const int32_t* first, uint1
   auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3((uint32_t)(bh * groups)), dim3(256), 0, s, c, first, x_k, x_v, n_max, (uint32_t)groups);
   };
-  c.int8 ? launch(k_paged8_gather<true>) : launch(k_paged8_gather<false>);
+  if (4 * bh * n_max * c.p.d > kLastLevel) c.int8 ? launch(k_paged8_gather<true, true>) : launch(k_paged8_gather<false, true>);
+  else c.int8 ? launch(k_paged8_gather<true, false>) : launch(k_paged8_gather<false, false>);
   return hipGetLastError();
 }
 

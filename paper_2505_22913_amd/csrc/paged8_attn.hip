@@ -453,7 +453,8 @@ struct Unit {
   int split, splits;
   uint32_t first;  // range of the launch that its first one is
 };
-__device__ __forceinline__ bool unit_of(const Paged8AttnArgs& a, uint32_t f, int BN, Unit& u) {
+// fixed > 0: so many of every tile of rows.
+__device__ __forceinline__ bool unit_of(const Paged8AttnArgs& a, uint32_t f, int BN, uint32_t fixed, Unit& u) {
   struct Entry {
     int cu, rows, base, tiles, n;  // its row in q, rows, position of the first; tiles of rows, and of tokens that they see
   };
@@ -463,7 +464,7 @@ __device__ __forceinline__ bool unit_of(const Paged8AttnArgs& a, uint32_t f, int
     Entry e = {rt.tok0, rt.rows, rt.base, 0, 0};
     if (rt.rows > 0) {
       e.tiles = a.mixed ? rt.rows <= kFewRows : (rt.rows + kFewRows - 1) / kFewRows;
-      e.n = TileList(rt.base, rt.base + min(a.cu[b + 1], a.n_q) - rt.tok0 - 1, a.window, a.sinks, BN).n;
+      if (fixed == 0) e.n = TileList(rt.base, rt.base + min(a.cu[b + 1], a.n_q) - rt.tok0 - 1, a.window, a.sinks, BN).n;
     }
     return e;
   };
@@ -476,9 +477,9 @@ __device__ __forceinline__ bool unit_of(const Paged8AttnArgs& a, uint32_t f, int
     units += (uint32_t)e.tiles;
   }
   auto sum = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)wave_incl_scan(x), kWave - 1); };
-  const uint64_t total = sum((uint32_t)(work & 0xffffu)) + ((uint64_t)sum((uint32_t)(work >> 16)) << 16);
-  uint32_t chunk = 1, count = 0;
-  auto ranges = [&](const Entry& x) { return max(((uint32_t)x.n + chunk - 1) / chunk, 1u); };
+  uint64_t total = 0;
+  uint32_t chunk = 1, count = units * fixed;
+  auto ranges = [&](const Entry& x) { return fixed > 0 ? fixed : max(((uint32_t)x.n + chunk - 1) / chunk, 1u); };
   auto divide = [&](uint32_t by) {
     chunk = total < 0x80000000u ? ((uint32_t)total + by - 1) / by : (uint32_t)min(total / by + 1, (uint64_t)0x7fffffff);
     chunk = max(chunk, (uint32_t)(kWave / BN));
@@ -489,9 +490,12 @@ __device__ __forceinline__ bool unit_of(const Paged8AttnArgs& a, uint32_t f, int
     }
   };
   // Each request's last range may be a part of one. Where that makes too many, one for each is kept back.
-  const uint32_t budget = (uint32_t)a.budget;
-  divide(budget);
-  if (sum(count) > budget) divide(budget - min(sum(units), budget - 1));
+  if (fixed == 0) {
+    const uint32_t budget = (uint32_t)a.budget;
+    total = sum((uint32_t)(work & 0xffffu)) + ((uint64_t)sum((uint32_t)(work >> 16)) << 16);
+    divide(budget);
+    if (sum(count) > budget) divide(budget - min(sum(units), budget - 1));
+  }
   uint32_t incl = wave_incl_scan(count), want = f;
   if (want >= (uint32_t)__builtin_amdgcn_readlane((int)incl, kWave - 1)) return false;
   int at = __builtin_popcountll(ballot(incl <= want)), b = at;
@@ -543,14 +547,13 @@ __global__ __launch_bounds__(kWave) void k_paged8_rows(Paged8AttnArgs a, PartOut
   const PagedView& p = a.p;
   const int h = blockIdx.x % p.H;
   Unit u;
-  if (a.flat) {
-    if (!unit_of(a, blockIdx.x / p.H, BN, u)) return;
+  if (a.flat || !a.mixed) {
+    if (!unit_of(a, blockIdx.x / p.H, BN, a.flat ? 0u : (uint32_t)part.n_splits, u)) return;
   } else {
-    const int tile = blockIdx.x / (p.H * part.n_splits);
     u.split = (blockIdx.x / p.H) % part.n_splits;
     u.splits = part.n_splits;
-    u.rt = a.mixed ? rows_of(a, tile) : row_tile<kFewRows>(a, tile, false);
-    if (u.rt.row0 >= u.rt.rows || (a.mixed && u.rt.rows > kFewRows)) return;
+    u.rt = rows_of(a, blockIdx.x / (p.H * part.n_splits));
+    if (u.rt.rows <= 0 || u.rt.rows > kFewRows) return;
   }
   const RowTile rt = u.rt;
   // Where the results of row r of the request go if they are a range's.

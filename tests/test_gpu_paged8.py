@@ -191,6 +191,19 @@ def test_as_many_requests_as_there_can_be():
     assert bool((err <= x[:, 0].float().abs() * 2.0 ** -4 + 2.0 ** -10).all())
 
 
+@pytest.mark.parametrize("dtype,code", [(torch.float16, "e4m3"), (torch.bfloat16, "int8")])
+def test_outputs_larger_than_the_caches_are_gathered(dtype, code):
+    B, H, d, P, n_max = 2, 8, 128, 64, 35001       # 287 MB
+    lens, first = [35100, 20], [98, 0]
+    cache, ks, vs = fill8(B, H, d, P, lens, dtype, code, 32, seed=9)
+    x = [torch.full((B, H, n_max, d), 7.0, dtype=torch.float16, device="cuda") for _ in range(2)]
+    mf.mustafar_paged8_gather(cache, n_max, first=ints(first), x_k=x[0], x_v=x[1])
+    for got, want in zip(x, (ks, vs)):
+        for b, (n, f) in enumerate(zip(lens, first)):
+            m = min(n - f, n_max)
+            assert torch.equal(got[b, :, :m], want[b][:, f:f + m].half()) and bool((got[b, :, m:] == 7).all())
+
+
 # ---- attention ---------------------------------------------------------------------------------
 def attend(dtype, code, H, G, d, P, block, cached, new, window=0, sinks=0, scale=0.0, n_splits=0, seed=0, layout="heads",
            packed=False, junk=None, k_scale=0, **hints):

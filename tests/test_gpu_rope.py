@@ -71,6 +71,20 @@ def test_many_heads_whose_pairs_lie_in_no_pieces(layout, d, rot, Hq, H):
     assert torch.equal(torch.cat([q, k], 1)[..., rot:], on[..., rot:])
 
 
+@pytest.mark.parametrize("layout,rot", [("half", 128), ("interleaved", 64), ("half", 36)])
+def test_rows_that_the_caches_do_not_hold(layout, rot):
+    """Inputs and outputs of 205 MB."""
+    n, Hq, H, d = 10000, 32, 8, 128
+    x = torch.randn(n, Hq + H, d, device="cuda").half()
+    pos = torch.arange(n, device="cuda").int() * 3
+    q, k = mf.mustafar_rope(mf.Rope(rot, layout=layout), x[:, :Hq], x[:, Hq:], positions=pos)
+    rows = list(range(0, n, 397)) + [n - 1]
+    close(torch.cat([q, k], 1)[rows], x[rows], pos[rows].cpu(), oracle8.rates(rot, 10000.0), rot, layout)
+    packed = x.clone()
+    mf.mustafar_rope(mf.Rope(rot, layout=layout), packed[:, :Hq], packed[:, Hq:], positions=pos, out_q=packed[:, :Hq], out_k=packed[:, Hq:])
+    assert torch.equal(packed, torch.cat([q, k], 1))
+
+
 @pytest.mark.parametrize("scaling,kw", [("linear", dict(factor=8.0)), ("base", dict(factor=4.0)),
                                         ("turns", dict(factor=8.0, original_len=8192, low_turns=1.0, high_turns=4.0))])
 @pytest.mark.parametrize("dtype", DTYPES)
