@@ -39,7 +39,8 @@ struct Paged8Plan : PagedPlan {
   int budget;
 };
 // Waves of k_paged8_rows, where requests are divided, and the tokens of a range from which they are shared out by the requests' lengths.
-constexpr int kFew8Waves = 1024, kFlat8Tokens = 768;
+// (A wave looks at all requests then, eight a lane at most.)
+constexpr int kFew8Waves = 1024, kFlat8Tokens = 768, kFlat8Requests = 512;
 
 // Rows of the ranges' results of k_paged8_rows, 16 of each of `flat`.
 template <class Plan>
@@ -61,7 +62,7 @@ struct Kernels8 {
     const int64_t units = requests > full ? requests : full, most_units = requests + (k.mixed ? 0 : (int64_t)n_q * G / kFewRows);
     const int64_t n = kFew8Waves / (units * p.H), most = max_tokens / 64;
     k.few = (int)(n < 1 || most < 1 ? 1 : n < most ? n : most);
-    if (k.few == 1 || requests == 1 || max_tokens < kFlat8Tokens * k.few) return k;
+    if (k.few == 1 || requests == 1 || max_tokens < kFlat8Tokens * k.few || p.B > kFlat8Requests) return k;
     k.few = 2;
     k.budget = kFew8Waves / p.H;
     k.flat = k.budget > most_units ? k.budget : most_units;
@@ -80,7 +81,7 @@ hipError_t launch_paged8_attn(const Paged8AttnArgs& a, hipStream_t s);
 // has 16 tokens of a head's keys or values, the waves of a block lie in one workgroup.
 constexpr int kWrite8Threads = 256, kWrite8Rows = 16;
 inline int64_t paged8_blocks(const PagedView& p, int log2_block, int n_new) {
-  return ((int64_t)n_new >> log2_block) + 2 * (int64_t)(p.B < n_new ? p.B : n_new);
+  return ((int64_t)n_new >> log2_block) + 2 * (int64_t)p.B;
 }
 inline int paged8_block_groups(const PagedView& p, int log2_block) {
   const int heads = kWrite8Threads / kWaveSize * kWrite8Rows >> log2_block;  // of keys and values, a workgroup

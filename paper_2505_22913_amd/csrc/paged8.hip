@@ -8,8 +8,8 @@ namespace mf {
 // ------------------------------------------------------------------------------------------
 // k_paged8_write: a wave has 16 tokens of one head's keys or values, the waves of a block of tokens share a workgroup and
 // their largest magnitude. The new tokens are read once and stay in registers; the block's earlier codes are read only where the
-// new tokens raise its exponent. A workgroup's block is found in the requests' lengths, so that no two have the same one whatever
-// the step.
+// new tokens raise its exponent. A workgroup's block is found from the starts and lengths, so that no two have the same one
+// whatever the step.
 // ------------------------------------------------------------------------------------------
 struct BlockTile {
   int b, row0, first, last;  // request, the row of its first new token, the positions of its first and last
@@ -30,29 +30,15 @@ __device__ __forceinline__ BlockTile new_tokens(const PagedView& p, int b, int c
   return t;
 }
 
+// Tile `tile` of the launch. n rows are in n / T + 2 blocks of T tokens at most, so that a request's tiles begin at cu / T + 2 b and
+// the next one's behind them; a step of 4096 requests finds them as fast as one of 65.
 __device__ __forceinline__ BlockTile block_tile(const PagedView& p, const int32_t* cu, int n_new, int log2_block, int tile) {
-  const int B = p.B, lane = (int)lane_id(), stride = (B + kWave - 1) / kWave;
-  auto entry = [&](int b) { return new_tokens(p, b, cu[b], cu[b + 1], p.state[b], n_new); };
-  auto blocks = [&](int b) {
-    const BlockTile t = entry(b);
-    return t.last < t.first ? 0u : (uint32_t)((t.last >> log2_block) - (t.first >> log2_block) + 1);
-  };
-  uint32_t n = 0;
-  for (int b = lane * stride; b < min((lane + 1) * stride, B); ++b) n += blocks(b);
-  uint32_t incl = wave_incl_scan(n), want = (uint32_t)tile;
-  if (want >= (uint32_t)__builtin_amdgcn_readlane((int)incl, kWave - 1)) return {0, 0, 0, -1, 0};
-  int at = __builtin_popcountll(ballot(incl <= want));
-  want -= (uint32_t)__builtin_amdgcn_readlane((int)(incl - n), at);
-  if (stride > 1) {
-    at *= stride;
-    n = lane < stride && at + lane < B ? blocks(at + lane) : 0u;
-    incl = wave_incl_scan(n);
-    const int x = __builtin_popcountll(ballot(incl <= want));
-    want -= (uint32_t)__builtin_amdgcn_readlane((int)(incl - n), x);
-    at += x;
-  }
-  BlockTile t = entry(__builtin_amdgcn_readfirstlane(at));
-  t.block = ((t.first >> log2_block) + (int)want) << log2_block;
+  auto start = [&](int c, int b) { return (c >> log2_block) + 2 * b; };
+  const Request r = last_request(cu, p.state, p.B, [&](int c, int b) { return start(c, b) <= tile; });
+  BlockTile t = new_tokens(p, r.b, r.cu, r.next, r.len, n_new);
+  const int64_t block = ((int64_t)(t.first >> log2_block) + (tile - start(r.cu, r.b))) << log2_block;
+  if (t.last < t.first || block > t.last) return {0, 0, 0, -1, 0};
+  t.block = (int)block;
   return t;
 }
 

@@ -92,24 +92,31 @@ __device__ __forceinline__ RowTile rows_of(const PagedAttnArgs& a, int b) {
   return rows_at(a, b, __builtin_amdgcn_readfirstlane(cu), __builtin_amdgcn_readfirstlane(next), __builtin_amdgcn_readfirstlane(len));
 }
 
-// The request that holds row t of a step, its rows [cu, next) and its length: of up to 64 requests by one round of loads, else by
-// two and its own.
+// The last request that `begins` (its first row, its number) is true of, its rows [cu, next) and its length: of up to 64 requests by one
+// round of loads, else by two and its own.
 struct Request {
   int b, cu, next, len;
 };
-__device__ __forceinline__ Request request_at(const int32_t* starts, const int32_t* lens, int B, int t) {
+template <class Begins>
+__device__ __forceinline__ Request last_request(const int32_t* starts, const int32_t* lens, int B, Begins begins) {
   const int lane = (int)lane_id();
   if (B <= kWave) {
     const int b = min(lane, B - 1), cu = starts[b], next = starts[b + 1], len = lens[b];
-    const int at = 63 - __builtin_clzll(ballot(lane < B && cu <= t) | 1);
+    const int at = 63 - __builtin_clzll(ballot(lane < B && begins(cu, b)) | 1);
     return {at, __builtin_amdgcn_readlane(cu, at), __builtin_amdgcn_readlane(next, at), __builtin_amdgcn_readlane(len, at)};
   }
   const int stride = (B + kWave - 1) / kWave;
-  int b = (63 - __builtin_clzll(ballot(lane * stride < B && starts[min(lane * stride, B - 1)] <= t) | 1)) * stride;
-  const uint64_t below = ballot(lane < stride && b + lane < B && starts[min(b + lane, B - 1)] <= t);
+  int b = min(lane * stride, B - 1);
+  b = (63 - __builtin_clzll(ballot(lane * stride < B && begins(starts[b], b)) | 1)) * stride;
+  const int in = min(b + lane, B - 1);
+  const uint64_t below = ballot(lane < stride && b + lane < B && begins(starts[in], in));
   b = __builtin_amdgcn_readfirstlane(b + 63 - (int)__builtin_clzll(below | 1));
   const int cu = starts[b], next = starts[b + 1], len = lens[b];
   return {b, __builtin_amdgcn_readfirstlane(cu), __builtin_amdgcn_readfirstlane(next), __builtin_amdgcn_readfirstlane(len)};
+}
+// The request that holds row t of a step.
+__device__ __forceinline__ Request request_at(const int32_t* starts, const int32_t* lens, int B, int t) {
+  return last_request(starts, lens, B, [&](int cu, int) { return cu <= t; });
 }
 __device__ __forceinline__ RowTile request_of(const PagedAttnArgs& a, int t) {
   const Request r = request_at(a.cu, a.p.state, a.p.B, t);

@@ -338,6 +338,57 @@ def test_large_scores(dtype, code, new, k_scale):
     attend(dtype, code, 1, 4, 128, 16, 16, [300, 50], new, k_scale=k_scale, seed=6)
 
 
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("new", [[1, 2], [70, 33]])
+def test_values_under_the_normal_ones_of_fp16(code, new):
+    """Keys and values whose largest magnitude is 2^-16: nothing takes them as 0."""
+    cache, _, _ = fill8(2, 1, 64, 16, [300, 90], torch.float16, code, 16, seed=8)
+    for codes, scale in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)):
+        bits = codes.view(torch.uint8)
+        if code == "e4m3":      # 2^-15 times magnitudes up to 0.5, all over 2^-9 the smallest step's
+            scale.fill_(127 - 15)
+            bits.copy_((torch.rand_like(codes.float()) * 0.5 * (torch.rand_like(codes.float()) - 0.5).sign()).to(torch.float8_e4m3fn).view(torch.uint8))
+        else:                   # 2^-24 times whole numbers
+            scale.fill_(127 - 24)
+    ks, vs = ([tokens_of(cache, w, b).half() for b in range(2)] for w in ("k", "v"))
+    assert all(float(x.abs().max()) <= 2.0 ** -16 and float(x.abs().max()) > 2.0 ** -18 for x in ks + vs)
+    q = (torch.randn(sum(new), 2, 64, device="cuda") * 3e4).clamp(-6e4, 6e4).half()
+    got = mf.mustafar_paged8_attn(q, cache, starts(new), scale=8.0)
+    check(got, q, ks, vs, new, [300, 90], torch.float16, scale=8.0, label="small")
+    assert float(got.abs().max()) > 2.0 ** -19
+
+
+@pytest.mark.parametrize("B", [65, 257, 700, 4096])
+def test_steps_of_many_requests(B):
+    """Where a request's rows are found by two rounds of looks: rows from none to several blocks' and tiles'."""
+    H, G, d = 1, 4, 64
+    rng = random.Random(B)
+    cache = mf.PagedCache8(B, H, d, 5 * B // 2, 16, max_pages=8)
+    lens = [0] * B
+    for _ in range(2):
+        new = [rng.choice([0, 1, 1, 2, 18]) for _ in range(B)]
+        new[rng.randrange(B)] = 60
+        n = sum(new)
+        x = torch.randn(n, 2, d, device="cuda").half()
+        cu, _ = mf.mustafar_paged_plan(cache, ints(new), n)
+        assert cache.status.tolist() == [0]
+        mf.mustafar_paged8_write(cache, x[:, :1], x[:, 1:], cu)
+        q = torch.randn(n, G, d, device="cuda").half()
+        got = [mf.mustafar_paged8_attn(q, cache, cu, max_q=most, max_tokens=300) for most in (1, 60)]
+        at = 0
+        for b in range(B):
+            lens[b] += new[b]
+            if new[b] and (b % 61 == 0 or b == B - 1 or new[b] == 60):
+                ks, vs = ([tokens_of(cache, w, b).half()] for w in ("k", "v"))
+                for w, held in ((0, ks), (1, vs)):
+                    rows = x[at:at + new[b], w].float()
+                    err = (held[0][0, lens[b] - new[b]:].float() - rows).abs()
+                    assert bool((err <= rows.abs() * 2.0 ** -4 + 2.0 ** -10).all())
+                for out in got:
+                    check(out[at:at + new[b]], q[at:at + new[b]], ks, vs, [new[b]], [lens[b]], torch.float16, label=f"request {b}")
+            at += new[b]
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("code", CODES)
 @pytest.mark.parametrize("v_scale", [-90, -14, 10, 100])
