@@ -13,6 +13,13 @@ namespace mf {
 // not lie in pieces like that (rot / 2 no multiple of 8, rot of interleaved pairs none), the rows go through LDS.
 //
 // The angle is p * r in 64 bits, reduced to a part of a turn there: in 32 bits position 10^6 would be off by up to 0.06 radians.
+//
+// y = m (u cos - v sin, v cos + u sin) of a pair (u, v): 4 bytes a channel read and written for two fused operations, so memory bounds
+// it. A token's angles serve all of the workgroup's heads, whose first pieces of rows are under way while they are computed: 9600 tokens
+// of 40 heads of 128, 198 MB, take 37 us, 5.3 TB/s. Through LDS only what is turned goes, and what is not is copied at once: 20 of 80
+// channels of 4096 tokens of 64 heads, 84 MB, take 22 us, 3.8 TB/s (all channels through LDS, loaded behind the angles, 30 a call for 24.7);
+// its two barriers and the conflicts of 2-byte reads, 40% of LDS's time, are the rest. 64 tokens take 3.7 us: a chain of latencies
+// (start, length, angle, store).
 // ------------------------------------------------------------------------------------------
 // What a row's request is, of row t of a step.
 struct RopeRow {
