@@ -693,7 +693,8 @@ int mustafar_paged8_init(mustafar_pages8_t* p, void* k, void* v, void* k_scale, 
  * (int32 device, ascending from 0: mustafar_paged_plan's) divides the n_new rows of k_new
  * and v_new among the entries; the rows of entry b are its last cu[b+1] - cu[b] tokens, as
  * in mustafar_paged_attn. Rows from cu[B] on, rows before an entry's first token and tokens
- * whose page is outside [0, n_pages) are left out. k_new, v_new: p->type, layout as for
+ * whose page is outside [0, n_pages) are left out. Entries may have pages in common that
+ * none of them gets new tokens in. k_new, v_new: p->type, layout as for
  * mustafar_paged_write.
  * A block of which no earlier token is left takes its exponent from the new tokens alone.
  * One that holds earlier tokens keeps its exponent or, if the new ones need a larger one,
