@@ -513,6 +513,7 @@ __device__ __forceinline__ bool unit_of(const Paged8AttnArgs& a, uint32_t f, int
     uint32_t tiles, n;  // of rows, and of tokens that they see
   };
   constexpr int kEach = kFlat8Requests / kWave;  // requests of a lane
+  constexpr int kHalvings = 2;
   const int B = a.p.B, lane = (int)lane_id(), stride = (B + kWave - 1) / kWave;
   auto entry = [&](int b, bool is) {
     Entry e;
@@ -550,10 +551,21 @@ __device__ __forceinline__ bool unit_of(const Paged8AttnArgs& a, uint32_t f, int
     for (int i = 0; i < kEach; ++i)
       if (i < stride) count += tiles[i] * ranges(n[i]);
   };
-  // Each request's last range may be a part of one. Where that makes too many, one for each is kept back.
+  // Each request's last range may be a part of one. Where that makes too many, one for each is kept back at most, and fewer where
+  // they do: by halves, 71.3 us to 69.0 for 16 ragged requests (more than two halvings find less than they take).
   const uint32_t budget = (uint32_t)a.budget;
   divide(budget);
-  if (sum(count) > budget) divide(budget - min(sum(units), budget - 1));
+  if (sum(count) > budget) {
+    uint32_t least = budget - min(sum(units), budget - 1), most = budget;
+#pragma unroll 1
+    for (int i = 0; i < kHalvings; ++i) {
+      const uint32_t by = (least + most) / 2;
+      divide(by);
+      if (sum(count) > budget) most = by;
+      else least = by;
+    }
+    divide(least);
+  }
   uint32_t incl = wave_incl_scan(count), want = f;
   if (want >= (uint32_t)__builtin_amdgcn_readlane((int)incl, kWave - 1)) return false;
   int at = __builtin_popcountll(ballot(incl <= want)), b = at;
