@@ -105,26 +105,36 @@ struct RopeArgs {
   int B;
   int64_t most;  // tokens that an entry can hold
 };
-// A workgroup of k_rope: kRopeTokens tokens of so many heads.
-constexpr int kRopeThreads = 256, kRopeTokens = 4, kMaxRopeHeads = 1 << 16;
-enum RopeForm { kRopeHalf, kRopePairs, kRopeAny };
+// A workgroup of k_rope: kRopeTokens tokens of so many heads, each row in `pieces` of 16 bytes, the `turned` ones first (in place: those
+// alone).
+constexpr int kRopeThreads = 256, kRopeTokens = 4, kRopeHeads = 8, kMaxRopeHeads = 1 << 16;
 struct RopePlan {
-  RopeForm form;
+  int width;  // 8: a piece and the one rot / 2 channels on are turned together; 0: pieces hold their pairs; 4, 2 or 1: so many channels
+              // and those rot / 2 on, in LDS
   int heads, head_groups;
+  int turned, pieces, units;  // units: of `width` pairs, of a row
+  // x / head_groups = x * groups_inverse >> 40 (x < 2^24, head_groups <= 2^14); x / pieces = x * pieces_inverse >> 24, and so for units
+  // (x < 2^14, pieces and units under 2^8).
+  uint64_t groups_inverse;
+  uint32_t pieces_inverse, units_inverse;
   int64_t groups;
 };
 inline RopePlan rope_plan(const RopeArgs& a) {
-  const int all = a.Hq + a.H;
+  const int all = a.Hq + a.H, pairs = a.rot / 2, whole = (a.rot + 7) & ~7;
   RopePlan r;
-  const bool half = a.layout == MUSTAFAR_ROPE_HALF;
-  r.form = a.rot % (half ? 16 : 8) != 0 ? kRopeAny : half ? kRopeHalf : kRopePairs;
-  // (12 and two pieces of rows a thread where they go through LDS: 24.8 us for 26.7 with 8, a part of 20 of 80 channels of 4096
-  // tokens of 64 heads; else 8 and one piece: 41.4 us for 42.1 with 20 heads, 45.7 with two pieces, 9600 tokens of 40 heads of 128)
-  // 32 KB of LDS at most.
-  const int fit = (8192 / ((a.rot + 7) & ~7) - 8) / 2, most = r.form != kRopeAny ? 8 : fit < 12 ? fit : 12;
-  r.heads = all < most ? all : most;
+  const bool in_place = (a.Hq == 0 || a.out_q == a.q) && (a.H == 0 || a.out_k == a.k);
+  r.width = a.layout != MUSTAFAR_ROPE_HALF ? 0 : pairs % 8 == 0 ? 8 : pairs % 4 == 0 ? 4 : pairs % 2 == 0 ? 2 : 1;
+  r.turned = r.width == 8 ? pairs / 8 : whole / 8;
+  r.pieces = r.turned + (in_place ? 0 : (a.d - whole) / 8);
+  r.units = r.width ? pairs / r.width : 1;
+  // (9600 tokens of 40 heads of 128: 42.0 us with 4 heads, 38.3 with 8, 37.7 with 16, where 64 tokens take 3.6 us for 3.1; 20 of 80
+  // channels of 4096 tokens of 64 heads: 21.1 with 5, 19.8 with 8, 19.1 with 12, 25 with 16)
+  r.heads = all < kRopeHeads ? all : kRopeHeads;
   r.head_groups = (all + r.heads - 1) / r.heads;
   r.groups = ((int64_t)a.n + kRopeTokens - 1) / kRopeTokens * r.head_groups;
+  r.groups_inverse = ((uint64_t)1 << 40) / (uint64_t)r.head_groups + 1;
+  r.pieces_inverse = (1u << 24) / (uint32_t)r.pieces + 1;
+  r.units_inverse = (1u << 24) / (uint32_t)r.units + 1;
   return r;
 }
 
