@@ -464,13 +464,14 @@ __global__ __launch_bounds__(chunk_waves(T) * kWave, T == 4 ? 1 : 2) void k_page
 // tokens at d = 64 for 0.96.) The probabilities meet the values in two parts of the type: errors are an output's own rounding's.
 //
 // 2 d bytes a token and head bound it, once the waves are busy as long: 16 requests of up to 16384 tokens with 8 kv-heads of 128
-// (317 MB, int8) take 66 us, 4.8 TB/s; 16 of 16384 (537 MB, e4m3) 89.5 with the join, 6.0. One wave a SIMD: its vector
-// instructions are 41% of its time there, its waits 37%. A single request of 4096 tokens with 32 kv-heads (34 MB) takes 12 to 13 us and the
-// join 4: the chain length, page, codes, products twice, and two launches. Loads past the caches, which hold nothing that is read twice:
-// 92 us for 105 at 537 MB. Two waves a SIMD and rings of two to four tiles: within 5% for the ragged batch, 99 us for 91 with 16 heads
-// a kv-head, 31 for 23 at d = 256, 178 for 163 with 32 kv-heads; four groups of 16 tokens a tile at d = 128, or the scores of a tile
-// between the outputs of the one before: nothing gained. Ranges shared out by what the requests see: the ragged batch 85 to 69 us; where ranges are
-// short, finding them costs 2 us (17.5 to 19.5 for a window of 1024 tokens), hence kFlat8Tokens.
+// (317 MB, int8) take 62 us, 5.1 TB/s; 16 of 16384 (537 MB, e4m3) 89.5 with the join, 6.0. One wave a SIMD: its vector
+// instructions are 42% of its time there, its waits 37%. A single request of 4096 tokens with 32 kv-heads (34 MB) takes 11 to 13 us and
+// the join 4: the chain length, page, codes, products twice, and two launches. Loads past the caches, which hold nothing that is read
+// twice: 92 us for 105 at 537 MB. Two waves a SIMD: the ragged batch 85 us for 68 with the join, the even one 108 for 89, 4 requests at
+// d = 256 32 for 24.5, the single one 18.8 for 15.4; one wave for two of them: 118, 127, 23.7 and 16.9. Four groups of 16 tokens a tile at
+// d = 128, or the scores of a tile between the outputs of the one before: nothing gained. Ranges shared out by what the requests see:
+// the ragged batch 85 to 68 us; where ranges are short, finding them costs 2 us (17.5 to 19.5 for a window of 1024 tokens), hence
+// kFlat8Tokens.
 // ------------------------------------------------------------------------------------------
 template <int T>
 constexpr int rows8_groups() { return T == 1 ? 4 : 2; }  // of 16 tokens, a tile
