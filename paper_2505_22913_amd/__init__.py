@@ -722,6 +722,8 @@ def _launch(owner, stream, what="the cache is") -> int | None:
     if owner.device.index != index:
         raise ValueError(f"{what} on {owner.device}, the current device is cuda:{index}")
     if stream is not None:
+        if getattr(stream, "device_index", index) != index:
+            raise ValueError(f"the stream is on cuda:{stream.device_index}, the current device is cuda:{index}")
         return stream.cuda_stream
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     return _stream(None) if raw is None else raw(index)

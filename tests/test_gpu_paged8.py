@@ -728,3 +728,19 @@ def test_the_binding_refuses_what_does_not_fit():
         call(**kw)                                                                     # nothing to do
     torch.cuda.synchronize()
     assert torch.equal(cache.k.view(torch.uint8), held[0]) and torch.equal(cache.v_scale, held[1])
+
+
+def test_a_stream_of_another_device_is_refused():
+    """Every call on pages, and rotations, before anything is launched or made."""
+    class Elsewhere:
+        device_index = torch.cuda.current_device() + 1
+        cuda_stream = 0
+    cache, _, _ = fill8(1, 1, 64, 16, [5], torch.float16, "int8", 16, seed=51)
+    dense = mf.PagedCache(1, 1, 64, 1, 16)
+    x, cu = torch.zeros(1, 1, 64, dtype=torch.float16, device="cuda"), starts([1])
+    other = Elsewhere()
+    for call in (lambda: mf.mustafar_paged8_write(cache, x, x, cu, stream=other), lambda: mf.mustafar_paged8_gather(cache, 4, stream=other),
+                 lambda: mf.mustafar_paged8_attn(x, cache, cu, stream=other), lambda: mf.mustafar_paged_attn(x, dense, cu, stream=other),
+                 lambda: mf.mustafar_rope(mf.Rope(64), x, x, ints([0]), stream=other)):
+        with pytest.raises(ValueError, match="stream"):
+            call()
