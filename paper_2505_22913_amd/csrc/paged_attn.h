@@ -209,6 +209,14 @@ struct RowState {
   float m, l, o[T];  // o: channels lane + 64 c
 };
 
+// Sums of bf16 values leave fp32 where their mean, the output, does not. So weights are at most 2^-one_below() here, 1 over
+// more than twice the tokens' number, and a sum is no larger than half the largest value. (It costs the smallest values precision:
+// products under 2^-126 are multiples of 2^-149, so that the output of n tokens is off by up to 4 n^2 2^-150.)
+template <bool BF16>
+__device__ __forceinline__ float one_below(TileList tl, int BN) {
+  return BF16 ? (float)(64 - __builtin_clz(tl.n | 1) - __builtin_clz(BN)) : 0.f;
+}
+
 // A token's key and value in 16-bit pages; `held` is what a lane keeps of its token, `passed` what one lane gets of another's.
 template <bool BF16>
 struct Pages16 {
@@ -228,6 +236,7 @@ __device__ __forceinline__ RowState<T> one_row(const PagedAttnArgs& a, const Pag
   constexpr int d = kTile * T;
   const PagedView& p = a.p;
   const int lane = (int)lane_id();
+  const float below = one_below<BF16>(tl, BN);
   RowState<T> s;
   s.m = -INFINITY;
   s.l = 0.f;
@@ -246,7 +255,7 @@ __device__ __forceinline__ RowState<T> one_row(const PagedAttnArgs& a, const Pag
     }
     const float mnew = fmaxf(s.m, wave_max(x));
     const float alpha = s.m == -INFINITY ? 1.f : at_least(__builtin_amdgcn_exp2f((s.m - mnew) * a.scale_log2));
-    const float w = x == -INFINITY ? 0.f : at_least(__builtin_amdgcn_exp2f((x - mnew) * a.scale_log2));
+    const float w = x == -INFINITY ? 0.f : at_least(__builtin_amdgcn_exp2f(fmaf(x - mnew, a.scale_log2, -below)));
     s.m = mnew;
     s.l = fmaf(s.l, alpha, wave_sum(w));
     for (int c = 0; c < T; ++c) s.o[c] *= alpha;
@@ -291,8 +300,10 @@ __device__ __forceinline__ void redo_rows(const PagedAttnArgs& a, const Pages& p
     if (part.n_splits > 1) {
       const int64_t row = result_at(r);
       // (what the maximum's rounding leaves goes into the sums: other ranges' are multiples of 2^m with theirs. Beyond 2^27 scores
-      // of fp32 differ by more than 2^8 or not at all.)
-      const float m = s.m * a.scale_log2, f = __builtin_amdgcn_exp2f(fminf(fmaxf(fmaf(s.m, a.scale_log2, -m), -8.f), 8.f));
+      // of fp32 differ by more than 2^8 or not at all. bf16: a factor of up to 2^8 is room that m gives the sums.)
+      const float below = one_below<BF16>(tl, BN), more = BF16 && fabsf(s.m * a.scale_log2) >= 0x1p24f ? 8.f : 0.f;
+      const float m = fmaf(s.m, a.scale_log2, below + more), left = fmaf(s.m, a.scale_log2, -m) + below;
+      const float f = __builtin_amdgcn_exp2f(fminf(fmaxf(left, -more - 8.f), -more + 8.f));
       if (lane == 0) part.ml[row] = make_float2(m, pos < 0 ? -1.f : s.l * f);
       for (int c = 0; c < T; ++c) part.o[row * d + kTile * c + lane] = s.o[c] * f;
     } else {
@@ -322,6 +333,8 @@ __device__ __forceinline__ void merge_row(const PagedAttnArgs& a, const float2* 
       if (s0 + kStep * k < n_splits) x[k] = *reinterpret_cast<const f32x4*>(o_of + ((s0 + kStep * k) * rows + row) * d + 4 * sub);
   };
   load(first);
+  // (bf16: ranges' outputs may be as large as fp32 holds; times less than 1 part in their number, so is their sum)
+  const float down = BF16 ? __builtin_bit_cast(float, (uint32_t)(95 + __builtin_clz(n_splits)) << 23) : 1.f;
   float M = -INFINITY, l = 0.f;
   for (int s = at; s < n_splits; s += OF) M = fmaxf(M, ml[s * rows + row].x);
 #pragma unroll
@@ -331,7 +344,7 @@ __device__ __forceinline__ void merge_row(const PagedAttnArgs& a, const float2* 
     // lane i of those: the weight of range s0 + i, 0 for one without any (its output is not looked at)
     float2 of = make_float2(-INFINITY, 0.f);
     if (s0 + at < n_splits) of = ml[(s0 + at) * rows + row];
-    const float w = of.x != -INFINITY || of.y != 0.f ? at_least(__builtin_amdgcn_exp2f(of.x - M)) : 0.f;
+    const float w = of.x != -INFINITY || of.y != 0.f ? at_least(__builtin_amdgcn_exp2f(of.x - M)) * down : 0.f;
     if (w != 0.f) l = fmaf(of.y, w, l);
     nothing |= ballot(of.y < 0.f);
     const int end = min(s0 + OF, n_splits);
