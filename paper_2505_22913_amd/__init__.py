@@ -707,13 +707,6 @@ def _page_state(B, n_pages, max_pages, device, table, state, free):
     return table, state, free
 
 
-def _current(cache):
-    """The cache's device has to be the current one: the launches go there."""
-    import torch
-    if cache.device.index != torch.cuda.current_device():
-        raise ValueError(f"the cache is on {cache.device}, the current device is cuda:{torch.cuda.current_device()}")
-
-
 def _launch(owner, stream, what="the cache is") -> int | None:
     """Raw handle of `stream`, or of torch's current stream, for a call on tensors of the owner's device, which has to be the
     current one (one look-up of it for both)."""
@@ -767,7 +760,7 @@ def mustafar_paged_plan(cache: PagedCache, new_len, n_slots: int, keep=None, sta
     status before the results."""
     import torch
     B, i32 = cache.desc.B, torch.int32
-    _current(cache)
+    handle = _launch(cache, stream)
     with _on_stream(stream):
         cu = torch.empty(B + 1, dtype=i32, device=cache.device) if cu is None else cu
         slots = torch.empty(n_slots, dtype=i32, device=cache.device) if slots is None else slots
@@ -779,7 +772,7 @@ def mustafar_paged_plan(cache: PagedCache, new_len, n_slots: int, keep=None, sta
             _want(name, x, (n,), i32, cache.device)
     _check("mustafar_paged_plan", lib().mustafar_paged_plan(
         ctypes.byref(cache.desc), _dptr(keep), _dptr(new_len), _dptr(state_out), _dptr(cu), _dptr(slots),
-        int(n_slots), _dptr(status), _stream(stream)))
+        int(n_slots), _dptr(status), handle))
     return cu, slots
 
 
@@ -788,11 +781,11 @@ def mustafar_paged_write(cache: PagedCache, k_new, v_new, slots, stream=None) ->
     [n] (int32; negative: left out)."""
     import torch
     n, H = k_new.shape[0], cache.desc.H
-    _current(cache)
+    handle = _launch(cache, stream)
     ks, vs = _rows("k_new", k_new, n, H, cache), _rows("v_new", v_new, n, H, cache)
     _want("slots", slots, (n,), torch.int32, cache.device)
     _check("mustafar_paged_write", lib().mustafar_paged_write(
-        ctypes.byref(cache.desc), _dptr(k_new), ks, _dptr(v_new), vs, _dptr(slots), n, _stream(stream)))
+        ctypes.byref(cache.desc), _dptr(k_new), ks, _dptr(v_new), vs, _dptr(slots), n, handle))
 
 
 def mustafar_paged_gather(cache: PagedCache, n_max: int, first=None, x_k=None, x_v=None, stream=None):

@@ -390,3 +390,24 @@ def test_a_captured_call_that_makes_its_own_tensors_replays(dtype, new):
         torch.cuda.synchronize()
         assert torch.equal(got, want) and bool((got[-3:] == 0).all()), r
         assert all(c.status.tolist() == [0] for c in caches) and torch.equal(caches[0].state, caches[1].state)
+
+
+# ---- streams -------------------------------------------------------------------------------------------
+def test_plans_and_writes_refuse_a_stream_of_another_device():
+    """Before anything is launched or made: tables, state, stack, status and pages stay as they were."""
+    class Elsewhere:
+        device_index = torch.cuda.current_device() + 1
+        cuda_stream = 0
+    cache, _, _ = fill(2, 1, 64, 16, [20, 3], torch.float16, seed=99)
+    cache.status.fill_(7)
+    held = [x.clone() for x in (cache.k, cache.v, cache.table, cache.state, cache.free, cache.status)]
+    x, ints = torch.zeros(2, 1, 64, dtype=torch.float16, device="cuda"), lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    for call in (lambda: mf.mustafar_paged_plan(cache, ints([1, 1]), 2, stream=Elsewhere()),
+                 lambda: mf.mustafar_paged_write(cache, x, x, ints([0, 1]), stream=Elsewhere()),
+                 lambda: mf.mustafar_paged_gather(cache, 4, stream=Elsewhere()),
+                 lambda: mf.mustafar_paged_attn(x, cache, starts([1, 1]), stream=Elsewhere())):
+        with pytest.raises(ValueError, match="stream"):
+            call()
+    torch.cuda.synchronize()
+    for now, was in zip((cache.k, cache.v, cache.table, cache.state, cache.free, cache.status), held):
+        assert torch.equal(now, was)
