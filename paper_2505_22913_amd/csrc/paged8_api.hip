@@ -112,9 +112,12 @@ int mustafar_rope_rates(double* rates, int rot, double base, int scaling, double
   if (!isfinite(base) || base <= 0 || scaling < MUSTAFAR_ROPE_PLAIN || scaling > MUSTAFAR_ROPE_TURNS) return MUSTAFAR_EINVAL;
   if (scaling == MUSTAFAR_ROPE_PLAIN) factor = 1;
   if (!isfinite(factor) || factor <= 0) return MUSTAFAR_EINVAL;
+  double slower = 1;  // factor's part of the rates is slower^(-2 i / (rot - 2)) where the enlarged base is no normal number
   if (scaling == MUSTAFAR_ROPE_BASE) {
     if (rot == 2) return MUSTAFAR_EINVAL;
-    base *= pow(factor, (double)rot / (rot - 2));
+    const double enlarged = base * pow(factor, (double)rot / (rot - 2));
+    if (isnormal(enlarged)) base = enlarged;
+    else slower = factor;
     factor = 1;
   }
   const bool turns = scaling == MUSTAFAR_ROPE_TURNS;
@@ -124,6 +127,7 @@ int mustafar_rope_rates(double* rates, int rot, double base, int scaling, double
   double r[MUSTAFAR_ROPE_MAX_D / 2];
   for (int i = 0; i < rot / 2; ++i) {
     r[i] = pow(base, -2.0 * i / rot);
+    if (slower != 1) r[i] *= pow(slower, -2.0 * i / (rot - 2));
     double keep = 0;
     if (turns) {
       keep = (original_len * r[i] / (2 * M_PI) - low_turns) / (high_turns - low_turns);

@@ -150,6 +150,18 @@ def test_rates_are_the_formulas(lib, rot, scaling, kw):
         assert got[0] == 1 and abs(got[-1] * kw["factor"] / 10000.0 ** (-(rot - 2) / rot) - 1) < 1e-12
 
 
+@pytest.mark.parametrize("rot,base,factor", [(8, 1e300, 1e10), (4, 1e160, 1e100), (64, 1e307, 16.0), (128, 1e-300, 1e-7), (6, 1e-200, 1e-100),
+                                             (64, 1e300, 1e-280)])
+def test_an_enlarged_base_beyond_doubles_range_has_its_rates(lib, rot, base, factor):
+    """base * factor^(rot / (rot - 2)) may leave fp64's range where its powers do not (the last pair's exponent is under 1): their logarithms,
+    off by 2^-52 of themselves, which are under 1500, and as little from the powers' own roundings."""
+    got = mf.mustafar_rope_rates(rot, base, "base", factor=factor)
+    for i, r in enumerate(got):
+        want = -2 * i / rot * (math.log(base) + rot / (rot - 2) * math.log(factor))
+        assert r > 0 and abs(math.log(r) - want) <= 8 * 1500 * 2.0 ** -52, (i, r, want)
+    assert got[0] == 1 and all(a > b if base > 1 else a < b for a, b in zip(got, got[1:]))
+
+
 def test_rates_refuse(lib):
     out = (ctypes.c_double * 256)(*[7.0] * 256)
     call = lambda rot=64, base=1e4, scaling=0, factor=2.0, L=4096.0, low=1.0, high=4.0, r=out: lib.mustafar_rope_rates(  # noqa: E731
