@@ -11,6 +11,7 @@ from oracle import paged8 as oracle8
 from tests.gpu_common import ATTN_TOL, announce, attn_error
 from tests.paged8_common import CODE, KIND, check, fill8, ints, tokens_of
 from tests.paged_common import starts
+from tests.test_gpu_paged_edges import causal, exact_scores, half_step, softmax_of
 
 pytestmark = pytest.mark.gpu
 
@@ -744,3 +745,51 @@ def test_a_stream_of_another_device_is_refused():
                  lambda: mf.mustafar_rope(mf.Rope(64), x, x, ints([0]), stream=other)):
         with pytest.raises(ValueError, match="stream"):
             call()
+
+
+# ---- the weights' precision ----------------------------------------------------------------------
+def whole_keys(cache, code):
+    """Keys that are whole numbers up to 3, of exponent 0, in every page."""
+    x = torch.randint(-3, 4, tuple(cache.k.shape), generator=torch.Generator().manual_seed(5)).float()
+    cache.k.copy_(x.to(CODE[code]).cuda())
+    cache.k_scale.fill_(127)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("H,G", [(4, 1), (2, 4), (1, 16)])
+@pytest.mark.parametrize("hints", [dict(n_splits=1), dict(n_splits=5), dict(max_tokens=400000), dict(max_q=2, max_tokens=400000)])
+def test_single_tokens_weights_are_not_rounded_to_the_type(dtype, code, d, H, G, hints):
+    """Tokens whose output is off by no more than its own rounding and what 2 parts of the type leave of the weights.
+
+    q and k are whole numbers up to 3, so every score is exact in fp32, and values are numbers of the type. A weight 2^x, x up to 8 in
+    magnitude, is off by ln 2 (2^-20 + 8 2^-24) from x's last rounding and the scale's, 2^-22 from the exponential, and from its two
+    parts by u^2 (u = half a step of the type; of fp16 also 2^-25 where the reference's is 2^7). The sums over the tokens add
+    (n + 32) 2^-24, and the normalised weights are off by twice all that.
+
+    That bound is the sums' worst case. Independent roundings to nearest are off by half a step over sqrt(3) in the 2-norm: of 768 outputs
+    and more that is within 15%, six standard deviations (the other errors are under a hundredth), where one rounding of each weight to the
+    type makes 1.3 to 1.5 times as much of 650 weights of a like size."""
+    lens, scale = [700, 650, 603], 2.0 ** -7
+    announce(f"weights8 {dtype} {code} d={d} H={H} G={G} {hints}")
+    cache, _, vs = fill8(3, H, d, 16, lens, dtype, code, 16, seed=d + G)
+    whole_keys(cache, code)
+    ks = [tokens_of(cache, "k", b) for b in range(3)]
+    q = torch.randint(-3, 4, (3, H * G, d), generator=torch.Generator().manual_seed(d)).to(dtype)
+    got = mf.mustafar_paged8_attn(q.cuda(), cache, starts([1, 1, 1]), scale=scale, **hints).double().cpu()
+    u, errors, steps = torch.finfo(dtype).eps / 2, [], []
+    for b, m in enumerate(lens):
+        score = exact_scores(q[b:b + 1], ks[b].cpu(), scale)
+        assert float(score.abs().max()) < 4 * 0.69
+        v = vs[b].cpu()
+        want, mean = softmax_of(score, v, causal(1, m, "cpu"))
+        rel = 0.6932 * (2.0 ** -20 + 8 * 2.0 ** -24) + 2.0 ** -22 + u * u + (m + 32) * 2.0 ** -24
+        least = m * 2.0 ** -32 * float(v.abs().max()) + 2.0 ** -25 if dtype == torch.float16 else 0.0
+        errors.append(got[b:b + 1] - want)
+        steps.append(half_step(want, dtype))
+        worst = float((errors[-1].abs() / (steps[-1] + 2 * rel * mean * (1 + u) + 2 * least)).max())
+        assert worst <= 1, f"request {b}: an element is {worst:.2f} of its bound off"
+    rms = float(torch.cat(errors).norm() / torch.cat(steps).norm()) * 3 ** 0.5
+    announce(f"  2-norm: {rms:.3f} of the output's roundings'")
+    assert rms <= 1.15
