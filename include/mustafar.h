@@ -640,7 +640,7 @@ size_t mustafar_paged_attn_workspace_bytes(const mustafar_pages_t* p, int Hq, in
  * entries of pages that no row sees need not be valid. (An entry outside [0, n_pages)
  * is read as page 0, and a length as at most max_pages * P.) Infinities and NaN of a
  * token reach the rows that see it and no other; rows near one are computed one by one
- * (a prompt of 4096 tokens with 32 heads takes up to 46 ms for 0.17). For the product with the
+ * (a prompt of 4096 tokens with 32 heads takes up to 51 ms for 0.17). For the product with the
  * values a probability is the sum of two numbers of the cache's type where the call's
  * requests have at most 16 rows a kv-head (their tokens times Hq/H: single tokens), and
  * rounded to the type where they have more; the softmax's maximum, sum and output are
@@ -740,7 +740,10 @@ enum mustafar_rope_scaling {
     MUSTAFAR_ROPE_TURNS = 3     /* r_i (g + (1 - g) / factor) with g = (n - low) / (high - low)
                                  * within [0, 1], n = original_len r_i / (2 pi) the turns that
                                  * the pair makes in original_len tokens: pairs of `high`
-                                 * turns and more stay, those of `low` and fewer are divided */
+                                 * turns and more stay, those of `low` and fewer are divided,
+                                 * linearly in their turns between (not in the pair's index
+                                 * between two rounded bounds, another rule that is in use:
+                                 * its rates are the caller's own)                           */
 };
 #define MUSTAFAR_ROPE_MAX_D 512
 
@@ -754,7 +757,7 @@ typedef struct mustafar_rotation {
 /* rates [rot / 2] (HOST memory) of a mustafar_rotation. factor > 0 (not looked at in
  * PLAIN), original_len > 0 and low < high in TURNS alone. Errors: EINVAL (also rot < 2 or
  * odd or over MUSTAFAR_ROPE_MAX_D, a base or factor that is not finite and over 0, rates
- * that are not finite). */
+ * that are not finite; a base that BASE enlarges beyond double's range has its rates). */
 int mustafar_rope_rates(double* rates, int rot, double base, int scaling, double factor,
                         double original_len, double low_turns, double high_turns);
 

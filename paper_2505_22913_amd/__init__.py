@@ -968,7 +968,8 @@ def mustafar_rope_rates(rot: int, base: float = 10000.0, scaling: str = "plain",
                         original_len: float = 0.0, low_turns: float = 1.0, high_turns: float = 32.0) -> list:
     """Radians per position of the rot / 2 pairs. scaling: "plain" (base**(-2 i / rot)), "linear" (divided by factor),
     "base" (a larger base, so that the slowest is divided by factor) or "turns" (pairs of up to low_turns turns in original_len
-    tokens are divided by factor, those of high_turns and more stay, the others lie between)."""
+    tokens are divided by factor, those of high_turns and more stay, the others lie between, linearly in their turns). A model
+    whose rule is another, such as a ramp in the pair's index between two rounded bounds, passes its own rates to Rope."""
     if scaling not in ROPE_SCALINGS:
         raise ValueError(f"scaling is one of {', '.join(ROPE_SCALINGS)}, not {scaling!r}")
     rates = (ctypes.c_double * max(1, int(rot) // 2))()
@@ -1000,7 +1001,9 @@ def mustafar_rope(rope: Rope, q, k=None, positions=None, cache=None, cu=None, in
                   stream=None):
     """q [n][Hq][d] and k [n][H][d] (float16 or bfloat16; rows of a packed projection too; k may be None) turned by
     their positions [n] (int32), or by those of a planned step's new tokens: cache (a PagedCache or PagedCache8) and cu. Rows
-    from cu[B] on are left as they were, 0 in tensors that the call makes. inverse: turned back, which is the gradient.
+    from cu[B] on are left as they were, 0 in tensors that the call makes. inverse: turned back, which is the gradient (autograd
+    does not see the call: what it returns requires no gradient, so that training calls it in a torch.autograd.Function of its
+    own, whose backward is the call with inverse=True).
     Returns (out_q, out_k), new tensors unless given; out_q=q, out_k=k turns in place."""
     import torch
     dtype, device = q.dtype, rope.device

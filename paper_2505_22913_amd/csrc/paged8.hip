@@ -144,7 +144,7 @@ hipError_t launch_paged8_write(const Paged8View& c, const uint16_t* k_new, int64
 // ------------------------------------------------------------------------------------------
 // k_paged8_gather: 8 codes of a key row and of its value row a thread, a head's rows a run of workgroups.
 //
-// 1 byte read and 2 written a channel, so memory bounds it: 166 + 331 MB take 85 to 90 us, 5.5 to 5.8 TB/s, past the last cache, which cannot hold
+// 1 byte read and 2 written a channel, so memory bounds it: 166 + 331 MB take 85 to 92 us, 5.4 to 5.8 TB/s, past the last cache, which cannot hold
 // them for their reader (through it 100 us); 25 MB, which it holds, 6.3 us, 3.9 TB/s with the launch's start and end.
 // ------------------------------------------------------------------------------------------
 template <bool INT8>

@@ -59,8 +59,8 @@ __device__ __forceinline__ int range_start(int n, int s, int of) {
 // the barrier, and the one that is written) and two of values.
 //
 // 4 d flops a visible pair bound it, and the matrix and vector units hardly work at once: 4 prompts of 4096 tokens with 32 heads of 128
-// (550 GFLOP, e4m3, bf16) 566 to 590 us, 0.93 to 0.97 PFLOP/s, where a product of 8192^3 reaches 1.25; 512 rows of 4 heads a kv-head
-// behind 16384 tokens (int8, fp16) 151 to 159 with their join. The same from 16-bit pages: 548 to 567 and 148 to 153; the difference
+// (550 GFLOP, e4m3, bf16) 566 to 604 us, 0.91 to 0.97 PFLOP/s, where a product of 8192^3 reaches 1.25; 512 rows of 4 heads a kv-head
+// behind 16384 tokens (int8, fp16) 151 to 165 with their join. The same from 16-bit pages: 548 to 568 and 148 to 155; the difference
 // is the conversion, 27% more vector instructions, and its stores to LDS (a sixth of LDS's cycles are their conflicts). With 16
 // rows a wave that converts its operands for itself they took 1766 us and 897. The probabilities are rounded to the type once:
 // errors against 64 bits 0.0021 for 0.0016 in bf16, 0.00029 for 0.00021 in fp16 (2-norms, relative); in two parts the products of the

@@ -196,8 +196,8 @@ __device__ __forceinline__ bool sees(int pos, int j, int window, int n_sinks) {
 // the row does not see. The kernels below come here with the rows of a wave whose result is not
 // finite: their matrix products take whole tiles, so that a value that is not finite reaches
 // the rows that do not see it (0 times infinity). Latency bounds it, a row of 4096 tokens takes more than a millisecond: a
-// prompt of 4096 with 32 heads, 170 us, takes 29 ms where every row of one head sees an infinity, 46 where those of all do, 42
-// where only the last row does.
+// prompt of 4096 with 32 heads, 170 us, takes 29 to 31 ms where every row of one head sees an infinity, 46 to 51 where those of all do,
+// 42 to 44 where only the last row does.
 // ------------------------------------------------------------------------------------------
 // The least weight of a visible token: an infinite value that one sees stays infinite
 // where its probability is under fp32's range (0 times infinity would be NaN).

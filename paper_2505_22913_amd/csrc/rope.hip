@@ -16,7 +16,7 @@ namespace mf {
 //
 // y = m (u cos - v sin, v cos + u sin) of a pair (u, v): 4 bytes a channel read and written for two fused operations, so memory bounds
 // it. A token's angles serve all of the workgroup's heads, whose first pieces are under way while they are computed: 9600 tokens of 40
-// heads of 128, 198 MB, take 35 us (38 one launch behind the other), 5.6 TB/s. Through LDS 20 of 80 channels of 4096 tokens of 64 heads, 84 MB, take 18 to 23 us, 3.6 to 4.7 TB/s:
+// heads of 128, 198 MB, take 35 us (38 one launch behind the other), 5.6 TB/s, interleaved or in halves. Through LDS 20 of 80 channels of 4096 tokens of 64 heads, 84 MB, take 18 to 23 us, 3.6 to 4.7 TB/s:
 // the rest of a row is copied past it, and the pairs are turned where they lie (each piece gathering its partners by itself there took
 // 24.6, without LDS by loads and stores of W channels 57: their number). Divisions are products with inverses from the host: 38.3 us for 40.5 and
 // 3.1 for 3.3 with 64 tokens, which are a chain of latencies (start, length, angle, store).
