@@ -611,6 +611,9 @@ __global__ __launch_bounds__(kWave) void k_paged8_rows(Paged8AttnArgs a, PartOut
   // int8 codes become whole numbers of the type without their scale, which multiplies the scores and, in bf16, whose exponents have
   // room for it, the probabilities: fewer instructions than to multiply them.
   constexpr bool kScaled = INT8 && BF16;
+  // Such sums of codes leave fp32 for queries of 2^113 and more, and one of -inf is a weight of 0 whatever the score. Rows with a query
+  // whose square leaves it, of 2^64 and more, are done by themselves, with keys that have their scale.
+  bool beyond = false;
   constexpr uint32_t kHalf = 1024 * kLoads, kSlot = 2 * kHalf;     // bytes of each, of a tile
   __shared__ __align__(1024) unsigned char smem[R * kSlot];
   const PagedView& p = a.p;
@@ -811,6 +814,17 @@ __global__ __launch_bounds__(kWave) void k_paged8_rows(Paged8AttnArgs a, PartOut
 #pragma unroll
     for (int i = 0; i < R; ++i)
       if (i < n) stage(i, i);
+    if constexpr (kScaled) {
+      // (the first tiles are under way)
+      float squares[2] = {};
+#pragma unroll
+      for (int i = 0; i < 4 * NC; ++i) {
+        const uint32_t pair = qb[i / 4][i % 4];
+        const bf16x2 x = __builtin_bit_cast(bf16x2, pair);
+        squares[i % 2] = __builtin_amdgcn_fdot2_f32_bf16(x, x, squares[i % 2], false);
+      }
+      beyond = !(squares[0] + squares[1] < INFINITY);
+    }
     int slot = 0;
     for (int t = 0; t < n; ++t) {
       // The tile's loads have arrived; those of the tiles behind it are under way.
@@ -836,7 +850,7 @@ __global__ __launch_bounds__(kWave) void k_paged8_rows(Paged8AttnArgs a, PartOut
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (rt.row0 + (int)(4 * q4) + e < rt.rows) z = fmaf(o[c][e], 0.f, z);
-  if (ballot(z != z || (rt.row0 + (int)r16 < rt.rows && fabsf(shift) >= kFar<BF16>))) {
+  if (ballot(z != z || (rt.row0 + (int)r16 < rt.rows && (beyond || fabsf(shift) >= kFar<BF16>)))) {
     redo_rows<T, BF16>(a, Pages8<INT8>{a}, part, rt, h, rt.row0, kFewRows, tl, t0, t0 + n, result_at, BN);
     return;
   }

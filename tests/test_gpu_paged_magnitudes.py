@@ -112,3 +112,26 @@ def test_equal_scores_of_any_size(d, n, n_splits, bits):
         tol = U * x.mean(0).abs() + 2 * (L + 32) * 2.0 ** -24 * x.abs().mean(0) * (1 + U)
         worst = ((got[i] - x.mean(0)).abs() / tol).amax(0)
         assert float(worst.max()) <= 1, f"row {i}: {[float(worst[c::4].max()) for c in range(4)]} of the bound, by channel"
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "int8"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("new", [[1, 1, 1], [33, 1, 5]])
+@pytest.mark.parametrize("hints", SPLITS)
+@pytest.mark.parametrize("sign", [-1.0, 1.0, 0.0])
+def test_large_queries_over_small_keys(kind, d, new, hints, sign):
+    """A query's channel of 2^122 over keys of 2^-104, whose codes' sums alone leave fp32: scores of one sign or both, around 1 by a scale
+    of 2^-18; the other channels' products are under 2^-100 of that."""
+    H, G, lens = 2, 2, [400, 40, 9]
+    announce(f"large queries {kind} d={d} new={new} {hints} sign={sign}")
+    g = torch.Generator().manual_seed(d)
+    ks, vs = [[torch.randn(H, n, d, generator=g) for n in lens] for _ in range(2)]
+    for k in ks:
+        k *= 2.0 ** -105
+        if sign:
+            k[..., 3] = sign * k[..., 3].abs()
+    cache, attn, check, ks, vs = held(kind, [k.to(BF16) for k in ks], [v.to(BF16) for v in vs])
+    q = torch.randn(sum(new), H * G, d, generator=g)
+    q[..., 3] = 2.0 ** 122
+    q = q.to(BF16).cuda()
+    check(attn(q, cache, starts(new), scale=2.0 ** -18, **hints), q, ks, vs, new, lens, BF16, scale=2.0 ** -18, label="large queries")
