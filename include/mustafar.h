@@ -643,8 +643,8 @@ size_t mustafar_paged_attn_workspace_bytes(const mustafar_pages_t* p, int Hq, in
  * (a prompt of 4096 tokens with 32 heads takes up to 51 ms for 0.17). For the product with the
  * values a probability is the sum of two numbers of the cache's type where the call's
  * requests have at most 16 rows a kv-head (their tokens times Hq/H: single tokens), and
- * rounded to the type where they have more; the softmax's maximum, sum and output are
- * held in fp32. Errors: EINVAL (also: sizes and n_splits that make a launch of 2^32
+ * rounded to the type where they have more; q.k, before its scale, the softmax's
+ * maximum, its sum and the output are held in fp32. Errors: EINVAL (also: sizes and n_splits that make a launch of 2^32
  * threads), EUNSUPPORTED (Hq/H over MUSTAFAR_PAGED_MAX_GROUP), EWORKSPACE. */
 int mustafar_paged_attn(const void* q, int64_t q_stride, int n_q, int Hq, const mustafar_pages_t* p,
                         const void* cu, int window, int sinks, float scale, void* out,
